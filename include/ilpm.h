@@ -1,5 +1,6 @@
 /*
- * ilpm.h -- batch-1 2-D convolution forward pass on AMD MI355X (gfx950).
+ * ilpm.h -- batch-1 2-D convolution forward pass on AMD MI355X (gfx950), and
+ * the operators between the projections of a token-by-token decoder step.
  *
  * The operation (ILP-M, Section 4 and Algorithm 2 of "ILP-M Conv: Optimize
  * Convolution Algorithm for Single-Image Convolution Neural Network Inference
@@ -29,7 +30,7 @@
  *
  * Conventions for every entry point:
  *   - Tensor pointers are DEVICE pointers to contiguous fp32 arrays, 4-byte
- *     aligned, on the current HIP device.  The caller owns (allocates and
+ *     aligned, on the current HIP device (the decoder-step operators: see there).  The caller owns (allocates and
  *     frees) them; the library keeps no tensor pointer after a call returns.
  *   - Work is only enqueued on `stream` (NULL = the default stream); no call
  *     synchronises the host.  A device-side fault shows up at the caller's
@@ -57,7 +58,8 @@ enum {
     ILPM_OK = 0,
     ILPM_ERR_INVALID_ARG = -1, /* null pointer, dimension <= 0, stride <= 0, pad < 0,
                                   no output pixel, out overlapping an input, bad plan */
-    ILPM_ERR_UNSUPPORTED = -2, /* a tensor above 2^31-1 elements */
+    ILPM_ERR_UNSUPPORTED = -2, /* a tensor above 2^31-1 elements; decoder-step operators: element types
+                                  or sizes that they do not take */
     ILPM_ERR_WORKSPACE = -3,   /* registered workspace smaller than the plan needs, or the
                                   library's own would have to grow during graph capture */
     ILPM_ERR_HIP = -4,         /* a HIP runtime call or kernel launch failed */
@@ -415,6 +417,156 @@ int ilpm_relu_inplace(float *x, int64_t n, hipStream_t stream);
  * in [C, H, W] -> out [C, H/2, W/2] (floor).  Requires H, W >= 2; no overlap.
  */
 int ilpm_maxpool2x2(const float *in, int C, int H, int W, float *out, hipStream_t stream);
+
+/* ---- a decoder step: paged cache, attention of single tokens, norms ----
+ *
+ * The operators between the projections of a language model's decoder layer
+ * when it answers token by token (a projection of one token is a 1x1
+ * convolution of a 1x1 map).  Keys and values of the tokens so far live in
+ * pages of a pool; a page table names each sequence's pages in order.
+ *
+ * They follow the conventions above, with these additions: tensors have the
+ * element type that their `dtype` names, are aligned to it and may be strided
+ * as stated (strides in elements, not negative; the innermost dimension is
+ * contiguous).  What a call writes must not overlap what it reads or else
+ * writes, except where a comment allows it, and must not overlap itself.
+ * Arithmetic and sums are fp32 or more; each output is rounded to its type
+ * once, to nearest even.  Sizes of zero tokens, sequences or rows are valid
+ * and launch nothing.
+ *
+ * What lies in device memory cannot be checked before a launch.  The kernels
+ * check lengths, positions, sequence numbers and page numbers themselves and
+ * never touch memory outside the tensors that they were given; what each does
+ * with a value out of range is stated there.
+ */
+enum { ILPM_F32 = 0, ILPM_F16 = 1, ILPM_BF16 = 2 };
+
+/* Rows of heads: element (row, head, i) at data[row * row_stride + head * head_stride + i], i < head_dim. */
+typedef struct ilpm_heads {
+    void *data;
+    int64_t row_stride, head_stride;
+    int dtype; /* ILPM_F32, ILPM_F16 or ILPM_BF16 */
+    int heads;
+} ilpm_heads;
+
+/*
+ * A paged cache: token p of sequence s, p < max_pages * page_size, is slot
+ * p % page_size of page page_table[s * table_stride + p / page_size]; its key
+ * of head h begins at k[page * k_page_stride + slot * k_slot_stride + h *
+ * k_head_stride], its value likewise.  The pools hold n_pages pages; an entry
+ * of the table outside [0, n_pages) names none.  Sequences may share pages,
+ * and table_stride may be 0 (all sequences the same pages).
+ */
+typedef struct ilpm_kv_cache {
+    void *k, *v;
+    int64_t k_page_stride, k_slot_stride, k_head_stride;
+    int64_t v_page_stride, v_slot_stride, v_head_stride;
+    const int32_t *page_table; /* [n_seqs][max_pages], rows table_stride apart */
+    int64_t table_stride;
+    int dtype; /* of keys and values */
+    int n_pages, page_size, kv_heads, head_dim;
+    int n_seqs, max_pages;
+} ilpm_kv_cache;
+
+/*
+ * ilpm_kv_append -- write the keys and values of n_tokens new tokens into the
+ * cache, keys (and the queries of the same tokens) rotated by their positions
+ * on the way.  Token t is token positions[t] of sequence seq_ids[t]; with
+ * R = rot_dim, c = cos[positions[t]][i], s = sin[positions[t]][i], i < R/2,
+ *   pairs = 0: (a, b) = elements (i, i + R/2) of a head
+ *   pairs = 1: (a, b) = elements (2i, 2i + 1)
+ *   a' = a*c - b*s,  b' = b*c + a*s;  elements from R on stay as they are.
+ *   k, v   [n_tokens] rows of kv_heads heads, of the cache's type or ILPM_F32
+ *   q      [n_tokens] rows of any number of heads, of k's type, or NULL
+ *   q_out  where the rotated queries go: q's type and heads; may be q itself
+ *          (same data and strides).  NULL with q NULL
+ *   cos, sin  fp32 [n_positions][rot_dim / 2], contiguous; rot_dim even, in
+ *          [0, head_dim]; with rot_dim 0 nothing is rotated and both may be NULL
+ * A token whose seq_ids is outside [0, n_seqs) or whose position lies outside
+ * its table or in no page of the pool is not written to the cache (padding
+ * tokens: seq_ids -1).  Its query, if its position is outside [0, n_positions),
+ * is copied without rotation; a key is then not written either.  Two tokens of
+ * one call must not name the same slot.
+ * Returns ILPM_ERR_UNSUPPORTED for element types other than those above.
+ */
+int ilpm_kv_append(const ilpm_kv_cache *cache, const ilpm_heads *k, const ilpm_heads *v, const ilpm_heads *q,
+                   const ilpm_heads *q_out, const int32_t *seq_ids, const int32_t *positions, int n_tokens,
+                   const float *cos, const float *sin, int n_positions, int rot_dim, int pairs, hipStream_t stream);
+
+/* How ilpm_attn_decode scores and which keys it sees. */
+typedef struct ilpm_attn_options {
+    const uint8_t *mask; /* [n_seqs][mask_len], rows mask_stride apart: key j of a sequence is seen where its
+                            byte is not 0 (none from mask_len on); NULL: all */
+    int64_t mask_stride;
+    float scale;         /* of the scores */
+    float softcap;       /* > 0: a score x becomes softcap * tanh(x / softcap); 0: stays */
+    int mask_len;
+    int window;          /* > 0: only the last `window` tokens are seen; 0: all */
+    int max_len;         /* no sequence is longer, as far as the caller knows; 0: unknown.  Only the
+                            split over the length goes by it, the result does not depend on it */
+} ilpm_attn_options;
+
+/*
+ * ilpm_attn_decode -- attention of one new token of each sequence over the
+ * cache:
+ *   x_j = scale * <q, k_j>, capped;  m = max x_j;  l = sum exp(x_j - m)
+ *   out = sum exp(x_j - m) v_j / l;  lse = m + ln l
+ * over the keys j seen: j < lengths[s], in the window, not masked, in a page
+ * of the pool.  Nothing else of the cache has a part in it, whatever it holds.
+ * A row that sees no key gives out = 0 and lse = -infinity.
+ *   q    [n_seqs] rows of q_heads heads, a multiple of the cache's kv_heads:
+ *        head h reads key head h / (q_heads / kv_heads).  The cache's type or ILPM_F32
+ *   lengths  int32 [n_seqs]: tokens in the cache, the new one among them; taken
+ *        as 0 below 0, and as the table's end beyond it
+ *   out  as q (may be q itself);  lse  fp32 [n_seqs][q_heads] contiguous, or NULL
+ * head_dim is at most 256 (ILPM_ERR_UNSUPPORTED above).
+ * Long sequences are split over their length into chunks whose partial
+ * results are joined in their order, in a workspace of
+ * ilpm_attn_decode_workspace_size bytes: `workspace` (256-byte aligned; its
+ * contents do not matter) if it is not NULL, else the one of the split plans (see
+ * ilpm_conv2d_fwd), whose rules then hold.  Calls with workspaces of their own
+ * may overlap in time.
+ */
+int ilpm_attn_decode(const ilpm_kv_cache *cache, const ilpm_heads *q, const int32_t *lengths,
+                     const ilpm_attn_options *options, const ilpm_heads *out, float *lse, void *workspace,
+                     size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ilpm_attn_decode (0 where it needs none), from the cache's
+ * sizes, q_heads, the window and max_len.  Pure host. */
+int ilpm_attn_decode_workspace_size(const ilpm_kv_cache *cache, int q_heads, int window, int max_len, size_t *bytes);
+
+/* Norms of ilpm_residual_norm over a row v of `width` values:
+ *   RMS    v / sqrt(mean(v^2) + eps) * w + b
+ *   LAYER  (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * w + b
+ * with w taken as 1 and b as 0 where they are NULL. */
+enum { ILPM_NORM_NONE = 0, ILPM_NORM_RMS = 1, ILPM_NORM_LAYER = 2 };
+
+/*
+ * ilpm_residual_norm -- what lies between two blocks of a layer, a row for each
+ * token:
+ *   r = x + scale * gate * post(y),   z = pre(r)
+ * where y is a block's output, x the residual stream, r the new one, z the next
+ * block's input; z is taken from r before r is rounded to its type.
+ *   x, r  [rows][width], rows x_stride and r_stride apart, of x_dtype; r may be
+ *         x itself (same stride), or NULL where only z is wanted
+ *   y, z  [rows][width] of y_dtype; y may be NULL (r = x, without gate, scale and
+ *         post); z may be y itself, or NULL with pre ILPM_NORM_NONE
+ *   post, pre  ILPM_NORM_*: post NONE leaves y as it is
+ *   post_w, post_b, pre_w, pre_b  [width] of param_dtype, or NULL
+ *   gate  of param_dtype: [width] with gate_stride 0, [rows][width] otherwise; NULL: 1
+ * x_dtype is y_dtype or ILPM_F32, and param_dtype too (ILPM_ERR_UNSUPPORTED for others).
+ */
+typedef struct ilpm_residual_norm_args {
+    const void *x, *y;
+    void *r, *z;
+    const void *post_w, *post_b, *pre_w, *pre_b, *gate;
+    int64_t x_stride, y_stride, r_stride, z_stride, gate_stride;
+    int rows, width;
+    int x_dtype, y_dtype, param_dtype;
+    int post, pre;
+    float scale, eps;
+} ilpm_residual_norm_args;
+int ilpm_residual_norm(const ilpm_residual_norm_args *args, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,87 @@
+// What the decoder-step operators share: element types, their arguments as the
+// kernels take them, and their launchers (the entry points check the
+// arguments, decode_api.hip).
+#pragma once
+
+#include "internal.h"
+
+namespace ilpm {
+
+// ---- element types (ILPM_F32, ILPM_F16, ILPM_BF16) ----
+template <int DT> struct ElementOf;
+template <> struct ElementOf<ILPM_F32> { using type = float; };
+template <> struct ElementOf<ILPM_F16> { using type = _Float16; };
+template <> struct ElementOf<ILPM_BF16> { using type = __bf16; };
+
+inline int element_bytes(int dtype) { return dtype == ILPM_F32 ? 4 : 2; }
+
+// N elements as one memory access (16 bytes at most).
+template <typename T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
+
+// ---- kv_append ----
+struct AppendArgs {
+    // rows of heads: [token][head][dim], strides in elements
+    const void *k, *v, *q;
+    void *q_out;
+    int64_t k_row, k_head, v_row, v_head, q_row, q_head, qo_row, qo_head;
+    int n_tokens, q_heads, kv_heads, dim;
+    // the cache's page pools, strides in elements
+    void *kc, *vc;
+    int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;
+    const int32_t *table;
+    int64_t table_stride;
+    int n_seqs, max_pages, n_pages, page_size;
+    const int32_t *seq_ids, *positions;
+    const float *cos, *sin;  // [n_positions][rot_dim / 2]
+    int n_positions, rot_dim, pairs;
+};
+hipError_t append_launch(const AppendArgs &a, int x_dtype, int cache_dtype, hipStream_t stream);
+
+// ---- attn_decode ----
+struct AttnArgs {
+    const void *q;
+    int64_t q_row, q_head;
+    void *out;
+    int64_t o_row, o_head;
+    float *lse;  // [n_seqs][q_heads] or NULL
+    int q_dtype;
+    const void *k, *v;
+    int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
+    const int32_t *table;
+    int64_t table_stride;
+    int n_pages, page_size;
+    int capacity;  // keys a row of the table can name
+    const int32_t *lengths;
+    const uint8_t *mask;  // [n_seqs][mask_len] or NULL
+    int64_t mask_stride;
+    int mask_len;
+    int window;
+    float scale, softcap;
+    int n_seqs, q_heads, kv_heads, group, dim;
+    int chunk, splits;  // keys of a split, and splits of the longest sequence planned for
+    float *part_o;      // [n_seqs][q_heads][splits][dim]
+    float *part_ml;     // [n_seqs][q_heads][splits][2]
+};
+// Fills chunk and splits for sequences of up to max_len visible keys; the
+// workspace bytes that they need.
+size_t attn_plan(AttnArgs *a, int max_len);
+hipError_t attn_launch(const AttnArgs &a, int cache_dtype, hipStream_t stream);
+
+// ---- residual_norm ----
+struct NormArgs {
+    const void *x, *y;
+    void *r, *z;
+    int64_t x_row, y_row, r_row, z_row;
+    const void *post_w, *post_b, *pre_w, *pre_b, *gate;
+    int64_t gate_row;  // 0: one gate for all rows
+    int rows, width, post, pre;
+    float scale, eps;
+};
+hipError_t norm_launch(const NormArgs &a, int x_dtype, int y_dtype, int param_dtype, hipStream_t stream);
+
+// ---- the C-ABI layer's helpers (ilpm_api.hip) ----
+int api_hip_fail(hipError_t e);
+int api_device_check(int *dev);
+int api_workspace(int dev, size_t need, hipStream_t stream, void **ws);
+
+}  // namespace ilpm

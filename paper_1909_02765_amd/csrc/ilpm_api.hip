@@ -9,7 +9,7 @@
 #include <mutex>
 #include <vector>
 
-#include "internal.h"
+#include "decode.h"
 
 // The no-alloc entry point's workspace: one fixed array per device, created
 // when the code object loads and kept until the process ends (host code uses
@@ -489,6 +489,12 @@ size_t prepacked_bytes(const ilpm_plan &p, int c_in, int c_out, int k, int *rc)
 }
 
 }  // namespace
+
+// The same checks and workspace for the decoder-step entry points (decode_api.hip).
+int api_hip_fail(hipError_t e) { return hip_fail(e); }
+int api_device_check(int *dev) { return device_check(dev); }
+int api_workspace(int dev, size_t need, hipStream_t stream, void **ws) { return get_workspace(dev, need, stream, ws); }
+
 }  // namespace ilpm
 
 using namespace ilpm;
