@@ -1,0 +1,8 @@
+// attn_decode's kernels for bf16 caches (see decode_attn.h).
+#include "decode_attn.h"
+
+namespace ilpm {
+
+hipError_t attn_split_bf16(const AttnArgs &a, hipStream_t stream) { return attn_split_by_dim<__bf16, true>(a, stream); }
+
+}  // namespace ilpm

@@ -1,0 +1,8 @@
+// attn_decode's kernels for bf16 caches and f32 queries (see decode_attn.h).
+#include "decode_attn.h"
+
+namespace ilpm {
+
+hipError_t attn_split_bf16_q32(const AttnArgs &a, hipStream_t stream) { return attn_split_by_dim<__bf16, false>(a, stream); }
+
+}  // namespace ilpm
