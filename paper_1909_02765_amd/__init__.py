@@ -144,9 +144,10 @@ def _torch():
 
 
 def _stream_handle(stream=None):
-    torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None:
+        # (The stream's address alone: the object around it costs 3 us a call.)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return ctypes.c_void_p(stream.cuda_stream)
 
 
 def _stream_obj(stream=None):
@@ -594,7 +595,7 @@ def kv_append(k, v, k_pages, v_pages, page_table, seq_ids, positions, *, q=None,
     qp = op = None
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = torch.empty_like(q)
         qp, op = _pack_heads(q, "q", n, dim), _pack_heads(q_out, "q_out", n, dim)
     elif q_out is not None:
         raise ValueError("q_out is given without q")
@@ -630,7 +631,7 @@ def attn_decode(q, k_pages, v_pages, page_table, lengths, *, scale: Optional[flo
         raise ValueError(f"lengths must be [{n}]")
     cache = _pack_cache(k_pages, v_pages, page_table)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q)
     qp, op, heads = _pack_heads(q, "q", n, dim), _pack_heads(out, "out", n, dim), q.shape[1]
     if lse is None and return_lse:
         lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
@@ -681,9 +682,9 @@ def residual_norm(x, y=None, *, post: Optional[str] = None, post_w=None, post_b=
         raise ValueError('post and pre must be None, "rms" or "layer"')
     kind = y if y is not None else z if z is not None else x
     if r is None:
-        r = torch.empty((rows, width), dtype=x.dtype, device=x.device) if y is not None else None
+        r = torch.empty_like(x) if y is not None else None
     if z is None and NORMS[pre]:
-        z = torch.empty((rows, width), dtype=kind.dtype, device=x.device)
+        z = torch.empty_like(kind)
     ptrs, param = [], None
     for t, name in ((post_w, "post_w"), (post_b, "post_b"), (pre_w, "pre_w"), (pre_b, "pre_b")):
         if t is not None:

@@ -15,8 +15,9 @@ template <> struct ElementOf<ILPM_BF16> { using type = __bf16; };
 
 inline int element_bytes(int dtype) { return dtype == ILPM_F32 ? 4 : 2; }
 
-// N elements as one memory access (16 bytes at most).
-template <typename T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
+// N elements that lie together, aligned to 16 bytes or their size: one memory
+// access up to 16 bytes, several of 16 beyond.
+template <typename T, int N> struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack { T v[N]; };
 
 // ---- kv_append ----
 struct AppendArgs {

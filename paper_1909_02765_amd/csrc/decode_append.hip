@@ -8,6 +8,8 @@
 // in place.
 #include "decode.h"
 
+#include <algorithm>
+
 namespace ilpm {
 namespace {
 
@@ -77,9 +79,162 @@ template <typename TX, typename TC> __global__ __launch_bounds__(256) void appen
     }
 }
 
+// Rows that divide into packs of VEC elements (of pairs: both halves do): a
+// thread takes one pack, or one of each half, of up to HPT heads of a token, so
+// it reads the angles once for all of them.  What bounds it: the bytes of
+// queries, keys and values, read and written once.
+template <typename TX, typename TC, int VEC, int HPT> __global__ __launch_bounds__(256) void append_packs(AppendArgs a)
+{
+    const int half = a.rot_dim / 2;
+    // Packs of a rotated head (the first `turned` of them with their partners, or
+    // in pairs of neighbours), and of a value head.
+    const int turned = (a.pairs ? a.rot_dim : half) / VEC, units = a.dim / VEC - (a.pairs ? 0 : half / VEC);
+    const int vunits = a.dim / VEC;
+    const int heads = a.q_heads + a.kv_heads, slots = (heads + HPT - 1) / HPT, vslots = (a.kv_heads + HPT - 1) / HPT;
+    const unsigned per = slots * units + vslots * vunits;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int t = (int)(id / per);
+    if (t >= a.n_tokens) return;
+    int i = (int)(id - (int64_t)t * per);
+    const int pos = a.positions[t];
+
+    if (i >= slots * units) {  // a value's packs
+        i -= slots * units;
+        const int slot = i / vunits, e = (i - slot * vunits) * VEC;
+        const TX *v = (const TX *)a.v + (int64_t)t * a.v_row + e;
+        Pack<TX, VEC> p[HPT];
+#pragma unroll
+        for (int n = 0; n < HPT; ++n) {
+            const int h = slot + n * vslots;
+            if (h < a.kv_heads) p[n] = *reinterpret_cast<const Pack<TX, VEC> *>(v + h * a.v_head);
+        }
+        Place at = place_of(a, t, pos);
+        if (at.page < 0 || (a.rot_dim > 0 && pos >= a.n_positions)) return;
+        TC *vc = (TC *)a.vc + (int64_t)at.page * a.vc_page + (int64_t)at.slot * a.vc_slot + e;
+#pragma unroll
+        for (int n = 0; n < HPT; ++n) {
+            const int h = slot + n * vslots;
+            Pack<TC, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o.v[j] = (TC)(float)p[n].v[j];
+            if (h < a.kv_heads) *reinterpret_cast<Pack<TC, VEC> *>(vc + h * a.vc_head) = o;
+        }
+        return;
+    }
+
+    const int slot = i / units, u = i - slot * units;
+    const bool rotated = u < turned;
+    // Elements e.. and, of halves, their partners from e2.
+    const int e = a.pairs || rotated ? u * VEC : half + u * VEC, e2 = e + half;
+    const bool two = rotated && !a.pairs;
+    Pack<TX, VEC> p[HPT], p2[HPT];
+    const TX *q = (const TX *)a.q + (int64_t)t * a.q_row, *k = (const TX *)a.k + (int64_t)t * a.k_row;
+#pragma unroll
+    for (int n = 0; n < HPT; ++n) {
+        const int h = slot + n * slots;
+        if (h >= heads) continue;
+        const TX *src = h < a.q_heads ? q + h * a.q_head : k + (h - a.q_heads) * a.k_head;
+        p[n] = *reinterpret_cast<const Pack<TX, VEC> *>(src + e);
+        if (two) p2[n] = *reinterpret_cast<const Pack<TX, VEC> *>(src + e2);
+    }
+    const bool known = a.rot_dim > 0 && pos >= 0 && pos < a.n_positions, turn = rotated && known;
+    // VEC angles for halves, VEC / 2 for pairs.
+    float c[VEC], s[VEC];
+    if (turn) {
+        const int first = a.pairs ? e / 2 : e;
+        const float *cos = a.cos + (int64_t)pos * half + first, *sin = a.sin + (int64_t)pos * half + first;
+        constexpr int HV = VEC > 1 ? VEC / 2 : 1;
+        const Pack<float, HV> c0 = *reinterpret_cast<const Pack<float, HV> *>(cos);
+        const Pack<float, HV> s0 = *reinterpret_cast<const Pack<float, HV> *>(sin);
+#pragma unroll
+        for (int j = 0; j < HV; ++j) c[j] = c0.v[j], s[j] = s0.v[j];
+        if (two) {
+            const Pack<float, HV> c1 = *reinterpret_cast<const Pack<float, HV> *>(cos + HV);
+            const Pack<float, HV> s1 = *reinterpret_cast<const Pack<float, HV> *>(sin + HV);
+#pragma unroll
+            for (int j = 0; j < HV; ++j) c[HV + j] = c1.v[j], s[HV + j] = s1.v[j];
+        }
+    }
+    // (The queries of a token are turned wherever its keys go.)
+    Place at = {-1, 0};
+    if (slot + (HPT - 1) * slots >= a.q_heads) at = place_of(a, t, pos);
+    if (a.rot_dim > 0 && !known) at.page = -1;
+    TC *kc = (TC *)a.kc + (int64_t)max(at.page, 0) * a.kc_page + (int64_t)at.slot * a.kc_slot;
+    TX *qo = (TX *)a.q_out + (int64_t)t * a.qo_row;
+#pragma unroll
+    for (int n = 0; n < HPT; ++n) {
+        const int h = slot + n * slots;
+        if (h >= heads) continue;
+        float x[VEC], y[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = (float)p[n].v[j], y[j] = two ? (float)p2[n].v[j] : 0.f;
+        if (turn && two) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float v = x[j];
+                x[j] = v * c[j] - y[j] * s[j];
+                y[j] = y[j] * c[j] + v * s[j];
+            }
+        } else if (turn) {
+#pragma unroll
+            for (int j = 0; j + 1 < VEC; j += 2) {
+                const float v = x[j], w = x[j + 1];
+                x[j] = v * c[j / 2] - w * s[j / 2];
+                x[j + 1] = w * c[j / 2] + v * s[j / 2];
+            }
+        }
+        auto put = [&](auto *dst) {
+            using TD = std::remove_reference_t<decltype(*dst)>;
+            Pack<TD, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o.v[j] = (TD)x[j];
+            *reinterpret_cast<Pack<TD, VEC> *>(dst + e) = o;
+            if (!two) return;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o.v[j] = (TD)y[j];
+            *reinterpret_cast<Pack<TD, VEC> *>(dst + e2) = o;
+        };
+        if (h < a.q_heads) put(qo + h * a.qo_head);
+        else if (at.page >= 0) put(kc + (h - a.q_heads) * a.kc_head);
+    }
+}
+
+// Whether everything divides into packs of `vec` elements, aligned to 16
+// bytes or the pack's size.
+bool packs_fit(const AppendArgs &a, int vec, int sx, int sc)
+{
+    auto at = [&](const void *p, int size) { return (uintptr_t)p % std::min(16, vec * size) == 0; };
+    const int half = a.rot_dim / 2;
+    if (a.dim % vec || (a.pairs ? a.rot_dim : half) % vec) return false;
+    // (Half of a pack of angles is the unit in which they are read.)
+    if (a.rot_dim > 0 && (half % (vec / 2) || !((uintptr_t)a.cos % std::min(16, vec / 2 * 4) == 0 && (uintptr_t)a.sin % std::min(16, vec / 2 * 4) == 0)))
+        return false;
+    for (int64_t s : {a.k_row, a.k_head, a.v_row, a.v_head, a.q_row, a.q_head, a.qo_row, a.qo_head, a.kc_page, a.kc_slot, a.kc_head,
+                      a.vc_page, a.vc_slot, a.vc_head})
+        if (s % vec) return false;
+    return at(a.k, sx) && at(a.v, sx) && at(a.q, sx) && at(a.q_out, sx) && at(a.kc, sc) && at(a.vc, sc);
+}
+
+template <typename TX, typename TC, int VEC> bool launch_packs(const AppendArgs &a, hipStream_t stream)
+{
+    if (!packs_fit(a, VEC, sizeof(TX), sizeof(TC))) return false;
+    const int half = a.rot_dim / 2, units = a.dim / VEC - (a.pairs ? 0 : half / VEC), vunits = a.dim / VEC;
+    auto groups = [&](int hpt) {
+        const int64_t per = (int64_t)ceil_div(a.q_heads + a.kv_heads, hpt) * units + (int64_t)ceil_div(a.kv_heads, hpt) * vunits;
+        return (per * a.n_tokens + 255) / 256;
+    };
+    // One head a thread until the card is full of threads, then four.
+    const bool four = groups(1) > 4096;
+    if (groups(four ? 4 : 1) > (1 << 24) - 1) return false;
+    if (four) hipLaunchKernelGGL((append_packs<TX, TC, VEC, 4>), dim3((unsigned)groups(4)), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((append_packs<TX, TC, VEC, 1>), dim3((unsigned)groups(1)), dim3(256), 0, stream, a);
+    return true;
+}
+
 template <typename TX, typename TC> hipError_t launch(const AppendArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((append_any<TX, TC>), dim3(a.n_tokens), dim3(256), 0, stream, a);
+    if (!launch_packs<TX, TC, 8>(a, stream) && !launch_packs<TX, TC, 4>(a, stream) && !launch_packs<TX, TC, 2>(a, stream))
+        hipLaunchKernelGGL((append_any<TX, TC>), dim3(a.n_tokens), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

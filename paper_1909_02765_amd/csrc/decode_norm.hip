@@ -1,6 +1,8 @@
 // residual_norm: r = x + scale * gate * post(y), z = pre(r), a row per token.
 #include "decode.h"
 
+#include <algorithm>
+
 namespace ilpm {
 namespace {
 
@@ -86,9 +88,199 @@ template <typename TX, typename TY, typename TP> __global__ __launch_bounds__(25
     });
 }
 
+// A sum over the 64 lanes of a wave, given to all of them: within rows of 16 by
+// lane permutations of the vector unit, then across the rows.
+template <int CTRL> __device__ inline float plus_permuted(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+
+__device__ inline float wave_sum(float v)
+{
+    v = plus_permuted<0xB1>(v);   // lanes 1 0 3 2 of each four
+    v = plus_permuted<0x4E>(v);   // lanes 2 3 0 1 of each four
+    v = plus_permuted<0x141>(v);  // the other four of eight
+    v = plus_permuted<0x140>(v);  // the other eight of sixteen
+    unsigned x = __builtin_bit_cast(unsigned, v);
+    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const unsigned p0 = p[0], p1 = p[1];
+    x = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1));
+    const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const unsigned q0 = q[0], q1 = q[1];
+    return __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
+}
+
+// Rows of up to T * E values: T threads hold a row in registers, E values each,
+// in packs of VEC (16 bytes of y; VEC 1 for any width, stride and alignment),
+// so each input is read once and each output written once.  T = 64 leaves a
+// row to one wave (four rows a workgroup, no barrier).  Weights and biases
+// stay in registers over the rows that a workgroup takes.
+//
+// Mean and variance come from the values in registers, in two steps, so a mean
+// far from zero costs the variance nothing.  What bounds it: the bytes of x, y,
+// gate, r and z.
+template <typename TX, typename TY, typename TP, int T, int E, int VEC>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
+{
+    constexpr int NV = E / VEC, ROWS = T < 256 ? 256 / T : 1, WAVES = T / 64;
+    constexpr bool HOLD = T * E <= 8192;  // (beyond, they do not fit beside the row: read again for each)
+    __shared__ float lds[WAVES > 1 ? 2 * WAVES : 1];
+    const int tid = threadIdx.x % T;
+    const float inv_n = 1.f / (float)a.width;
+    int turn = 0;
+    auto total = [&](float v) {
+        v = wave_sum(v);
+        if constexpr (WAVES > 1) {
+            // Two sets of places in turn: what is written now was read before the last barrier.
+            float *part = lds + turn * WAVES;
+            turn ^= 1;
+            if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
+            __syncthreads();
+            v = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v += part[w];
+        }
+        return v;
+    };
+    auto get = [&](const auto *row, int i) {
+        using TD = std::remove_cv_t<std::remove_reference_t<decltype(*row)>>;
+        Pack<TD, VEC> p = {};
+        const int at = (tid + i * T) * VEC;
+        if (row && at < a.width) p = *reinterpret_cast<const Pack<TD, VEC> *>(row + at);
+        return p;
+    };
+    Pack<TP, VEC> post_w[NV], post_b[NV], pre_w[NV], pre_b[NV];
+#pragma unroll
+    for (int i = 0; HOLD && i < NV; ++i) {
+        post_w[i] = get((const TP *)a.post_w, i);
+        post_b[i] = get((const TP *)a.post_b, i);
+        pre_w[i] = get((const TP *)a.pre_w, i);
+        pre_b[i] = get((const TP *)a.pre_b, i);
+    }
+    // (v - mean) / sqrt(variance + eps) * w + b of the values in v, which are 0
+    // beyond the row's end; `live` says which are not.
+    auto normed = [&](float (&v)[NV][VEC], int kind, const void *w, const void *b, const auto &wh, const auto &bh) {
+        float mean = 0.f, s = 0.f;
+        if (kind == ILPM_NORM_LAYER) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) s += v[i][j];
+            mean = total(s) * inv_n;
+            s = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool live = (tid + i * T) * VEC < a.width;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[i][j] = live ? v[i][j] - mean : 0.f;
+                s += v[i][j] * v[i][j];
+            }
+        }
+        const float rstd = 1.f / sqrtf(total(s) * inv_n + a.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const Pack<TP, VEC> wp = HOLD ? wh[i] : get((const TP *)w, i), bp = HOLD ? bh[i] : get((const TP *)b, i);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[i][j] *= rstd;
+                if (w) v[i][j] *= (float)wp.v[j];
+                if (b) v[i][j] += (float)bp.v[j];
+            }
+        }
+    };
+
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
+        float v[NV][VEC], u[NV][VEC];
+        Pack<TX, VEC> x[NV];
+        Pack<TY, VEC> y[NV];
+        Pack<TP, VEC> gate[NV];
+        const TP *grow = a.gate ? (const TP *)a.gate + row * a.gate_row : nullptr;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) y[i] = get(a.y ? (const TY *)a.y + row * a.y_row : (const TY *)nullptr, i);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] = get((const TX *)a.x + row * a.x_row, i);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) gate[i] = get(grow, i);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i][j] = (float)x[i].v[j];
+        if (a.y) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) u[i][j] = (float)y[i].v[j];
+            if (a.post != ILPM_NORM_NONE) normed(u, a.post, a.post_w, a.post_b, post_w, post_b);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const bool live = (tid + i * T) * VEC < a.width;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    if (a.gate) u[i][j] *= (float)gate[i].v[j];
+                    v[i][j] = live ? v[i][j] + a.scale * u[i][j] : 0.f;
+                }
+            }
+        }
+        if (a.r) {
+            TX *r = (TX *)a.r + row * a.r_row;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int at = (tid + i * T) * VEC;
+                Pack<TX, VEC> p;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.v[j] = (TX)v[i][j];
+                if (at < a.width) *reinterpret_cast<Pack<TX, VEC> *>(r + at) = p;
+            }
+        }
+        if (a.z) {
+            normed(v, a.pre, a.pre_w, a.pre_b, pre_w, pre_b);
+            TY *z = (TY *)a.z + row * a.z_row;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int at = (tid + i * T) * VEC;
+                Pack<TY, VEC> p;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.v[j] = (TY)v[i][j];
+                if (at < a.width) *reinterpret_cast<Pack<TY, VEC> *>(z + at) = p;
+            }
+        }
+    }
+}
+
+template <typename TX, typename TY, typename TP, int T, int E, int VEC>
+void launch_rows(const NormArgs &a, hipStream_t stream)
+{
+    constexpr int block = T < 256 ? 256 : T, per = T < 256 ? 256 / T : 1;
+    const int groups = std::min(ceil_div(a.rows, per), 256 * 2048 / block);
+    hipLaunchKernelGGL((norm_rows<TX, TY, TP, T, E, VEC>), dim3(groups), dim3(block), 0, stream, a);
+}
+
+template <typename TX, typename TY, typename TP, int VEC> bool launch_width(const NormArgs &a, hipStream_t stream)
+{
+    if (a.width <= 512) launch_rows<TX, TY, TP, 64, 8, VEC>(a, stream);
+    else if (a.width <= 1024) launch_rows<TX, TY, TP, 64, 16, VEC>(a, stream);
+    else if (a.width <= 2048) launch_rows<TX, TY, TP, 256, 8, VEC>(a, stream);
+    else if (a.width <= 4096) launch_rows<TX, TY, TP, 256, 16, VEC>(a, stream);
+    else if (a.width <= 8192) launch_rows<TX, TY, TP, 1024, 8, VEC>(a, stream);
+    else if (a.width <= 16384) launch_rows<TX, TY, TP, 1024, 16, VEC>(a, stream);
+    else return false;
+    return true;
+}
+
 template <typename TX, typename TY, typename TP> hipError_t launch(const NormArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((norm_any<TX, TY, TP>), dim3(a.rows), dim3(256), 0, stream, a);
+    constexpr int VEC = 16 / (int)sizeof(TY);
+    auto fits = [&](const void *p, int64_t stride, int size) {
+        return (uintptr_t)p % std::min(16, VEC * size) == 0 && stride % VEC == 0;
+    };
+    const int sx = sizeof(TX), sy = sizeof(TY), sp = sizeof(TP);
+    const bool packs = a.width % VEC == 0 && fits(a.x, a.x_row, sx) && fits(a.r, a.r_row, sx) && fits(a.y, a.y_row, sy) &&
+                       fits(a.z, a.z_row, sy) && fits(a.gate, a.gate_row, sp) && fits(a.post_w, 0, sp) &&
+                       fits(a.post_b, 0, sp) && fits(a.pre_w, 0, sp) && fits(a.pre_b, 0, sp);
+    if (!(packs ? launch_width<TX, TY, TP, VEC>(a, stream) : launch_width<TX, TY, TP, 1>(a, stream)))
+        hipLaunchKernelGGL((norm_any<TX, TY, TP>), dim3(a.rows), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
