@@ -12,7 +12,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -67,6 +66,11 @@ import torch  # noqa: E402,F401
 
 lib = ctypes.CDLL(LIBRARY)
 
+if not os.path.exists(os.path.join(PKG, "_binding.so")):
+    raise ImportError(f"{os.path.join(PKG, '_binding.so')} is not built: run `python paper_1909_02765_amd/build.py` "
+                      "(or __graft_entry__.build()) first")
+from . import _binding  # noqa: E402
+
 
 def _hip_runtimes_mapped():
     paths = set()
@@ -117,7 +121,6 @@ _SIGS = {
     "ilpm_conv2d_fwd_winograd": ([_vp, _vp, _vp] + [_i] * 5 + [_vp, _vp], _i),
     "ilpm_relu_inplace": ([_vp, ctypes.c_int64, _vp], _i),
     "ilpm_maxpool2x2": ([_vp, _i, _i, _i, _vp, _vp], _i),
-    # (Structures go in as packed bytes, see _pack_cache and the like.)
     "ilpm_kv_append": ([_vp] * 7 + [_i, _vp, _vp, _i, _i, _i, _vp], _i),
     "ilpm_attn_decode": ([_vp] * 7 + [ctypes.c_size_t, _vp], _i),
     "ilpm_attn_decode_workspace_size": ([_vp, _i, _i, _i, ctypes.POINTER(ctypes.c_size_t)], _i),
@@ -521,55 +524,6 @@ def maxpool2x2(x, stream=None):
 
 F32, F16, BF16 = 0, 1, 2                     # ILPM_F32, ILPM_F16, ILPM_BF16
 NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}  # ILPM_NORM_*
-_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
-
-# The header's structures as the C compiler lays them out (ilpm_heads,
-# ilpm_kv_cache, ilpm_attn_options, ilpm_residual_norm_args).
-_HEADS = struct.Struct("@Pqqii")
-_CACHE = struct.Struct("@PPqqqqqqPqiiiiiii4x")
-_OPTIONS = struct.Struct("@Pqffiii4x")
-_NORM = struct.Struct("@PPPPPPPPPqqqqqiiiiiiiff4x")
-
-
-def _dtype(t, name):
-    d = _DTYPES.get(t.dtype)
-    if d is None:
-        raise TypeError(f"{name} must be a float32, float16 or bfloat16 tensor")
-    return d
-
-
-def _pack_heads(t, name, rows, dim):
-    """A [rows, heads, dim] CUDA tensor, its last dimension contiguous, as an ilpm_heads."""
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != rows or shape[2] != dim or (stride[2] != 1 and dim > 1):
-        raise ValueError(f"{name} must be [{rows}, heads, {dim}] with its last dimension contiguous")
-    return _HEADS.pack(t.data_ptr(), stride[0], stride[1], _dtype(t, name), shape[1])
-
-
-def _int32(t, name, dims):
-    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != dims:
-        raise TypeError(f"{name} must be a {dims}-dimensional int32 CUDA tensor")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{name}'s last dimension must be contiguous")
-    return t.data_ptr()
-
-
-def _pack_cache(k_pages, v_pages, page_table):
-    """Page pools [n_pages, page_size, kv_heads, head_dim] (any strides of the first
-    three dimensions) and a page table [n_seqs, max_pages] as an ilpm_kv_cache."""
-    if not (k_pages.is_cuda and v_pages.is_cuda):
-        raise TypeError("k_pages and v_pages must be CUDA tensors")
-    shape, ks, vs = k_pages.shape, k_pages.stride(), v_pages.stride()
-    if len(shape) != 4 or v_pages.shape != shape or k_pages.dtype != v_pages.dtype:
-        raise ValueError("k_pages and v_pages must be [n_pages, page_size, kv_heads, head_dim] of one type")
-    if shape[3] > 1 and not ks[3] == vs[3] == 1:
-        raise ValueError("the last dimension of k_pages and v_pages must be contiguous")
-    table = _int32(page_table, "page_table", 2)
-    return _CACHE.pack(k_pages.data_ptr(), v_pages.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], table,
-                       page_table.stride(0), _dtype(k_pages, "k_pages"), shape[0], shape[1], shape[2], shape[3],
-                       page_table.shape[0], page_table.shape[1])
 
 
 def kv_append(k, v, k_pages, v_pages, page_table, seq_ids, positions, *, q=None, cos=None, sin=None,
@@ -582,36 +536,22 @@ def kv_append(k, v, k_pages, v_pages, page_table, seq_ids, positions, *, q=None,
     rotated: elements (i, i + rot_dim/2) of a head together, or (2i, 2i + 1) with pairs.  Returns q_out, the rotated
     queries (a new tensor if not given, which may be q itself), or None without q.  k, v and q have the cache's type or
     float32.  See ilpm_kv_append in include/ilpm.h."""
-    n, dim = k.shape[0], k_pages.shape[3]
-    if positions.shape[0] != n or seq_ids.shape[0] != n:
-        raise ValueError(f"seq_ids and positions must be [{n}]")
-    n_positions = half = 0
-    angles = (None, None)
-    if cos is not None or sin is not None:
-        if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape:
-            raise ValueError("cos and sin must both be [n_positions, rot_dim / 2]")
-        n_positions, half = cos.shape
-        angles = (_dev_f32(cos, "cos"), _dev_f32(sin, "sin"))
-    qp = op = None
-    if q is not None:
-        if q_out is None:
-            q_out = torch.empty_like(q)
-        qp, op = _pack_heads(q, "q", n, dim), _pack_heads(q_out, "q_out", n, dim)
-    elif q_out is not None:
-        raise ValueError("q_out is given without q")
-    _check(lib.ilpm_kv_append(_pack_cache(k_pages, v_pages, page_table), _pack_heads(k, "k", n, dim),
-                              _pack_heads(v, "v", n, dim), qp, op, _int32(seq_ids, "seq_ids", 1),
-                              _int32(positions, "positions", 1), n, angles[0], angles[1], n_positions, 2 * half,
-                              1 if pairs else 0, _stream_handle(stream)), "ilpm_kv_append")
-    return q_out
+    if stream is not None:
+        with torch.cuda.stream(stream):  # (what is allocated then belongs to that stream)
+            return kv_append(k, v, k_pages, v_pages, page_table, seq_ids, positions, q=q, cos=cos, sin=sin, pairs=pairs,
+                             q_out=q_out)
+    got = _binding.kv_append(k, v, k_pages, v_pages, page_table, seq_ids, positions, q, cos, sin, pairs, q_out)
+    if type(got) is int:
+        raise IlpmError(got, "ilpm_kv_append")
+    return got
 
 
 def attn_decode_workspace_size(k_pages, v_pages, page_table, q_heads: int, window: int = 0, max_len: int = 0) -> int:
     """Bytes of workspace attn_decode needs for this cache (0 where it needs none)."""
-    n = ctypes.c_size_t()
-    _check(lib.ilpm_attn_decode_workspace_size(_pack_cache(k_pages, v_pages, page_table), q_heads, window, max_len,
-                                               ctypes.byref(n)), "ilpm_attn_decode_workspace_size")
-    return n.value
+    got = _binding.attn_decode_workspace_size(k_pages, v_pages, page_table, q_heads, window, max_len)
+    if got < 0:
+        raise IlpmError(got, "ilpm_attn_decode_workspace_size")
+    return got
 
 
 def attn_decode(q, k_pages, v_pages, page_table, lengths, *, scale: Optional[float] = None, window: int = 0,
@@ -625,46 +565,16 @@ def attn_decode(q, k_pages, v_pages, page_table, lengths, *, scale: Optional[flo
     is not 0; max_len: an upper bound of the lengths, if known.  Returns out (like q), or (out, lse) with return_lse
     or lse given, lse float32 [n_seqs, q_heads]: the logarithm of the sum of the exponentials of the scores.  A row that
     sees no key gives 0 and -inf.  workspace: a CUDA tensor of attn_decode_workspace_size bytes, for calls that must
-    not allocate; by default it comes from torch's allocator, on the current stream.  See ilpm_attn_decode in include/ilpm.h."""
-    n, dim = page_table.shape[0], k_pages.shape[3]
-    if lengths.shape[0] != n:
-        raise ValueError(f"lengths must be [{n}]")
-    cache = _pack_cache(k_pages, v_pages, page_table)
-    if out is None:
-        out = torch.empty_like(q)
-    qp, op, heads = _pack_heads(q, "q", n, dim), _pack_heads(out, "out", n, dim), q.shape[1]
-    if lse is None and return_lse:
-        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
-    elif lse is not None and lse.shape != (n, heads):
-        raise ValueError(f"lse must be [{n}, {heads}]")
-    mask_p, mask_stride, mask_len = 0, 0, 0
-    if mask is not None:
-        if not mask.is_cuda or mask.dtype not in (torch.bool, torch.uint8):
-            raise TypeError("mask must be a bool or uint8 CUDA tensor")
-        if mask.dim() != 2 or mask.shape[0] != n or (mask.stride(1) != 1 and mask.shape[1] > 1):
-            raise ValueError(f"mask must be [{n}, keys] with its last dimension contiguous")
-        # (A mask of no columns has no memory, and still hides every key: it is never read then.)
-        mask_p, mask_stride, mask_len = mask.data_ptr() or lengths.data_ptr(), mask.stride(0), mask.shape[1]
-    need = ctypes.c_size_t()
-    _check(lib.ilpm_attn_decode_workspace_size(cache, heads, window, max_len, ctypes.byref(need)),
-           "ilpm_attn_decode_workspace_size")
-    if workspace is None and need.value:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-    ws, ws_bytes = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
-    options = _OPTIONS.pack(mask_p, mask_stride, dim ** -0.5 if scale is None else scale, softcap, mask_len, window, max_len)
-    _check(lib.ilpm_attn_decode(cache, qp, _int32(lengths, "lengths", 1), options, op,
-                                _dev_f32(lse, "lse") if lse is not None else None, ws, ws_bytes,
-                                _stream_handle(stream)), "ilpm_attn_decode")
-    return out if lse is None else (out, lse)
-
-
-def _row_stride(t, name, rows, width):
-    """The row stride of a CUDA tensor [rows, width] whose last dimension is contiguous."""
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or (t.stride(1) != 1 and width > 1):
-        raise ValueError(f"{name} must be [{rows}, {width}] with its last dimension contiguous")
-    return t.stride(0)
+    not allocate; by default it comes from torch's allocator.  See ilpm_attn_decode in include/ilpm.h."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attn_decode(q, k_pages, v_pages, page_table, lengths, scale=scale, window=window, softcap=softcap,
+                               mask=mask, max_len=max_len, out=out, lse=lse, return_lse=return_lse, workspace=workspace)
+    got = _binding.attn_decode(q, k_pages, v_pages, page_table, lengths, scale, window, softcap, mask, max_len, out, lse,
+                               return_lse, workspace)
+    if type(got) is int:
+        raise IlpmError(got, "ilpm_attn_decode")
+    return got
 
 
 def residual_norm(x, y=None, *, post: Optional[str] = None, post_w=None, post_b=None, gate=None, scale: float = 1.0,
@@ -675,43 +585,13 @@ def residual_norm(x, y=None, *, post: Optional[str] = None, post_w=None, post_b=
     "layer", with weights and biases [width]; gate [width] or [rows, width].  Returns (r, z): r of x's type (r=x adds in
     place), z of y's (None without pre).  x is of y's type or float32, and so are weights, biases and gate, all of one
     type.  See ilpm_residual_norm in include/ilpm.h."""
-    if x.dim() != 2:
-        raise ValueError("x must be [rows, width]")
-    rows, width = x.shape
     if post not in NORMS or pre not in NORMS:
         raise ValueError('post and pre must be None, "rms" or "layer"')
-    kind = y if y is not None else z if z is not None else x
-    if r is None:
-        r = torch.empty_like(x) if y is not None else None
-    if z is None and NORMS[pre]:
-        z = torch.empty_like(kind)
-    ptrs, param = [], None
-    for t, name in ((post_w, "post_w"), (post_b, "post_b"), (pre_w, "pre_w"), (pre_b, "pre_b")):
-        if t is not None:
-            if not t.is_cuda or t.shape != (width,) or (width > 1 and t.stride(0) != 1):
-                raise ValueError(f"{name} must be a contiguous CUDA tensor [{width}]")
-            if param is not None and t.dtype != param:
-                raise TypeError("weights, biases and gate must be of one type")
-            param = t.dtype
-        ptrs.append(t.data_ptr() if t is not None else 0)
-    gate_stride = 0
-    if gate is not None:
-        if param is not None and gate.dtype != param:
-            raise TypeError("weights, biases and gate must be of one type")
-        param = gate.dtype
-        if gate.dim() == 1:
-            if not gate.is_cuda or gate.shape[0] != width or (width > 1 and gate.stride(0) != 1):
-                raise ValueError(f"gate must be a contiguous CUDA tensor [{width}], or [{rows}, {width}]")
-        else:
-            gate_stride = _row_stride(gate, "gate", rows, width)
-    if (z is not None and z.dtype != kind.dtype) or (r is not None and r.dtype != x.dtype):
-        raise TypeError("r must be of x's type and z of y's")
-    param = _DTYPES.get(param, -1) if param is not None else _dtype(kind, "y")
-    args = _NORM.pack(x.data_ptr(), y.data_ptr() if y is not None else 0, r.data_ptr() if r is not None else 0,
-                      z.data_ptr() if z is not None else 0, *ptrs, gate.data_ptr() if gate is not None else 0,
-                      _row_stride(x, "x", rows, width), _row_stride(y, "y", rows, width) if y is not None else 0,
-                      _row_stride(r, "r", rows, width) if r is not None else 0,
-                      _row_stride(z, "z", rows, width) if z is not None else 0, gate_stride, rows, width,
-                      _dtype(x, "x"), _dtype(kind, "y"), param, NORMS[post], NORMS[pre], scale, eps)
-    _check(lib.ilpm_residual_norm(args, _stream_handle(stream)), "ilpm_residual_norm")
-    return (x if r is None else r), z
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return residual_norm(x, y, post=post, post_w=post_w, post_b=post_b, gate=gate, scale=scale, pre=pre,
+                                 pre_w=pre_w, pre_b=pre_b, eps=eps, r=r, z=z)
+    got = _binding.residual_norm(x, y, NORMS[post], post_w, post_b, gate, scale, NORMS[pre], pre_w, pre_b, eps, r, z)
+    if type(got) is int:
+        raise IlpmError(got, "ilpm_residual_norm")
+    return got

@@ -1,4 +1,5 @@
-"""Build libilpm.so (the HIP kernels and the C ABI) for gfx950 with hipcc.
+"""Build libilpm.so (the HIP kernels and the C ABI) for gfx950 with hipcc, and the
+Python module _binding.so beside it.
 
     python paper_1909_02765_amd/build.py            # build in-tree
     python paper_1909_02765_amd/build.py --isa DIR  # also keep the gfx950 assembly in DIR
@@ -87,6 +88,26 @@ def build(output: str = LIBRARY, isa_dir: str | None = None, verbose: bool = Fal
     return output
 
 
+BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
+BINDING = os.path.join(PKG, "_binding.so")
+
+
+def build_binding(output: str = BINDING) -> str:
+    """The Python module of the decoder-step operators (host code on torch's headers), beside the library it calls."""
+    import importlib.util
+    import sysconfig
+    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
+    tmp = output + ".tmp"
+    includes = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+                "/opt/rocm/include", sysconfig.get_paths()["include"], INCLUDE]
+    subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM"]
+                   + [f"-I{d}" for d in includes] + [BINDING_SOURCE, "-o", tmp, "-L", os.path.join(torch_dir, "lib"),
+                      "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-L", PKG, "-l:" + os.path.basename(LIBRARY),
+                      "-Wl,-rpath,$ORIGIN"], check=True)
+    os.replace(tmp, output)
+    return output
+
+
 PEAKS_SOURCE = os.path.join(ROOT, "bench_peaks.hip")
 PEAKS_LIBRARY = os.path.join(ROOT, "bench_peaks.so")
 
@@ -105,6 +126,7 @@ def main():
     ap.add_argument("-v", action="store_true")
     args = ap.parse_args()
     print(build(isa_dir=args.isa, verbose=args.v))
+    print(build_binding())
     print(build_peaks())
 
 

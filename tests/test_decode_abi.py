@@ -10,6 +10,7 @@ import subprocess
 
 import pytest
 
+import decode_abi
 import paper_1909_02765_amd as ilpm
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -25,7 +26,7 @@ def test_structures_have_the_c_compilers_sizes(tmp_path):
     subprocess.run([cc, "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I", "/opt/rocm/include", str(src),
                     "-o", str(tmp_path / "sizes")], check=True)
     got = subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, check=True).stdout.split()
-    assert [int(v) for v in got] == [ilpm._HEADS.size, ilpm._CACHE.size, ilpm._OPTIONS.size, ilpm._NORM.size]
+    assert [int(v) for v in got] == [decode_abi.HEADS.size, decode_abi.CACHE.size, decode_abi.OPTIONS.size, decode_abi.NORM.size]
 
 
 def test_constants_agree_with_the_header():
@@ -41,11 +42,11 @@ def cache(**kw):
     c = dict(k=GB, v=2 * GB, kp=16 * 8 * 128, ks=8 * 128, kh=128, vp=16 * 8 * 128, vs=8 * 128, vh=128, table=3 * GB, tstride=20,
              dtype=BF16, pages=100, size=16, heads=8, dim=128, seqs=4, wide=20)
     c.update(kw)
-    return ilpm._CACHE.pack(*c.values())
+    return decode_abi.CACHE.pack(*c.values())
 
 
 def heads(at, n=8, dtype=BF16, row=None, head=128):
-    return ilpm._HEADS.pack(at, n * 128 if row is None else row, head, dtype, n)
+    return decode_abi.HEADS.pack(at, n * 128 if row is None else row, head, dtype, n)
 
 
 def append(c=None, k=heads(4 * GB), v=heads(5 * GB), q=heads(6 * GB, 32), q_out=heads(7 * GB, 32), seq=8 * GB, pos=9 * GB,
@@ -88,7 +89,7 @@ def test_append_of_nothing_is_fine():
 
 
 def options(mask=0, mstride=0, scale=0.1, cap=0.0, mlen=0, window=0, max_len=0):
-    return ilpm._OPTIONS.pack(mask, mstride, scale, cap, mlen, window, max_len)
+    return decode_abi.OPTIONS.pack(mask, mstride, scale, cap, mlen, window, max_len)
 
 
 def attn(c=None, q=heads(4 * GB, 32), lengths=5 * GB, opt=None, out=heads(6 * GB, 32), lse=7 * GB, ws=8 * GB, ws_bytes=GB):
@@ -153,7 +154,7 @@ def norm(**kw):
     a = dict(x=GB, y=2 * GB, r=3 * GB, z=4 * GB, post_w=5 * GB, post_b=6 * GB, pre_w=7 * GB, pre_b=8 * GB, gate=9 * GB, xs=512, ys=512,
              rs=512, zs=512, gs=512, rows=10, width=512, xd=F32, yd=BF16, pd=F32, post=1, pre=2, scale=1.0, eps=1e-6)
     a.update(kw)
-    return ilpm.lib.ilpm_residual_norm(ilpm._NORM.pack(*a.values()), None)
+    return ilpm.lib.ilpm_residual_norm(decode_abi.NORM.pack(*a.values()), None)
 
 
 @pytest.mark.parametrize("kw", [

@@ -7,6 +7,7 @@ import math
 import pytest
 import torch
 
+import decode_abi
 import decode_ref as ref
 from gpu_common import note, torch_cuda
 
@@ -331,7 +332,6 @@ def test_attention_workspaces():
     need = ilpm.attn_decode_workspace_size(t["kp"], t["vp"], t["table"], 8)
     assert need > 0
     want = ilpm.attn_decode(*t.values())
-    ws, untouched = guarded((need // 2,), BF16)
     ws = torch.full((need + 512,), 255, dtype=torch.uint8, device="cuda")   # NaN bytes
     got = ilpm.attn_decode(*t.values(), workspace=ws[:need])
     torch.cuda.synchronize()
@@ -344,9 +344,9 @@ def test_attention_workspaces():
     assert e.value.status == ilpm.ERR_INVALID_ARG
     # Without one the C call takes the workspace of the split plans.
     out = torch.empty_like(want)
-    call = (ilpm._pack_cache(t["kp"], t["vp"], t["table"]), ilpm._pack_heads(t["q"], "q", 2, 128), t["lengths"].data_ptr(),
-            ilpm._OPTIONS.pack(0, 0, 128 ** -0.5, 0.0, 0, 0, 0), ilpm._pack_heads(out, "out", 2, 128), None, None, 0,
-            ilpm._stream_handle())
+    call = (decode_abi.cache(t["kp"], t["vp"], t["table"], ilpm.BF16), decode_abi.heads(t["q"], ilpm.BF16),
+            t["lengths"].data_ptr(), decode_abi.OPTIONS.pack(0, 0, 128 ** -0.5, 0.0, 0, 0, 0),
+            decode_abi.heads(out, ilpm.BF16), None, None, 0, ilpm._stream_handle())
     try:
         ilpm.set_workspace(ws[:256])
         assert ilpm.lib.ilpm_attn_decode(*call) == ilpm.ERR_WORKSPACE
@@ -366,8 +366,11 @@ def test_attention_repeats_bit_for_bit_on_any_stream():
     torch.cuda.synchronize()
     streams, got = [torch.cuda.Stream() for _ in range(3)], []
     for i in range(9):
-        with torch.cuda.stream(streams[i % 3]):
-            got.append(ilpm.attn_decode(*t.values(), return_lse=True))
+        if i < 6:
+            with torch.cuda.stream(streams[i % 3]):
+                got.append(ilpm.attn_decode(*t.values(), return_lse=True))
+        else:
+            got.append(ilpm.attn_decode(*t.values(), return_lse=True, stream=streams[i % 3]))
     torch.cuda.synchronize()
     for o, l in got:
         assert torch.equal(o, want[0]) and torch.equal(l, want[1])
