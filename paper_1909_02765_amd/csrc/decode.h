@@ -39,6 +39,15 @@ struct AppendArgs {
 hipError_t append_launch(const AppendArgs &a, int x_dtype, int cache_dtype, hipStream_t stream);
 
 // ---- attn_decode ----
+constexpr int kAttnHeads = 16;  // query heads of a workgroup
+constexpr int kAttnCus = 256;   // compute units of the card
+constexpr int kMinShare = 8;    // tiles of 16 keys: a workgroup's smallest share (two tiles a wave)
+
+// A unit (key head x block of its query heads) that `count` workgroups share.
+struct AttnPart {
+    int seq, unit, count, pad;
+};
+
 struct AttnArgs {
     const void *q;
     int64_t q_row, q_head;
@@ -46,6 +55,7 @@ struct AttnArgs {
     int64_t o_row, o_head;
     float *lse;  // [n_seqs][q_heads] or NULL
     int q_dtype;
+    bool q_pieces;  // rows of q lie in 16-byte pieces
     const void *k, *v;
     int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
     const int32_t *table;
@@ -59,13 +69,21 @@ struct AttnArgs {
     int window;
     float scale, softcap;
     int n_seqs, q_heads, kv_heads, group, dim;
-    int chunk, splits;  // keys of a split, and splits of the longest sequence planned for
-    float *part_o;      // [n_seqs][q_heads][splits][dim]
-    float *part_ml;     // [n_seqs][q_heads][splits][2]
+    int blocks;  // of up to kAttnHeads query heads of a key head
+    int grid;
+    bool split;  // the workgroups share all tiles out (else each takes a unit)
+    int part_heads;  // heads of a part
+    // The workspace of a split call: for each workgroup the unit that it began
+    // and others went on with; its two parts (the one that goes on with a unit,
+    // the one that begins one), each its sums [part_heads][dim] and its maximum
+    // and sum [part_heads][2].
+    AttnPart *parts;
+    float *part_o, *part_ml;
 };
-// Fills chunk and splits for sequences of up to max_len visible keys; the
-// workspace bytes that they need.
-size_t attn_plan(AttnArgs *a, int max_len);
+// Fills blocks, grid, split and part_heads for sequences of up to max_len keys; the
+// workspace bytes that they need, and their places in it.
+size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len);
+void attn_workspace(AttnArgs *a, void *ws);
 hipError_t attn_launch(const AttnArgs &a, int cache_dtype, hipStream_t stream);
 
 // ---- residual_norm ----

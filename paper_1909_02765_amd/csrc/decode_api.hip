@@ -127,7 +127,7 @@ int capacity_of(const ilpm_kv_cache &c)
     return (int)std::min<int64_t>((int64_t)c.max_pages * c.page_size, INT_MAX - 4096);
 }
 
-int attn_sizes(const ilpm_kv_cache *c, int q_heads, int window, int max_len, AttnArgs *a, size_t *bytes)
+int attn_sizes(const ilpm_kv_cache *c, int q_heads, bool q32, int window, int max_len, AttnArgs *a, size_t *bytes)
 {
     if (q_heads <= 0 || q_heads % c->kv_heads != 0 || window < 0 || max_len < 0) return ILPM_ERR_INVALID_ARG;
     if (c->head_dim > 256) return ILPM_ERR_UNSUPPORTED;
@@ -139,7 +139,7 @@ int attn_sizes(const ilpm_kv_cache *c, int q_heads, int window, int max_len, Att
     a->dim = c->head_dim;
     a->window = window;
     a->capacity = capacity_of(*c);
-    *bytes = attn_plan(a, max_len > 0 ? std::min(max_len, a->capacity) : a->capacity);
+    *bytes = attn_plan(a, c->dtype, q32, max_len > 0 ? std::min(max_len, a->capacity) : a->capacity);
     return ILPM_OK;
 }
 
@@ -244,7 +244,7 @@ int attn_decode(const ilpm_kv_cache *cache, const ilpm_heads *q, const int32_t *
     if (!q || !out || !opt || q->heads <= 0 || out->heads != q->heads) return ILPM_ERR_INVALID_ARG;
     AttnArgs a = {};
     size_t need = 0;
-    if ((rc = attn_sizes(cache, q->heads, opt->window, opt->max_len, &a, &need)) != ILPM_OK) return rc;
+    if ((rc = attn_sizes(cache, q->heads, q->dtype == ILPM_F32, opt->window, opt->max_len, &a, &need)) != ILPM_OK) return rc;
     if (!std::isfinite(opt->scale) || !(opt->softcap >= 0.f) || !std::isfinite(opt->softcap)) return ILPM_ERR_INVALID_ARG;
     if (opt->mask && (opt->mask_len < 0 || !stride_ok(opt->mask_stride))) return ILPM_ERR_INVALID_ARG;
     if (c.n_seqs == 0) return ILPM_OK;
@@ -307,8 +307,7 @@ int attn_decode(const ilpm_kv_cache *cache, const ilpm_heads *q, const int32_t *
     a.mask_len = opt->mask_len;
     a.scale = opt->scale;
     a.softcap = opt->softcap;
-    a.part_o = (float *)ws;
-    a.part_ml = a.part_o + (size_t)a.n_seqs * a.q_heads * a.splits * a.dim;
+    if (a.split) attn_workspace(&a, ws);
     (void)hipGetLastError();
     const hipError_t e = attn_launch(a, c.dtype, stream);
     return e == hipSuccess ? ILPM_OK : api_hip_fail(e);
@@ -424,7 +423,12 @@ int ilpm_attn_decode_workspace_size(const ilpm_kv_cache *cache, int q_heads, int
     int rc = check_cache_sizes(cache);
     if (rc != ILPM_OK) return rc;
     AttnArgs a = {};
-    return attn_sizes(cache, q_heads, window, max_len, &a, bytes);
+    // Of either type of queries, the larger.
+    size_t other = 0;
+    if ((rc = attn_sizes(cache, q_heads, true, window, max_len, &a, &other)) != ILPM_OK) return rc;
+    rc = attn_sizes(cache, q_heads, false, window, max_len, &a, bytes);
+    *bytes = std::max(*bytes, other);
+    return rc;
 }
 
 int ilpm_residual_norm(const ilpm_residual_norm_args *args, hipStream_t stream)

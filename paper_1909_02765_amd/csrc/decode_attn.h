@@ -1,26 +1,39 @@
 // attn_decode's kernel: attention of one new token a sequence over a paged
 // cache,
 //   x_j = scale <q, k_j>,  out = sum e^(x_j - m) v_j / sum e^(x_j - m),  m = max x_j,
-// in one pass over the keys with the running maximum and sum of the softmax,
-// split over the length and joined (decode_attn.hip).
+// in one pass over the keys with the running maximum and sum of the softmax.
 //
 // Both products run on the matrix cores, 16 keys x 16 query heads of one key
 // head at a time.  The first gives the scores transposed, S[key][head] = sum_d
 // K[key][d] Q[head][d], so that lane (n, g) = (lane % 16, lane / 16) holds keys
-// 4g..4g+3 of head n.  That is the layout in which the second one
-// (v_mfma_f32_16x16x4_f32) wants its operand, O[d][head] = sum_key V[key][d]
-// P[key][head], with keys 4g + r as the contraction of instruction r: the
-// probabilities stay in 32 bits and never leave their lane, the statistics of a
-// head are one value per lane, and a lane's V operand is V[4g + r][d], an element
-// of a row that it loads as it lies in memory (a 16-bit second product would
-// want values of several keys in one register, and probabilities of 16 bits).
-// The first product takes the 16-bit instruction (16x16x32) where queries and
-// cache are of one 16-bit type, as both are exact there, else the 32-bit one.
+// 4g..4g+3 of head n.  That is the layout in which the second one wants its
+// operand, O[d][head] = sum_key V[key][d] P[key][head], with keys 4g..4g+3 of
+// the contraction in lane (n, g): the probabilities never leave their lane, and
+// the statistics of a head are one value per lane.  A lane's V operand is values
+// V[4g..4g+3][d], of rows that it loads as they lie in memory.
 //
-// What bounds it: the cache's bytes.  A tile of 16 keys of 128 16-bit values is 8
-// KiB and keeps a SIMD's matrix core busy for 1088 cycles, 30 bytes a cycle for
-// a compute unit, where its share of the memory's rate is 8.
+//   f32 cache: 16x16x4 instructions on 32-bit values, one key of each lane a time.
+//   16-bit cache: 16x16x32 for the scores; for the second product 16x16x16, whose
+//     operand of four keys comes together from four rows by byte permutations,
+//     and in them keys that are not seen become 0.  Probabilities, and queries
+//     of 32 bits, go in as 16-bit parts whose sum keeps their bits (hi = the value
+//     rounded, the next part what is left): queries in three; probabilities in two
+//     (16 bits of bf16, 22 of f16, more than an output of the type keeps), or
+//     three under 32-bit queries over bf16.  f16 parts are scaled by powers of two
+//     so that none of their bits fall below f16's smallest values.  The first part
+//     has an accumulator of its own: an infinity in the cache makes infinities or
+//     NaN of it as the definition does, while the products with the small parts may
+//     be NaN where it has none (0 times infinity), and are left out if so.
+//
+// How the work is divided: the tiles of 16 keys of all (sequence, key head)
+// units lie in one row, which the workgroups share out evenly, as many as the
+// card holds at once (see Share).  A workgroup takes its share unit by unit; a
+// unit that spans workgroups leaves partial results, which attn_join adds.
+//
+// What bounds it: the cache's bytes.
 #pragma once
+
+#include <climits>
 
 #include "decode.h"
 
@@ -30,41 +43,31 @@ namespace {
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kHeads = 16;  // query heads of a workgroup
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // How rows lie in memory: whole (16-byte pieces, dim is the class's size), in
 // 16-byte pieces, or in no such order (element by element).
 enum Rows { kWhole, kPieces, kAny };
 
-__device__ inline float load_f32(const void *p, int64_t i, int dtype)
-{
-    if (dtype == ILPM_F32) return ((const float *)p)[i];
-    if (dtype == ILPM_F16) return (float)((const _Float16 *)p)[i];
-    return (float)((const __bf16 *)p)[i];
-}
-
-__device__ inline void store_f32(void *p, int64_t i, int dtype, float v)
-{
-    if (dtype == ILPM_F32) ((float *)p)[i] = v;
-    else if (dtype == ILPM_F16) ((_Float16 *)p)[i] = (_Float16)v;
-    else ((__bf16 *)p)[i] = (__bf16)v;
-}
-
 // The keys of a sequence that the window leaves: [first, end).
-__device__ inline void visible_range(const AttnArgs &a, int seq, int *first, int *end)
+__device__ inline void visible_range(const AttnArgs &a, int length, int *first, int *end)
 {
-    const int length = a.lengths[seq], n = min(max(length, 0), a.capacity);
+    const int n = min(max(length, 0), a.capacity);
     *end = n;
     // (The window counts from the sequence's own length, also where the table ends before it.)
     *first = a.window > 0 ? min(n, max(length - a.window, 0)) : 0;
 }
 
-// Splits that a sequence's visible keys fill.
-__device__ inline int splits_of(const AttnArgs &a, int keys)
+// Tiles of 16 keys of a unit of a sequence of this length; 1 for one without
+// keys, so that somebody writes its output.
+__device__ inline int tiles_of(const AttnArgs &a, int length)
 {
-    return min((int)(((int64_t)keys + a.chunk - 1) / a.chunk), a.splits);
+    int first, end;
+    visible_range(a, length, &first, &end);
+    return max(1, (int)(((unsigned)(end - first) + 15) / 16));
 }
 
 // The maximum over the four lanes of a head (n, 0..3).  (The halves of a swap
@@ -80,29 +83,85 @@ __device__ inline float max_of_head(float v)
     return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
-// N elements of a row from element d on.  What lies beyond `dim` is 0 with
-// ZERO, else any of the row's own values.
-template <typename T, int N, Rows R, bool ZERO> __device__ inline Pack<T, N> load_row(const T *row, int d, int dim)
+// tanh to a few units of the last place: its series near 0, where the form by
+// the exponential would lose bits, else 1 - 2 / (e^2x + 1).
+__device__ inline float tanh_of(float x)
+{
+    const float x2 = x * x;
+    float near = 62.f / 2835.f;
+    near = near * x2 - 17.f / 315.f;
+    near = near * x2 + 2.f / 15.f;
+    near = near * x2 - 1.f / 3.f;
+    near = near * x2 * x + x;
+    const float e = __builtin_amdgcn_exp2f(fminf(fabsf(x), 20.f) * (2.f * kLog2e));
+    float far = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x);
+    asm("" : "+v"(near), "+v"(far));  // (both, without a branch)
+    far = x != x ? x : far;
+    return fabsf(x) < 0.25f ? near : far;
+}
+
+// N elements of a row from element d on.  Beyond `dim` they are any of the
+// row's own values (cleared where they matter, once they have arrived).
+template <typename T, int N, Rows R> __device__ inline Pack<T, N> load_row(const T *row, int d, int dim)
 {
     Pack<T, N> p;
     if constexpr (R == kAny) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) p.v[i] = d + i < dim ? row[d + i] : (T)0.f;
+        for (int i = 0; i < N; ++i) p.v[i] = row[min(d + i, dim - 1)];
     } else {
         p = *reinterpret_cast<const Pack<T, N> *>(row + (R == kWhole || d < dim ? d : 0));
-        if (R == kPieces && ZERO && d >= dim) p = Pack<T, N>{};
     }
     return p;
 }
 
-// TC: the cache's type.  Q16: the queries are of that same 16-bit type (else
-// any, taken in 32 bits).  DC: the head size's class (64, 128 or 256).
+// p with what lies beyond `dim` cleared.
+template <typename T, int N, Rows R> __device__ inline Pack<T, N> cleared(Pack<T, N> p, int d, int dim)
+{
+    if constexpr (R != kWhole) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p.v[i] = d + i < dim ? p.v[i] : (T)0.f;
+    }
+    return p;
+}
+
+__device__ inline floatx4 mfma_scores(const Pack<__bf16, 8> &k, const Pack<__bf16, 8> &q, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+}
+__device__ inline floatx4 mfma_scores(const Pack<_Float16, 8> &k, const Pack<_Float16, 8> &q, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k), __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
+}
+// (An f32 cache never comes to these.)
+__device__ inline floatx4 mfma_scores(const Pack<float, 4> &, const Pack<float, 4> &, floatx4 c) { return c; }
+__device__ inline floatx4 mfma_values(uint2, const Pack<float, 4> &, floatx4 c) { return c; }
+__device__ inline floatx4 mfma_values(uint2 v, const Pack<__bf16, 4> &p, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(shortx4, v), __builtin_bit_cast(shortx4, p), c, 0, 0, 0);
+}
+__device__ inline floatx4 mfma_values(uint2 v, const Pack<_Float16, 4> &p, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, v), __builtin_bit_cast(f16x4, p), c, 0, 0, 0);
+}
+
+// TC: the cache's type.  Q16: queries and outputs are of that same 16-bit type
+// (else f32).  DC: the head size's class (64, 96, 128, 192 or 256).
 template <typename TC, bool Q16, int DC, Rows R> struct AttnKernel {
+    static constexpr bool C16 = sizeof(TC) == 2;
     static constexpr int KV = 16 / (int)sizeof(TC);          // elements of a K load
     static constexpr int NK = DC / (4 * KV);                 // K loads of a lane
-    static constexpr int VV = KV < DC / 16 ? KV : DC / 16;   // elements of a V load
-    static constexpr int NV = DC / (16 * VV);                // V loads of a lane and key
+    // Elements of a V load: 16 bytes, or 8 where sixteen lanes then make up the row.
+    static constexpr int VV = C16 && DC != 64 && DC != 192 ? 8 : 4;
+    static constexpr int NV = (DC + 16 * VV - 1) / (16 * VV);  // V loads of a lane and key
     static constexpr int NO = NV * VV;                       // output tiles of 16 values
+    static constexpr int DO = NO * 16;                       // values that they hold
+    static constexpr int QP = C16 && !Q16 ? 3 : 1;           // parts of a query
+    static constexpr int PP = __is_same(TC, __bf16) && !Q16 ? 3 : 2;  // parts of a probability (16-bit caches)
+    // f16: probabilities go in times 2^SHIFT.
+    static constexpr int SHIFT = __is_same(TC, _Float16) ? 15 : 0;
+    // Workgroups that a compute unit holds at once (waves of a SIMD): what the
+    // registers of two tiles, the queries and the output leave.
+    static constexpr int PER_CU = DC == 64 ? (C16 && !Q16 ? 3 : 4) : DC <= 128 ? 2 : 1;
     // A tile of 16 keys: lane (n, g) holds pieces g, g + 4, ... of key n's K row,
     // and pieces n, n + 16, ... of the V rows of keys 4g..4g+3.
     struct Tile {
@@ -118,36 +177,128 @@ struct Places {
     int64_t k[64], v[64];
 };
 
-template <typename TC, bool Q16, int DC, Rows R> __global__ __launch_bounds__(256) void attn_split(AttnArgs a)
+// How the tiles are shared out: in shares of `tiles`, or (whole) a unit to a
+// workgroup at a time, where the units are short and too few to fill the card.
+// (All units together have less than 2^31 tiles: attn_plan.)
+struct Share {
+    int total;  // tiles of all units
+    int tiles;
+    bool whole;
+};
+
+// What is the same in all lanes, as the compiler cannot know of values from LDS.
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+struct FindShare {
+    int sum[4], top[4];
+    int seq, tiles, before;
+};
+
+// The sum over the workgroup of a value of each thread; *up_to: the sum up to
+// and with this thread's.
+__device__ inline int scan256(int v, int *up_to, FindShare &f)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll 1
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    __syncthreads();
+    if (lane == 63) f.sum[wave] = v;
+    __syncthreads();
+    const int s0 = f.sum[0], s1 = s0 + f.sum[1], s2 = s1 + f.sum[2];
+    *up_to = v + (wave == 0 ? 0 : wave == 1 ? s0 : wave == 2 ? s1 : s2);
+    return uniform(s2 + f.sum[3]);
+}
+
+// Units of a sequence (key heads x blocks of up to 16 of their query heads).
+__device__ inline int units_of(const AttnArgs &a) { return a.kv_heads * a.blocks; }
+
+// The shares of this call, and the sequence in which share `wg` begins (f.seq,
+// its tiles per unit f.tiles, and the tiles of all units before it, f.before).
+__device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f)
+{
+    const int tid = threadIdx.x, units = units_of(a);
+    int mine = 0, top = 0, total, up_to;
+    if (a.n_seqs == 1) {
+        total = top = tiles_of(a, uniform(a.lengths[0]));
+        f.seq = f.before = 0;
+        f.tiles = top;
+    } else {
+        for (int i = tid; i < a.n_seqs; i += 256) {
+            const int t = tiles_of(a, a.lengths[i]);
+            mine += t;
+            top = max(top, t);
+        }
+#pragma unroll 1
+        for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
+        if ((tid & 63) == 0) f.top[tid >> 6] = top;
+        total = scan256(mine, &up_to, f);
+        top = uniform(max(max(f.top[0], f.top[1]), max(f.top[2], f.top[3])));
+    }
+    Share s;
+    s.total = total * units;
+    const int even = (int)(((unsigned)s.total + gridDim.x - 1) / gridDim.x);
+    s.tiles = max(kMinShare, (even + 3) / 4 * 4);
+    s.whole = s.tiles == kMinShare && top <= 2 * kMinShare;
+    if (s.whole || a.n_seqs == 1) return s;
+    // The sequence that holds tile wg * s.tiles, counted in tiles of one unit.
+    const int want = (int)min((int64_t)wg * s.tiles / units, (int64_t)INT_MAX);
+    int carry = 0;
+    for (int i0 = 0; i0 < a.n_seqs && want >= carry; i0 += 256) {
+        const int t = i0 + tid < a.n_seqs ? tiles_of(a, a.lengths[i0 + tid]) : 0;
+        // (Up to 256 sequences the sums are there.)
+        const int sum = a.n_seqs <= 256 ? total : scan256(t, &up_to, f);
+        const int to = carry + up_to;
+        if (want >= to - t && want < to) {
+            f.seq = i0 + tid;
+            f.tiles = t;
+            f.before = (to - t) * units;
+        }
+        carry += sum;
+    }
+    __syncthreads();
+    return s;
+}
+
+// Some of a unit's keys, as a workgroup takes them.
+struct Segment {
+    int seq, kvh, hb;
+    int k0, k1;  // [k0, k1) of the sequence's tokens
+};
+
+template <int DO> struct AttnLds {
+    Places places[4][2];
+    // Each wave's maxima, sums and outputs of a segment (the rows 4 banks apart).
+    float m[4][kAttnHeads], l[4][kAttnHeads];
+    float o[4][kAttnHeads][DO + 4];
+    FindShare found;
+};
+
+// A wave's part of a segment, every fourth tile of it, its results left in LDS.
+template <typename TC, bool Q16, int DC, Rows R>
+__device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &seg, AttnLds<AttnKernel<TC, Q16, DC, R>::DO> &lds)
 {
     using Cfg = AttnKernel<TC, Q16, DC, R>;
     using Tile = typename Cfg::Tile;
+    using TQ = std::conditional_t<Q16, TC, float>;
     constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
-    __shared__ Places places[4][2];
-    __shared__ float sm[4][kHeads], sl[4][kHeads];
-    __shared__ float so[2][64][NO * 4 + 1];
+    constexpr int QP = Cfg::QP, PP = Cfg::PP;
+    constexpr bool C16 = Cfg::C16;
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // (Formed anew for each segment: kept over them, what comes of the lane
+    // would take the registers that the tiles need.)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int wave = uniform((int)(threadIdx.x >> 6));
     const int n16 = lane & 15, g = lane >> 4;
-    const int blocks = (a.group + kHeads - 1) / kHeads;      // of a key head's query heads
-    int id = blockIdx.x;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int hb = id % blocks;
-    id /= blocks;
-    const int kvh = id % a.kv_heads, seq = id / a.kv_heads;
-    const int in_group = hb * kHeads + n16;                  // this lane's query head
+    const int in_group = seg.hb * kAttnHeads + n16;  // this lane's query head
     const bool has_head = in_group < a.group;
-    const int head = kvh * a.group + in_group;
-
-    int first, end;
-    visible_range(a, seq, &first, &end);
-    const int ns = splits_of(a, end - first);
-    if (split >= max(ns, 1)) return;
-    const int k0 = first + split * a.chunk;
-    const int k1 = split == a.splits - 1 ? end : min(k0 + a.chunk, end);
-    // Tile j of this wave is tile 4j + wave of the split.
-    const int tiles = max(0, ((k1 - k0 + 15) / 16 - wave + 3) / 4);
+    const int seq = seg.seq, k0 = seg.k0, k1 = seg.k1;
+    // Tile j of this wave is tile 4j + wave of the segment.  (None where there
+    // are no keys: then there may be no pool either.)
+    const int tiles = max(0, ((int)(((unsigned)(k1 - k0) + 15) / 16) - wave + 3) / 4);
 
     // Lane (n, t) looks up key n of tile 4*group + t.
     struct Entry {
@@ -157,16 +308,16 @@ template <typename TC, bool Q16, int DC, Rows R> __global__ __launch_bounds__(25
         Entry e = {-1, 0};
         const int64_t key = k0 + ((int64_t)(group * 4 + g) * 4 + wave) * 16 + n16;
         if (key < k1) {
-            const int at = (int)key / a.page_size;
-            e.slot = (int)key - at * a.page_size;
-            e.page = a.table[(int64_t)seq * a.table_stride + at];
+            const int p = (int)key / a.page_size;
+            e.slot = (int)key - p * a.page_size;
+            e.page = a.table[(int64_t)seq * a.table_stride + p];
             if (a.mask && (key >= a.mask_len || !a.mask[(int64_t)seq * a.mask_stride + key])) e.page = -1;
         }
         return e;
     };
     auto place = [&](int group, Entry e) {
         const bool ok = e.page >= 0 && e.page < a.n_pages;
-        Places &p = places[wave][group & 1];
+        Places &p = lds.places[wave][group & 1];
         p.k[lane] = ok ? (int64_t)e.page * a.k_page + (int64_t)e.slot * a.k_slot : -1;
         p.v[lane] = ok ? (int64_t)e.page * a.v_page + (int64_t)e.slot * a.v_slot : -1;
         // (Only this wave reads them, and a wave's LDS accesses keep their order.)
@@ -174,73 +325,113 @@ template <typename TC, bool Q16, int DC, Rows R> __global__ __launch_bounds__(25
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
-    const TC *kh = (const TC *)a.k + (int64_t)kvh * a.k_head;
-    const TC *vh = (const TC *)a.v + (int64_t)kvh * a.v_head;
+    const TC *kh = (const TC *)a.k + (int64_t)seg.kvh * a.k_head;
+    const TC *vh = (const TC *)a.v + (int64_t)seg.kvh * a.v_head;
     // A key that is not seen reads the pool's first row, and none of it is used.
     auto load = [&](int j, Tile &t) {
-        const Places &p = places[wave][(j >> 2) & 1];
-        const int at = (j & 3) * 16;
-        const TC *krow = kh + max(p.k[at + n16], (int64_t)0);
+        const Places &p = lds.places[wave][(j >> 2) & 1];
+        const int i0 = (j & 3) * 16;
+        const TC *krow = kh + max(p.k[i0 + n16], (int64_t)0);
 #pragma unroll
-        for (int c = 0; c < NK; ++c) t.k[c] = load_row<TC, KV, R, true>(krow, (g + 4 * c) * KV, a.dim);
+        for (int c = 0; c < NK; ++c) t.k[c] = load_row<TC, KV, R>(krow, (g + 4 * c) * KV, a.dim);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int64_t vo = p.v[at + 4 * g + r];
+            const int64_t vo = p.v[i0 + 4 * g + r];
             t.seen[r] = vo >= 0;
             const TC *vrow = vh + max(vo, (int64_t)0);
 #pragma unroll
-            for (int c = 0; c < NV; ++c) t.v[r][c] = load_row<TC, VV, R, false>(vrow, (n16 + 16 * c) * VV, a.dim);
+            for (int c = 0; c < NV; ++c) t.v[r][c] = load_row<TC, VV, R>(vrow, (n16 + 16 * c) * VV, a.dim);
         }
     };
-
     Entry next = {};
     if (tiles > 0) {
         place(0, look_up(0));
         if (tiles > 4) next = look_up(1);
     }
 
-    // The queries, in the layout of the K loads.
-    Pack<TC, KV> q16[NK];
-    float q32[NK][KV];
+    // The queries, in the layout of the K loads.  (Lanes without a head take
+    // the last one's, and give nothing.)
+    Pack<std::conditional_t<QP == 3, TC, TQ>, KV> q[QP][NK];
+    float unscale = 1.f;  // f16 parts of 32-bit queries are those of the queries over this
+    {
+        const TQ *row = (const TQ *)a.q + (int64_t)seq * a.q_row + ((int64_t)seg.kvh * a.group + min(in_group, a.group - 1)) * a.q_head;
+        Pack<TQ, KV> whole[NK];
+        if (a.q_pieces) {
 #pragma unroll
-    for (int c = 0; c < NK; ++c)
+            for (int c = 0; c < NK; ++c) whole[c] = load_row<TQ, KV, R == kAny ? kPieces : R>(row, (g + 4 * c) * KV, a.dim);
+        } else {
 #pragma unroll
-        for (int i = 0; i < KV; ++i) {
-            const int d = (g + 4 * c) * KV + i;
-            const bool ok = has_head && d < a.dim;
-            const int64_t at = (int64_t)seq * a.q_row + (int64_t)head * a.q_head + d;
-            if constexpr (Q16) q16[c].v[i] = ok ? ((const TC *)a.q)[at] : (TC)0.f;
-            else q32[c][i] = ok ? load_f32(a.q, at, a.q_dtype) : 0.f;
+            for (int c = 0; c < NK; ++c) whole[c] = load_row<TQ, KV, kAny>(row, (g + 4 * c) * KV, a.dim);
         }
-
-    floatx4 o[NO];
 #pragma unroll
-    for (int i = 0; i < NO; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < NK; ++c) whole[c] = cleared<TQ, KV, R>(whole[c], (g + 4 * c) * KV, a.dim);
+        if constexpr (QP == 3) {
+            float f = 1.f;
+            if constexpr (__is_same(TC, _Float16)) {
+                // The largest becomes 2^14 to 2^15: parts keep what is above 2^-39 of it.
+                float most = 0.f;
+#pragma unroll
+                for (int c = 0; c < NK; ++c)
+#pragma unroll
+                    for (int i = 0; i < KV; ++i) most = fmaxf(most, fabsf(whole[c].v[i]));
+                most = max_of_head(most);
+                const int e = (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127;  // 2^e <= most < 2^(e+1)
+                const int by = most > 0.f && e < 128 ? min(14 - e, 126) : 0;
+                f = __builtin_ldexpf(1.f, by);
+                unscale = __builtin_ldexpf(1.f, -by);
+            }
+#pragma unroll
+            for (int c = 0; c < NK; ++c)
+#pragma unroll
+                for (int i = 0; i < KV; ++i) {
+                    float v = whole[c].v[i] * f;
+                    q[0][c].v[i] = (TC)v;
+                    v -= (float)q[0][c].v[i];
+                    q[1][c].v[i] = (TC)v;
+                    q[2][c].v[i] = (TC)(v - (float)q[1][c].v[i]);
+                }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NK; ++c) q[0][c] = whole[c];
+        }
+    }
+
+    floatx4 o[NO], ol[C16 ? NO : 1];  // (ol: of the probabilities' small parts)
     float m = -INFINITY, l = 0.f;
-    const float scale2 = a.softcap > 0.f ? a.scale / a.softcap : a.scale * kLog2e;
+    const float scale2 = (a.softcap > 0.f ? a.scale / a.softcap : a.scale * kLog2e) * unscale;
     const float cap2 = a.softcap * kLog2e;
 
     auto compute = [&](const Tile &t) {
         floatx4 s = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (!C16) {
 #pragma unroll
-        for (int c = 0; c < NK; ++c) {
-            if constexpr (Q16 && sizeof(TC) == 2 && __is_same(TC, __bf16)) {
-                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[c]),
-                                                            __builtin_bit_cast(bf16x8, q16[c]), s, 0, 0, 0);
-            } else if constexpr (Q16) {
-                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, t.k[c]),
-                                                           __builtin_bit_cast(f16x8, q16[c]), s, 0, 0, 0);
-            } else {
+            for (int c = 0; c < NK; ++c) {
+                const Pack<TC, KV> k = cleared<TC, KV, R>(t.k[c], (g + 4 * c) * KV, a.dim);
 #pragma unroll
                 for (int i = 0; i < KV; ++i)
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32((float)t.k[c].v[i], q32[c][i], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32((float)k.v[i], (float)q[0][c].v[i], s, 0, 0, 0);
+            }
+        } else {
+            floatx4 low = s;
+#pragma unroll
+            for (int c = 0; c < NK; ++c) {
+                const Pack<TC, KV> k = cleared<TC, KV, R>(t.k[c], (g + 4 * c) * KV, a.dim);
+                s = mfma_scores(k, q[0][c], s);
+                if constexpr (QP == 3) {
+                    low = mfma_scores(k, q[1][c], low);
+                    low = mfma_scores(k, q[2][c], low);
+                }
+            }
+            if constexpr (QP == 3) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[r] += low[r] - low[r] == 0.f ? low[r] : 0.f;
             }
         }
         float top = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float x = s[r] * scale2;
-            if (a.softcap > 0.f) x = cap2 * tanhf(x);
+            if (a.softcap > 0.f) x = cap2 * tanh_of(x);
             s[r] = t.seen[r] ? x : -INFINITY;
             top = fmaxf(top, s[r]);
         }
@@ -251,24 +442,69 @@ template <typename TC, bool Q16, int DC, Rows R> __global__ __launch_bounds__(25
             m = m_new;
             l *= alpha;
 #pragma unroll
-            for (int i = 0; i < NO; ++i) o[i] *= alpha;
+            for (int i = 0; i < NO; ++i) {
+                o[i] *= alpha;
+                if constexpr (C16) ol[i] *= alpha;
+            }
         }
         float p[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - base);
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - base + (float)Cfg::SHIFT);
         l += (p[0] + p[1]) + (p[2] + p[3]);
+        if constexpr (!C16) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < NV; ++c)
+#pragma unroll
+                    for (int i = 0; i < VV; ++i)
+                        o[c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.seen[r] ? (float)t.v[r][c].v[i] : 0.f, p[r],
+                                                                            o[c * VV + i], 0, 0, 0);
+        } else {
+            Pack<TC, 4> part[PP];
+#pragma unroll
+            for (int i = 0; i < PP; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    part[i].v[r] = (TC)p[r];
+                    p[r] -= (float)part[i].v[r];
+                }
+            // Selectors of the lower and the upper halves of two rows' registers: a byte 0x0c gives 0.
+            unsigned lower[2], upper[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned keep = (t.seen[2 * h] ? 0xffffu : 0u) | (t.seen[2 * h + 1] ? 0xffff0000u : 0u);
+                lower[h] = (0x05040100u & keep) | (0x0c0c0c0cu & ~keep);
+                upper[h] = (0x07060302u & keep) | (0x0c0c0c0cu & ~keep);
+            }
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
-                for (int i = 0; i < VV; ++i)
-                    o[c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.seen[r] ? (float)t.v[r][c].v[i] : 0.f, p[r],
-                                                                        o[c * VV + i], 0, 0, 0);
+                for (int i = 0; i < VV; ++i) {
+                    struct Words {
+                        unsigned w[VV / 2];
+                    };
+                    unsigned w[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) w[r] = __builtin_bit_cast(Words, t.v[r][c]).w[i / 2];
+                    const uint2 v = {__builtin_amdgcn_perm(w[1], w[0], i & 1 ? upper[0] : lower[0]),
+                                     __builtin_amdgcn_perm(w[3], w[2], i & 1 ? upper[1] : lower[1])};
+#pragma unroll
+                    for (int k = 0; k < PP; ++k) {
+                        floatx4 &sum = k == 0 ? o[c * VV + i] : ol[c * VV + i];
+                        sum = mfma_values(v, part[k], sum);
+                    }
+                }
+        }
     };
 
     // While a tile is computed the next one's rows are on their way, and the
     // next group's table entries.
+#pragma unroll
+    for (int i = 0; i < NO; ++i) {
+        o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (C16) ol[i] = o[i];
+    }
     Tile buf[2];
     if (tiles > 0) load(0, buf[0]);
     for (int j = 0; j < tiles; j += 2) {
@@ -281,66 +517,131 @@ template <typename TC, bool Q16, int DC, Rows R> __global__ __launch_bounds__(25
         if (j + 2 < tiles) load(j + 2, buf[0]);
         if (j + 1 < tiles) compute(buf[1]);
     }
-
-    // Join the four waves: l first over the lanes of a head, then all to their
-    // common maximum.
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (g == 0) {
-        sm[wave][n16] = m;
-        sl[wave][n16] = l;
+    if constexpr (C16) {
+#pragma unroll
+        for (int i = 0; i < NO; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[i][r] += ol[i][r] - ol[i][r] == 0.f ? ol[i][r] : 0.f;
     }
-    __syncthreads();
-    const float top = fmaxf(fmaxf(sm[0][n16], sm[1][n16]), fmaxf(sm[2][n16], sm[3][n16]));
-    const float base = top == -INFINITY ? 0.f : top;
-    l = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) l += sl[w][n16] * __builtin_amdgcn_exp2f(sm[w][n16] - base);
-    const float f = __builtin_amdgcn_exp2f(m - base);
-#pragma unroll
-    for (int i = 0; i < NO; ++i) o[i] *= f;
-    auto give = [&](int slot) {
-#pragma unroll
-        for (int i = 0; i < NO; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) so[slot][lane][i * 4 + r] = o[i][r];
-    };
-    auto take = [&](int slot) {
-#pragma unroll
-        for (int i = 0; i < NO; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[i][r] += so[slot][lane][i * 4 + r];
-    };
-    if (wave >= 2) give(wave - 2);
-    __syncthreads();
-    if (wave < 2) take(wave);
-    if (wave == 1) give(1);
-    __syncthreads();
-    if (wave != 0 || !has_head) return;
-    take(1);
-    const bool whole = ns <= 1;
-    const int64_t row = (int64_t)seq * a.q_heads + head;
-    const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-    float *part = whole ? nullptr : a.part_o + (row * a.splits + split) * a.dim;
-#pragma unroll
-    for (int c = 0; c < NV; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int i = 0; i < VV; ++i) {
-                const int d = (4 * g + r + 16 * c) * VV + i;
-                if (d >= a.dim) continue;
-                const float v = o[c * VV + i][r] * inv;
-                if (whole) store_f32(a.out, (int64_t)seq * a.o_row + (int64_t)head * a.o_head + d, a.q_dtype, v);
-                else part[d] = v;
-            }
+    // Lane (n, g) holds values (4g + r + 16c) * VV + i of head n.
     if (g == 0) {
-        if (whole) {
-            if (a.lse) a.lse[row] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
-        } else {
-            float *ml = a.part_ml + (row * a.splits + split) * 2;
-            ml[0] = top;
-            ml[1] = l;
+        lds.m[wave][n16] = m;
+        lds.l[wave][n16] = l;
+    }
+    if (has_head) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                Pack<float, VV> p;
+#pragma unroll
+                for (int i = 0; i < VV; ++i) p.v[i] = o[c * VV + i][r];
+                *reinterpret_cast<Pack<float, VV> *>(&lds.o[wave][n16][(4 * g + r + 16 * c) * VV]) = p;
+            }
+    }
+}
+
+template <typename TC, bool Q16, int DC, Rows R>
+__global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void attn_split(AttnArgs a)
+{
+    using Cfg = AttnKernel<TC, Q16, DC, R>;
+    using TQ = std::conditional_t<Q16, TC, float>;
+    __shared__ AttnLds<Cfg::DO> lds;
+
+    const int units = units_of(a), wg = blockIdx.x;
+    Share share = {0, 0, true};
+    if (a.split) share = find_share(a, wg, lds.found);
+
+    // This workgroup's place in its share.
+    int seq, unit, tile0 = 0, tiles_all;
+    int at = 0, last = 0;
+    if (a.split && threadIdx.x == 0) a.parts[wg] = AttnPart{-1, 0, 0, 0};  // (whatever follows, attn_join reads it)
+    if (share.whole) {
+        if (wg >= a.n_seqs * units) return;
+        seq = wg / units;
+        unit = wg - seq * units;
+        tiles_all = tiles_of(a, uniform(a.lengths[seq]));
+    } else {
+        if ((int64_t)wg * share.tiles >= share.total) return;
+        at = wg * share.tiles;
+        last = (int)min((int64_t)at + share.tiles, (int64_t)share.total);
+        seq = uniform(lds.found.seq);
+        tiles_all = uniform(lds.found.tiles);
+        const int in = at - uniform(lds.found.before);
+        unit = in / tiles_all;
+        tile0 = in - unit * tiles_all;
+    }
+
+    for (;;) {
+        const int seg_tiles = share.whole ? tiles_all : min(tiles_all - tile0, last - at);
+        Segment seg;
+        seg.seq = seq;
+        seg.kvh = unit / a.blocks;
+        seg.hb = unit - seg.kvh * a.blocks;
+        int first, end;
+        visible_range(a, uniform(a.lengths[seq]), &first, &end);
+        seg.k0 = first + tile0 * 16;
+        seg.k1 = (int)min((int64_t)end, (int64_t)seg.k0 + (int64_t)seg_tiles * 16);
+        attn_segment<TC, Q16, DC, R>(a, seg, lds);
+        __syncthreads();
+
+        // Join the four waves; each writes a head at a time.
+        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+        const bool all = seg_tiles == tiles_all;  // of the unit's tiles
+        // The part that begins a unit, or the one that goes on with it.
+        const int64_t part = ((int64_t)wg * 2 + (tile0 == 0 ? 1 : 0)) * a.part_heads;
+        const int heads = min(kAttnHeads, a.group - seg.hb * kAttnHeads), head0 = seg.kvh * a.group + seg.hb * kAttnHeads;
+        for (int h = wave; h < heads; h += 4) {
+            float top = lds.m[0][h], sum = 0.f, f[4];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) top = fmaxf(top, lds.m[w][h]);
+            const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                f[w] = __builtin_amdgcn_exp2f(lds.m[w][h] - base);
+                sum += lds.l[w][h] * f[w];
+            }
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            TQ *out = (TQ *)a.out + (int64_t)seq * a.o_row + (int64_t)(head0 + h) * a.o_head;
+            float *po = a.part_o + (part + h) * a.dim;
+#pragma unroll 1
+            for (int d = lane; d < a.dim; d += 64) {
+                const float v = (lds.o[0][h][d] * f[0] + lds.o[1][h][d] * f[1]) + (lds.o[2][h][d] * f[2] + lds.o[3][h][d] * f[3]);
+                if (all) out[d] = (TQ)(v * inv);
+                else po[d] = v;
+            }
+            if (lane == 0 && all && a.lse)
+                a.lse[(int64_t)seq * a.q_heads + head0 + h] =
+                    sum == 0.f ? -INFINITY : (top + (__builtin_amdgcn_logf(sum) - (float)Cfg::SHIFT)) * kLn2;
+            if (lane == 0 && !all) {
+                a.part_ml[(part + h) * 2] = top - (float)Cfg::SHIFT;
+                a.part_ml[(part + h) * 2 + 1] = sum;
+            }
+        }
+        if (share.whole) {
+            // (Long before 2^31: units are at most 2^24, workgroups too.)
+            const int u = seq * units + unit + (int)gridDim.x;
+            if (!a.split || u >= a.n_seqs * units) return;
+            seq = u / units;
+            unit = u - seq * units;
+            tiles_all = tiles_of(a, uniform(a.lengths[seq]));
+            __syncthreads();  // the LDS that the next unit's waves write has been read
+            continue;
+        }
+        // Who begins a unit that others go on with says so.
+        if (threadIdx.x == 0 && !all && tile0 == 0) {
+            const int rest = tiles_all - seg_tiles;
+            a.parts[wg] = AttnPart{seq, unit, 1 + (int)(((unsigned)rest + share.tiles - 1) / (unsigned)share.tiles), 0};
+        }
+        at += seg_tiles;
+        if (at >= last) return;
+        __syncthreads();  // as above
+        tile0 = 0;
+        if (++unit == units) {
+            unit = 0;
+            tiles_all = tiles_of(a, uniform(a.lengths[++seq]));
         }
     }
 }
@@ -350,18 +651,32 @@ template <typename TC, bool Q16, int DC> hipError_t attn_split_launch(const Attn
     const int64_t step = 16 / (int64_t)sizeof(TC);
     const bool pieces = a.dim % step == 0 && ((uintptr_t)a.k | (uintptr_t)a.v) % 16 == 0 &&
                         (a.k_page | a.k_slot | a.k_head | a.v_page | a.v_slot | a.v_head) % step == 0;
-    const dim3 grid((unsigned)(a.n_seqs * a.kv_heads * ceil_div(a.group, kHeads) * a.splits));
-    if (pieces && a.dim == DC) hipLaunchKernelGGL((attn_split<TC, Q16, DC, kWhole>), grid, dim3(256), 0, stream, a);
-    else if (pieces) hipLaunchKernelGGL((attn_split<TC, Q16, DC, kPieces>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((attn_split<TC, Q16, DC, kAny>), grid, dim3(256), 0, stream, a);
+    AttnArgs args = a;
+    const int64_t qs = Q16 ? sizeof(TC) : 4, qstep = 16 / qs;
+    args.q_pieces = a.dim % step == 0 && (uintptr_t)a.q % 16 == 0 && (a.q_row | a.q_head) % qstep == 0;
+    if (pieces && a.dim == DC) hipLaunchKernelGGL((attn_split<TC, Q16, DC, kWhole>), dim3(a.grid), dim3(256), 0, stream, args);
+    else if (pieces) hipLaunchKernelGGL((attn_split<TC, Q16, DC, kPieces>), dim3(a.grid), dim3(256), 0, stream, args);
+    else hipLaunchKernelGGL((attn_split<TC, Q16, DC, kAny>), dim3(a.grid), dim3(256), 0, stream, args);
     return hipGetLastError();
 }
 
 template <typename TC, bool Q16> hipError_t attn_split_by_dim(const AttnArgs &a, hipStream_t stream)
 {
     if (a.dim <= 64) return attn_split_launch<TC, Q16, 64>(a, stream);
+    if (a.dim <= 96) return attn_split_launch<TC, Q16, 96>(a, stream);
     if (a.dim <= 128) return attn_split_launch<TC, Q16, 128>(a, stream);
+    if (a.dim <= 192) return attn_split_launch<TC, Q16, 192>(a, stream);
     return attn_split_launch<TC, Q16, 256>(a, stream);
+}
+
+// Workgroups of the class of a head size that the card holds at once.
+template <typename TC, bool Q16> int attn_card_by_dim(int dim)
+{
+    return kAttnCus * (dim <= 64    ? AttnKernel<TC, Q16, 64, kWhole>::PER_CU
+                       : dim <= 96  ? AttnKernel<TC, Q16, 96, kWhole>::PER_CU
+                       : dim <= 128 ? AttnKernel<TC, Q16, 128, kWhole>::PER_CU
+                       : dim <= 192 ? AttnKernel<TC, Q16, 192, kWhole>::PER_CU
+                                    : AttnKernel<TC, Q16, 256, kWhole>::PER_CU);
 }
 
 }  // namespace

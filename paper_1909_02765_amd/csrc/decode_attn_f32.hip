@@ -4,5 +4,6 @@
 namespace ilpm {
 
 hipError_t attn_split_f32(const AttnArgs &a, hipStream_t stream) { return attn_split_by_dim<float, false>(a, stream); }
+int attn_card_f32(int dim) { return attn_card_by_dim<float, false>(dim); }
 
 }  // namespace ilpm
