@@ -42,6 +42,7 @@ hipError_t append_launch(const AppendArgs &a, int x_dtype, int cache_dtype, hipS
 constexpr int kAttnHeads = 16;  // query heads of a workgroup
 constexpr int kAttnCus = 256;   // compute units of the card
 constexpr int kMinShare = 8;    // tiles of 16 keys: a workgroup's smallest share (two tiles a wave)
+constexpr int kUnitCost = 6;    // what a unit costs beside its tiles, in tiles
 
 // A unit (key head x block of its query heads) that `count` workgroups share.
 struct AttnPart {

@@ -92,10 +92,10 @@ template <typename TX, typename TC, int VEC, int HPT> __global__ __launch_bounds
     const int vunits = a.dim / VEC;
     const int heads = a.q_heads + a.kv_heads, slots = (heads + HPT - 1) / HPT, vslots = (a.kv_heads + HPT - 1) / HPT;
     const unsigned per = slots * units + vslots * vunits;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const unsigned id = blockIdx.x * 256u + threadIdx.x;  // (at most 2^24 workgroups)
     const int t = (int)(id / per);
     if (t >= a.n_tokens) return;
-    int i = (int)(id - (int64_t)t * per);
+    int i = (int)(id - t * per);
     const int pos = a.positions[t];
 
     if (i >= slots * units) {  // a value's packs

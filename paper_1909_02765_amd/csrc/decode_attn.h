@@ -62,7 +62,9 @@ __device__ inline void visible_range(const AttnArgs &a, int length, int *first, 
 }
 
 // Tiles of 16 keys of a unit of a sequence of this length; 1 for one without
-// keys, so that somebody writes its output.
+// keys, so that somebody writes its output.  What a unit costs beside its tiles
+// counts as kUnitCost of them (without it one workgroup got all the shortest
+// sequences of a batch: 82 us where the others took 25).
 __device__ inline int tiles_of(const AttnArgs &a, int length)
 {
     int first, end;
@@ -177,12 +179,13 @@ struct Places {
     int64_t k[64], v[64];
 };
 
-// How the tiles are shared out: in shares of `tiles`, or (whole) a unit to a
+// How the units are shared out: they lie in one row, each kUnitCost and then
+// its tiles long, cut into shares of `size`; or (whole) a unit goes to a
 // workgroup at a time, where the units are short and too few to fill the card.
-// (All units together have less than 2^31 tiles: attn_plan.)
+// (All units together are shorter than 2^31: attn_plan.)
 struct Share {
-    int total;  // tiles of all units
-    int tiles;
+    int total;  // the row's length
+    int size;
     bool whole;
 };
 
@@ -216,19 +219,20 @@ __device__ inline int scan256(int v, int *up_to, FindShare &f)
 __device__ inline int units_of(const AttnArgs &a) { return a.kv_heads * a.blocks; }
 
 // The shares of this call, and the sequence in which share `wg` begins (f.seq,
-// its tiles per unit f.tiles, and the tiles of all units before it, f.before).
+// the tiles of its units f.tiles, and the length of all units before it, f.before).
 __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f)
 {
     const int tid = threadIdx.x, units = units_of(a);
     int mine = 0, top = 0, total, up_to;
     if (a.n_seqs == 1) {
-        total = top = tiles_of(a, uniform(a.lengths[0]));
+        top = tiles_of(a, uniform(a.lengths[0]));
+        total = top + kUnitCost;
         f.seq = f.before = 0;
         f.tiles = top;
     } else {
         for (int i = tid; i < a.n_seqs; i += 256) {
             const int t = tiles_of(a, a.lengths[i]);
-            mine += t;
+            mine += t + kUnitCost;
             top = max(top, t);
         }
 #pragma unroll 1
@@ -240,20 +244,20 @@ __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f)
     Share s;
     s.total = total * units;
     const int even = (int)(((unsigned)s.total + gridDim.x - 1) / gridDim.x);
-    s.tiles = max(kMinShare, (even + 3) / 4 * 4);
-    s.whole = s.tiles == kMinShare && top <= 2 * kMinShare;
+    s.size = max(kMinShare + kUnitCost, even);
+    s.whole = s.size == kMinShare + kUnitCost && top <= 2 * kMinShare;
     if (s.whole || a.n_seqs == 1) return s;
-    // The sequence that holds tile wg * s.tiles, counted in tiles of one unit.
-    const int want = (int)min((int64_t)wg * s.tiles / units, (int64_t)INT_MAX);
+    // The sequence that holds place wg * s.size, counted in one unit of each.
+    const int want = (int)min((int64_t)wg * s.size / units, (int64_t)INT_MAX);
     int carry = 0;
     for (int i0 = 0; i0 < a.n_seqs && want >= carry; i0 += 256) {
-        const int t = i0 + tid < a.n_seqs ? tiles_of(a, a.lengths[i0 + tid]) : 0;
+        const int t = i0 + tid < a.n_seqs ? tiles_of(a, a.lengths[i0 + tid]) + kUnitCost : 0;
         // (Up to 256 sequences the sums are there.)
         const int sum = a.n_seqs <= 256 ? total : scan256(t, &up_to, f);
         const int to = carry + up_to;
         if (want >= to - t && want < to) {
             f.seq = i0 + tid;
-            f.tiles = t;
+            f.tiles = t - kUnitCost;
             f.before = (to - t) * units;
         }
         carry += sum;
@@ -268,17 +272,69 @@ struct Segment {
     int k0, k1;  // [k0, k1) of the sequence's tokens
 };
 
-template <int DO> struct AttnLds {
+template <typename Cfg, typename TC> struct AttnLds {
     Places places[4][2];
     // Each wave's maxima, sums and outputs of a segment (the rows 4 banks apart).
     float m[4][kAttnHeads], l[4][kAttnHeads];
-    float o[4][kAttnHeads][DO + 4];
+    float o[4][kAttnHeads][Cfg::DO + 4];
     FindShare found;
+    // The three parts of 32-bit queries, as the lanes of the first product take them.
+    Pack<TC, Cfg::KV> q[Cfg::QP == 3 ? 3 : 1][Cfg::QP == 3 ? Cfg::NK : 1][Cfg::QP == 3 ? 64 : 1];
+    float unscale[kAttnHeads];
 };
+
+// The workgroup splits a unit's 32-bit queries into their parts (once for its
+// four waves, and in a loop: instructions that run once cost their fetching).
+template <typename TC, int DC, Rows R, typename Lds> __device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &seg, Lds &lds)
+{
+    using Cfg = AttnKernel<TC, false, DC, R>;
+    constexpr int KV = Cfg::KV, NK = Cfg::NK;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), n16 = lane & 15, g = lane >> 4;
+    const int in_group = min(seg.hb * kAttnHeads + n16, a.group - 1);
+    const float *row = (const float *)a.q + (int64_t)seg.seq * a.q_row + ((int64_t)seg.kvh * a.group + in_group) * a.q_head;
+    auto get = [&](int c) {
+        const int d = (g + 4 * c) * KV;
+        const Pack<float, KV> p = a.q_pieces ? load_row<float, KV, kPieces>(row, d, a.dim) : load_row<float, KV, kAny>(row, d, a.dim);
+        return cleared<float, KV, kPieces>(p, d, a.dim);
+    };
+    float f = 1.f, back = 1.f;
+    if constexpr (__is_same(TC, _Float16)) {
+        // The largest becomes 2^14 to 2^15: parts keep what is above 2^-39 of it.
+        float most = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < NK; ++c) {
+            const Pack<float, KV> p = get(c);
+#pragma unroll
+            for (int i = 0; i < KV; ++i) most = fmaxf(most, fabsf(p.v[i]));
+        }
+        most = max_of_head(most);
+        const int e = (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127;  // 2^e <= most < 2^(e+1)
+        const int by = most > 0.f && e < 128 ? min(14 - e, 126) : 0;
+        f = __builtin_ldexpf(1.f, by);
+        back = __builtin_ldexpf(1.f, -by);
+    }
+    if (wave == 0 && g == 0) lds.unscale[n16] = back;
+#pragma unroll 1
+    for (int c = wave; c < NK; c += 4) {
+        const Pack<float, KV> p = get(c);
+        Pack<TC, KV> part[3];
+#pragma unroll
+        for (int i = 0; i < KV; ++i) {
+            float v = p.v[i] * f;
+            part[0].v[i] = (TC)v;
+            v -= (float)part[0].v[i];
+            part[1].v[i] = (TC)v;
+            part[2].v[i] = (TC)(v - (float)part[1].v[i]);
+        }
+#pragma unroll
+        for (int n = 0; n < 3; ++n) lds.q[n][c][lane] = part[n];
+    }
+    __syncthreads();
+}
 
 // A wave's part of a segment, every fourth tile of it, its results left in LDS.
 template <typename TC, bool Q16, int DC, Rows R>
-__device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &seg, AttnLds<AttnKernel<TC, Q16, DC, R>::DO> &lds)
+__device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &seg, AttnLds<AttnKernel<TC, Q16, DC, R>, TC> &lds)
 {
     using Cfg = AttnKernel<TC, Q16, DC, R>;
     using Tile = typename Cfg::Tile;
@@ -353,47 +409,23 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
     // the last one's, and give nothing.)
     Pack<std::conditional_t<QP == 3, TC, TQ>, KV> q[QP][NK];
     float unscale = 1.f;  // f16 parts of 32-bit queries are those of the queries over this
-    {
+    if constexpr (QP == 3) {
+        unscale = lds.unscale[n16];
+#pragma unroll
+        for (int n = 0; n < 3; ++n)
+#pragma unroll
+            for (int c = 0; c < NK; ++c) q[n][c] = lds.q[n][c][lane];
+    } else {
         const TQ *row = (const TQ *)a.q + (int64_t)seq * a.q_row + ((int64_t)seg.kvh * a.group + min(in_group, a.group - 1)) * a.q_head;
-        Pack<TQ, KV> whole[NK];
         if (a.q_pieces) {
 #pragma unroll
-            for (int c = 0; c < NK; ++c) whole[c] = load_row<TQ, KV, R == kAny ? kPieces : R>(row, (g + 4 * c) * KV, a.dim);
+            for (int c = 0; c < NK; ++c) q[0][c] = load_row<TQ, KV, R == kAny ? kPieces : R>(row, (g + 4 * c) * KV, a.dim);
         } else {
 #pragma unroll
-            for (int c = 0; c < NK; ++c) whole[c] = load_row<TQ, KV, kAny>(row, (g + 4 * c) * KV, a.dim);
+            for (int c = 0; c < NK; ++c) q[0][c] = load_row<TQ, KV, kAny>(row, (g + 4 * c) * KV, a.dim);
         }
 #pragma unroll
-        for (int c = 0; c < NK; ++c) whole[c] = cleared<TQ, KV, R>(whole[c], (g + 4 * c) * KV, a.dim);
-        if constexpr (QP == 3) {
-            float f = 1.f;
-            if constexpr (__is_same(TC, _Float16)) {
-                // The largest becomes 2^14 to 2^15: parts keep what is above 2^-39 of it.
-                float most = 0.f;
-#pragma unroll
-                for (int c = 0; c < NK; ++c)
-#pragma unroll
-                    for (int i = 0; i < KV; ++i) most = fmaxf(most, fabsf(whole[c].v[i]));
-                most = max_of_head(most);
-                const int e = (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127;  // 2^e <= most < 2^(e+1)
-                const int by = most > 0.f && e < 128 ? min(14 - e, 126) : 0;
-                f = __builtin_ldexpf(1.f, by);
-                unscale = __builtin_ldexpf(1.f, -by);
-            }
-#pragma unroll
-            for (int c = 0; c < NK; ++c)
-#pragma unroll
-                for (int i = 0; i < KV; ++i) {
-                    float v = whole[c].v[i] * f;
-                    q[0][c].v[i] = (TC)v;
-                    v -= (float)q[0][c].v[i];
-                    q[1][c].v[i] = (TC)v;
-                    q[2][c].v[i] = (TC)(v - (float)q[1][c].v[i]);
-                }
-        } else {
-#pragma unroll
-            for (int c = 0; c < NK; ++c) q[0][c] = whole[c];
-        }
+        for (int c = 0; c < NK; ++c) q[0][c] = cleared<TQ, KV, R>(q[0][c], (g + 4 * c) * KV, a.dim);
     }
 
     floatx4 o[NO], ol[C16 ? NO : 1];  // (ol: of the probabilities' small parts)
@@ -548,14 +580,14 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
 {
     using Cfg = AttnKernel<TC, Q16, DC, R>;
     using TQ = std::conditional_t<Q16, TC, float>;
-    __shared__ AttnLds<Cfg::DO> lds;
+    __shared__ AttnLds<Cfg, TC> lds;
 
     const int units = units_of(a), wg = blockIdx.x;
     Share share = {0, 0, true};
     if (a.split) share = find_share(a, wg, lds.found);
 
-    // This workgroup's place in its share.
-    int seq, unit, tile0 = 0, tiles_all;
+    // This workgroup's place: a unit, its tiles, and how far into its length the share has come.
+    int seq, unit, tiles_all, x0 = 0;
     int at = 0, last = 0;
     if (a.split && threadIdx.x == 0) a.parts[wg] = AttnPart{-1, 0, 0, 0};  // (whatever follows, attn_join reads it)
     if (share.whole) {
@@ -564,18 +596,20 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
         unit = wg - seq * units;
         tiles_all = tiles_of(a, uniform(a.lengths[seq]));
     } else {
-        if ((int64_t)wg * share.tiles >= share.total) return;
-        at = wg * share.tiles;
-        last = (int)min((int64_t)at + share.tiles, (int64_t)share.total);
+        if ((int64_t)wg * share.size >= share.total) return;
+        at = wg * share.size;
+        last = (int)min((int64_t)at + share.size, (int64_t)share.total);
         seq = uniform(lds.found.seq);
         tiles_all = uniform(lds.found.tiles);
         const int in = at - uniform(lds.found.before);
-        unit = in / tiles_all;
-        tile0 = in - unit * tiles_all;
+        unit = in / (tiles_all + kUnitCost);
+        x0 = in - unit * (tiles_all + kUnitCost);
     }
 
     for (;;) {
-        const int seg_tiles = share.whole ? tiles_all : min(tiles_all - tile0, last - at);
+        const int x1 = share.whole ? tiles_all + kUnitCost : min(tiles_all + kUnitCost, x0 + (last - at));
+        const int tile0 = max(0, x0 - kUnitCost), seg_tiles = max(0, x1 - kUnitCost) - tile0;
+        if (seg_tiles == 0) return;  // the share ends before the unit's first tile
         Segment seg;
         seg.seq = seq;
         seg.kvh = unit / a.blocks;
@@ -584,6 +618,7 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
         visible_range(a, uniform(a.lengths[seq]), &first, &end);
         seg.k0 = first + tile0 * 16;
         seg.k1 = (int)min((int64_t)end, (int64_t)seg.k0 + (int64_t)seg_tiles * 16);
+        if constexpr (Cfg::QP == 3) split_queries<TC, DC, R>(a, seg, lds);
         attn_segment<TC, Q16, DC, R>(a, seg, lds);
         __syncthreads();
 
@@ -633,12 +668,12 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
         // Who begins a unit that others go on with says so.
         if (threadIdx.x == 0 && !all && tile0 == 0) {
             const int rest = tiles_all - seg_tiles;
-            a.parts[wg] = AttnPart{seq, unit, 1 + (int)(((unsigned)rest + share.tiles - 1) / (unsigned)share.tiles), 0};
+            a.parts[wg] = AttnPart{seq, unit, 1 + (int)(((unsigned)rest + share.size - 1) / (unsigned)share.size), 0};
         }
-        at += seg_tiles;
+        at += x1 - x0;
         if (at >= last) return;
         __syncthreads();  // as above
-        tile0 = 0;
+        x0 = 0;
         if (++unit == units) {
             unit = 0;
             tiles_all = tiles_of(a, uniform(a.lengths[++seq]));

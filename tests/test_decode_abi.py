@@ -135,11 +135,14 @@ def size(q_heads=32, window=0, max_len=0, **kw):
 
 def test_workspace_sizes():
     assert size(wide=1) == size(window=16) == size(max_len=16) == size(pages=0) == size(seqs=0) == 0
-    assert size(seqs=100000, q_heads=8) == 0            # enough rows without a split
+    # At most 1024 workgroups, each with 16 bytes of its own and two parts of up to 16 heads.
+    most = 1024 * (16 + 2 * 16 * 130 * 4)
     long = size(seqs=1, wide=1 << 16)
-    assert 0 < long <= 32 * 256 * 130 * 4
-    assert size(seqs=1, wide=1 << 16, max_len=2048) < long
-    assert size(seqs=1, wide=1 << 30) <= 32 * 256 * 130 * 4   # more keys than an int counts
+    assert 0 < long <= most
+    assert 0 < size(seqs=1, wide=1 << 16, max_len=2048) < long
+    assert size(seqs=100000, q_heads=8) <= most
+    assert size(seqs=1, wide=1 << 30) <= most     # more keys than an int counts
+    assert size(seqs=1 << 19, q_heads=8, wide=1 << 30) == 0   # more tiles than an int counts: no split
     n = ctypes.c_size_t()
     f = ilpm.lib.ilpm_attn_decode_workspace_size
     for args, want in (((None, 32, 0, 0), ilpm.ERR_INVALID_ARG), ((cache(), 30, 0, 0), ilpm.ERR_INVALID_ARG),
