@@ -19,6 +19,32 @@ inline int element_bytes(int dtype) { return dtype == ILPM_F32 ? 4 : 2; }
 // access up to 16 bytes, several of 16 beyond.
 template <typename T, int N> struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack { T v[N]; };
 
+// A pack in memory, moved as whole words of the machine (taken by its elements
+// the compiler may break a store into pieces: 16-bit values that only pass
+// through were stored in four).
+template <int BYTES> struct PackWord { typedef unsigned type __attribute__((ext_vector_type(4))); };
+template <> struct PackWord<8> { typedef unsigned type __attribute__((ext_vector_type(2))); };
+template <> struct PackWord<4> { typedef unsigned type; };
+template <> struct PackWord<2> { typedef unsigned short type; };
+
+template <typename T, int N> __device__ inline Pack<T, N> load_pack(const T *p)
+{
+    using W = typename PackWord<(int)sizeof(Pack<T, N>)>::type;
+    struct Words { W w[sizeof(Pack<T, N>) / sizeof(W)]; } words;
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(words) / sizeof(W); ++i) words.w[i] = reinterpret_cast<const W *>(p)[i];
+    return __builtin_bit_cast(Pack<T, N>, words);
+}
+
+template <typename T, int N> __device__ inline void store_pack(T *p, const Pack<T, N> &v)
+{
+    using W = typename PackWord<(int)sizeof(Pack<T, N>)>::type;
+    struct Words { W w[sizeof(Pack<T, N>) / sizeof(W)]; };
+    const Words words = __builtin_bit_cast(Words, v);
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(words) / sizeof(W); ++i) reinterpret_cast<W *>(p)[i] = words.w[i];
+}
+
 // ---- kv_append ----
 struct AppendArgs {
     // rows of heads: [token][head][dim], strides in elements

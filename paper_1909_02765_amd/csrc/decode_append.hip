@@ -80,123 +80,98 @@ template <typename TX, typename TC> __global__ __launch_bounds__(256) void appen
 }
 
 // Rows that divide into packs of VEC elements (of pairs: both halves do): a
-// thread takes one pack, or one of each half, of up to HPT heads of a token, so
-// it reads the angles once for all of them.  What bounds it: the bytes of
-// queries, keys and values, read and written once.
-template <typename TX, typename TC, int VEC, int HPT> __global__ __launch_bounds__(256) void append_packs(AppendArgs a)
+// thread takes one pack of a token's head, or one of each half.  What bounds
+// it: the bytes of queries, keys and values, read and written once.  (Threads
+// that took several heads, to read the angles once for them, were slower: 16381
+// tokens of 40 + 8 heads of 128 in bf16 90 us with one head a thread, 5.3 TB/s,
+// 92 with two, 108 with four.)
+template <typename TX, typename TC, int VEC> __global__ __launch_bounds__(256) void append_packs(AppendArgs a)
 {
     const int half = a.rot_dim / 2;
     // Packs of a rotated head (the first `turned` of them with their partners, or
     // in pairs of neighbours), and of a value head.
     const int turned = (a.pairs ? a.rot_dim : half) / VEC, units = a.dim / VEC - (a.pairs ? 0 : half / VEC);
-    const int vunits = a.dim / VEC;
-    const int heads = a.q_heads + a.kv_heads, slots = (heads + HPT - 1) / HPT, vslots = (a.kv_heads + HPT - 1) / HPT;
-    const unsigned per = slots * units + vslots * vunits;
+    const int vunits = a.dim / VEC, rotated_heads = a.q_heads + a.kv_heads;
+    const unsigned per = rotated_heads * units + a.kv_heads * vunits;
     const unsigned id = blockIdx.x * 256u + threadIdx.x;  // (at most 2^24 workgroups)
     const int t = (int)(id / per);
     if (t >= a.n_tokens) return;
-    int i = (int)(id - t * per);
+    const int i = (int)(id - t * per);
     const int pos = a.positions[t];
+    const bool known = a.rot_dim > 0 && pos >= 0 && pos < a.n_positions;
 
-    if (i >= slots * units) {  // a value's packs
-        i -= slots * units;
-        const int slot = i / vunits, e = (i - slot * vunits) * VEC;
-        const TX *v = (const TX *)a.v + (int64_t)t * a.v_row + e;
-        Pack<TX, VEC> p[HPT];
+    if (i >= rotated_heads * units) {  // of a value
+        const int j = i - rotated_heads * units, h = j / vunits, e = (j - h * vunits) * VEC;
+        const Pack<TX, VEC> p = load_pack<TX, VEC>((const TX *)a.v + (int64_t)t * a.v_row + h * a.v_head + e);
+        const Place at = place_of(a, t, pos);
+        if (at.page < 0 || (a.rot_dim > 0 && !known)) return;
+        Pack<TC, VEC> o;
 #pragma unroll
-        for (int n = 0; n < HPT; ++n) {
-            const int h = slot + n * vslots;
-            if (h < a.kv_heads) p[n] = *reinterpret_cast<const Pack<TX, VEC> *>(v + h * a.v_head);
-        }
-        Place at = place_of(a, t, pos);
-        if (at.page < 0 || (a.rot_dim > 0 && pos >= a.n_positions)) return;
-        TC *vc = (TC *)a.vc + (int64_t)at.page * a.vc_page + (int64_t)at.slot * a.vc_slot + e;
-#pragma unroll
-        for (int n = 0; n < HPT; ++n) {
-            const int h = slot + n * vslots;
-            Pack<TC, VEC> o;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) o.v[j] = (TC)(float)p[n].v[j];
-            if (h < a.kv_heads) *reinterpret_cast<Pack<TC, VEC> *>(vc + h * a.vc_head) = o;
-        }
+        for (int j = 0; j < VEC; ++j) o.v[j] = (TC)(float)p.v[j];
+        store_pack<TC, VEC>((TC *)a.vc + (int64_t)at.page * a.vc_page + (int64_t)at.slot * a.vc_slot + h * a.vc_head + e, o);
         return;
     }
 
-    const int slot = i / units, u = i - slot * units;
-    const bool rotated = u < turned;
+    const int h = i / units, u = i - h * units;
+    const bool rotated = u < turned, two = rotated && !a.pairs, turn = rotated && known, query = h < a.q_heads;
     // Elements e.. and, of halves, their partners from e2.
     const int e = a.pairs || rotated ? u * VEC : half + u * VEC, e2 = e + half;
-    const bool two = rotated && !a.pairs;
-    Pack<TX, VEC> p[HPT], p2[HPT];
-    const TX *q = (const TX *)a.q + (int64_t)t * a.q_row, *k = (const TX *)a.k + (int64_t)t * a.k_row;
-#pragma unroll
-    for (int n = 0; n < HPT; ++n) {
-        const int h = slot + n * slots;
-        if (h >= heads) continue;
-        const TX *src = h < a.q_heads ? q + h * a.q_head : k + (h - a.q_heads) * a.k_head;
-        p[n] = *reinterpret_cast<const Pack<TX, VEC> *>(src + e);
-        if (two) p2[n] = *reinterpret_cast<const Pack<TX, VEC> *>(src + e2);
-    }
-    const bool known = a.rot_dim > 0 && pos >= 0 && pos < a.n_positions, turn = rotated && known;
+    const TX *src = query ? (const TX *)a.q + (int64_t)t * a.q_row + h * a.q_head
+                          : (const TX *)a.k + (int64_t)t * a.k_row + (h - a.q_heads) * a.k_head;
+    const Pack<TX, VEC> p = load_pack<TX, VEC>(src + e);
+    Pack<TX, VEC> p2 = {};
+    if (two) p2 = load_pack<TX, VEC>(src + e2);
     // VEC angles for halves, VEC / 2 for pairs.
+    constexpr int HV = VEC / 2;
     float c[VEC], s[VEC];
     if (turn) {
-        const int first = a.pairs ? e / 2 : e;
-        const float *cos = a.cos + (int64_t)pos * half + first, *sin = a.sin + (int64_t)pos * half + first;
-        constexpr int HV = VEC > 1 ? VEC / 2 : 1;
-        const Pack<float, HV> c0 = *reinterpret_cast<const Pack<float, HV> *>(cos);
-        const Pack<float, HV> s0 = *reinterpret_cast<const Pack<float, HV> *>(sin);
+        const int64_t first = (int64_t)pos * half + (a.pairs ? e / 2 : e);
 #pragma unroll
-        for (int j = 0; j < HV; ++j) c[j] = c0.v[j], s[j] = s0.v[j];
-        if (two) {
-            const Pack<float, HV> c1 = *reinterpret_cast<const Pack<float, HV> *>(cos + HV);
-            const Pack<float, HV> s1 = *reinterpret_cast<const Pack<float, HV> *>(sin + HV);
+        for (int n = 0; n < 2; ++n) {
+            if (n == 1 && !two) break;
+            const Pack<float, HV> cp = load_pack<float, HV>(a.cos + first + n * HV);
+            const Pack<float, HV> sp = load_pack<float, HV>(a.sin + first + n * HV);
 #pragma unroll
-            for (int j = 0; j < HV; ++j) c[HV + j] = c1.v[j], s[HV + j] = s1.v[j];
+            for (int j = 0; j < HV; ++j) c[n * HV + j] = cp.v[j], s[n * HV + j] = sp.v[j];
         }
     }
     // (The queries of a token are turned wherever its keys go.)
     Place at = {-1, 0};
-    if (slot + (HPT - 1) * slots >= a.q_heads) at = place_of(a, t, pos);
-    if (a.rot_dim > 0 && !known) at.page = -1;
-    TC *kc = (TC *)a.kc + (int64_t)max(at.page, 0) * a.kc_page + (int64_t)at.slot * a.kc_slot;
-    TX *qo = (TX *)a.q_out + (int64_t)t * a.qo_row;
-#pragma unroll
-    for (int n = 0; n < HPT; ++n) {
-        const int h = slot + n * slots;
-        if (h >= heads) continue;
-        float x[VEC], y[VEC];
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = (float)p[n].v[j], y[j] = two ? (float)p2[n].v[j] : 0.f;
-        if (turn && two) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float v = x[j];
-                x[j] = v * c[j] - y[j] * s[j];
-                y[j] = y[j] * c[j] + v * s[j];
-            }
-        } else if (turn) {
-#pragma unroll
-            for (int j = 0; j + 1 < VEC; j += 2) {
-                const float v = x[j], w = x[j + 1];
-                x[j] = v * c[j / 2] - w * s[j / 2];
-                x[j + 1] = w * c[j / 2] + v * s[j / 2];
-            }
-        }
-        auto put = [&](auto *dst) {
-            using TD = std::remove_reference_t<decltype(*dst)>;
-            Pack<TD, VEC> o;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) o.v[j] = (TD)x[j];
-            *reinterpret_cast<Pack<TD, VEC> *>(dst + e) = o;
-            if (!two) return;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) o.v[j] = (TD)y[j];
-            *reinterpret_cast<Pack<TD, VEC> *>(dst + e2) = o;
-        };
-        if (h < a.q_heads) put(qo + h * a.qo_head);
-        else if (at.page >= 0) put(kc + (h - a.q_heads) * a.kc_head);
+    if (!query) {
+        at = place_of(a, t, pos);
+        if (at.page < 0 || (a.rot_dim > 0 && !known)) return;
     }
+    float x[VEC], y[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) x[j] = (float)p.v[j], y[j] = (float)p2.v[j];
+    if (turn && two) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float v = x[j];
+            x[j] = v * c[j] - y[j] * s[j];
+            y[j] = y[j] * c[j] + v * s[j];
+        }
+    } else if (turn) {
+#pragma unroll
+        for (int j = 0; j < VEC; j += 2) {
+            const float v = x[j], w = x[j + 1];
+            x[j] = v * c[j / 2] - w * s[j / 2];
+            x[j + 1] = w * c[j / 2] + v * s[j / 2];
+        }
+    }
+    auto put = [&](auto *dst) {
+        using TD = std::remove_reference_t<decltype(*dst)>;
+        Pack<TD, VEC> o;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o.v[j] = (TD)x[j];
+        store_pack<TD, VEC>(dst + e, o);
+        if (!two) return;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o.v[j] = (TD)y[j];
+        store_pack<TD, VEC>(dst + e2, o);
+    };
+    if (query) put((TX *)a.q_out + (int64_t)t * a.qo_row + h * a.qo_head);
+    else put((TC *)a.kc + (int64_t)at.page * a.kc_page + (int64_t)at.slot * a.kc_slot + (h - a.q_heads) * a.kc_head);
 }
 
 // Whether everything divides into packs of `vec` elements, aligned to 16
@@ -218,16 +193,11 @@ bool packs_fit(const AppendArgs &a, int vec, int sx, int sc)
 template <typename TX, typename TC, int VEC> bool launch_packs(const AppendArgs &a, hipStream_t stream)
 {
     if (!packs_fit(a, VEC, sizeof(TX), sizeof(TC))) return false;
-    const int half = a.rot_dim / 2, units = a.dim / VEC - (a.pairs ? 0 : half / VEC), vunits = a.dim / VEC;
-    auto groups = [&](int hpt) {
-        const int64_t per = (int64_t)ceil_div(a.q_heads + a.kv_heads, hpt) * units + (int64_t)ceil_div(a.kv_heads, hpt) * vunits;
-        return (per * a.n_tokens + 255) / 256;
-    };
-    // One head a thread until the card is full of threads, then four.
-    const bool four = groups(1) > 4096;
-    if (groups(four ? 4 : 1) > (1 << 24) - 1) return false;
-    if (four) hipLaunchKernelGGL((append_packs<TX, TC, VEC, 4>), dim3((unsigned)groups(4)), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((append_packs<TX, TC, VEC, 1>), dim3((unsigned)groups(1)), dim3(256), 0, stream, a);
+    const int units = a.dim / VEC - (a.pairs ? 0 : a.rot_dim / 2 / VEC);
+    const int64_t per = (int64_t)(a.q_heads + a.kv_heads) * units + (int64_t)a.kv_heads * (a.dim / VEC);
+    const int64_t groups = (per * a.n_tokens + 255) / 256;
+    if (groups > (1 << 24) - 1) return false;
+    hipLaunchKernelGGL((append_packs<TX, TC, VEC>), dim3((unsigned)groups), dim3(256), 0, stream, a);
     return true;
 }
 
