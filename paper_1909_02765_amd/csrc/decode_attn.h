@@ -163,7 +163,7 @@ template <typename TC, bool Q16, int DC, Rows R> struct AttnKernel {
     static constexpr int SHIFT = __is_same(TC, _Float16) ? 15 : 0;
     // Workgroups that a compute unit holds at once (waves of a SIMD): what the
     // registers of two tiles, the queries and the output leave.
-    static constexpr int PER_CU = DC == 64 ? (C16 && !Q16 ? 3 : 4) : DC <= 128 ? 2 : 1;
+    static constexpr int PER_CU = DC == 64 ? (QP == 3 ? 3 : 4) : DC <= 128 ? 2 : 1;
     // A tile of 16 keys: lane (n, g) holds pieces g, g + 4, ... of key n's K row,
     // and pieces n, n + 16, ... of the V rows of keys 4g..4g+3.
     struct Tile {
@@ -218,37 +218,63 @@ __device__ inline int scan256(int v, int *up_to, FindShare &f)
 // Units of a sequence (key heads x blocks of up to 16 of their query heads).
 __device__ inline int units_of(const AttnArgs &a) { return a.kv_heads * a.blocks; }
 
-// The shares of this call, and the sequence in which share `wg` begins (f.seq,
-// the tiles of its units f.tiles, and the length of all units before it, f.before).
-__device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f)
+// The shares of this call, and the sequence in which share `wg` begins, the
+// tiles of its units, and the length of all units before it (0 tiles where the
+// share is beyond the row's end).
+struct Begin {
+    int seq, tiles, before;
+};
+
+__device__ inline Share share_of(const AttnArgs &a, int total, int top)
 {
-    const int tid = threadIdx.x, units = units_of(a);
-    int mine = 0, top = 0, total, up_to;
-    if (a.n_seqs == 1) {
-        top = tiles_of(a, uniform(a.lengths[0]));
-        total = top + kUnitCost;
-        f.seq = f.before = 0;
-        f.tiles = top;
-    } else {
-        for (int i = tid; i < a.n_seqs; i += 256) {
-            const int t = tiles_of(a, a.lengths[i]);
-            mine += t + kUnitCost;
-            top = max(top, t);
-        }
-#pragma unroll 1
-        for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
-        if ((tid & 63) == 0) f.top[tid >> 6] = top;
-        total = scan256(mine, &up_to, f);
-        top = uniform(max(max(f.top[0], f.top[1]), max(f.top[2], f.top[3])));
-    }
     Share s;
-    s.total = total * units;
+    s.total = total * units_of(a);
     const int even = (int)(((unsigned)s.total + gridDim.x - 1) / gridDim.x);
     s.size = max(kMinShare + kUnitCost, even);
-    s.whole = s.size == kMinShare + kUnitCost && top <= 2 * kMinShare;
-    if (s.whole || a.n_seqs == 1) return s;
-    // The sequence that holds place wg * s.size, counted in one unit of each.
-    const int want = (int)min((int64_t)wg * s.size / units, (int64_t)INT_MAX);
+    s.whole = s.size == kMinShare + kUnitCost && top <= kWholeTiles;
+    return s;
+}
+
+__device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f, Begin *begin)
+{
+    const int tid = threadIdx.x, units = units_of(a);
+    *begin = Begin{0, 0, 0};
+    if (a.n_seqs <= 64) {  // each wave for itself
+        const int lane = tid & 63;
+        const int t = lane < a.n_seqs ? tiles_of(a, a.lengths[lane]) : 0, cost = t > 0 ? t + kUnitCost : 0;
+        int top = t, up_to = cost;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(up_to, d);
+            up_to += lane >= d ? o : 0;
+        }
+        const Share s = share_of(a, __builtin_amdgcn_readlane(up_to, 63), uniform(top));
+        const int64_t at = (int64_t)wg * s.size;
+        if (s.whole || at >= s.total) return s;
+        // The sequence that holds this place, counted in one unit of each.
+        const int want = (int)at / units;
+        const int seq = __builtin_ctzll(__builtin_amdgcn_ballot_w64(want < up_to));
+        begin->seq = seq;
+        begin->tiles = __builtin_amdgcn_readlane(t, seq);
+        begin->before = (__builtin_amdgcn_readlane(up_to, seq) - begin->tiles - kUnitCost) * units;
+        return s;
+    }
+    int mine = 0, top = 0, up_to;
+    for (int i = tid; i < a.n_seqs; i += 256) {
+        const int t = tiles_of(a, a.lengths[i]);
+        mine += t + kUnitCost;
+        top = max(top, t);
+    }
+#pragma unroll 1
+    for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) f.top[tid >> 6] = top;
+    const int total = scan256(mine, &up_to, f);
+    const Share s = share_of(a, total, uniform(max(max(f.top[0], f.top[1]), max(f.top[2], f.top[3]))));
+    const int64_t at = (int64_t)wg * s.size;
+    if (s.whole || at >= s.total) return s;
+    const int want = (int)at / units;
     int carry = 0;
     for (int i0 = 0; i0 < a.n_seqs && want >= carry; i0 += 256) {
         const int t = i0 + tid < a.n_seqs ? tiles_of(a, a.lengths[i0 + tid]) + kUnitCost : 0;
@@ -263,6 +289,7 @@ __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f)
         carry += sum;
     }
     __syncthreads();
+    *begin = Begin{uniform(f.seq), uniform(f.tiles), uniform(f.before)};
     return s;
 }
 
@@ -301,7 +328,7 @@ template <typename TC, int DC, Rows R, typename Lds> __device__ __forceinline__ 
     if constexpr (__is_same(TC, _Float16)) {
         // The largest becomes 2^14 to 2^15: parts keep what is above 2^-39 of it.
         float most = 0.f;
-#pragma unroll 1
+#pragma unroll 2
         for (int c = 0; c < NK; ++c) {
             const Pack<float, KV> p = get(c);
 #pragma unroll
@@ -314,9 +341,13 @@ template <typename TC, int DC, Rows R, typename Lds> __device__ __forceinline__ 
         back = __builtin_ldexpf(1.f, -by);
     }
     if (wave == 0 && g == 0) lds.unscale[n16] = back;
-#pragma unroll 1
-    for (int c = wave; c < NK; c += 4) {
-        const Pack<float, KV> p = get(c);
+    Pack<float, KV> mine[(NK + 3) / 4];
+#pragma unroll
+    for (int j = 0; j < (NK + 3) / 4; ++j) mine[j] = get(min(wave + 4 * j, NK - 1));
+#pragma unroll
+    for (int j = 0; j < (NK + 3) / 4; ++j) {
+        const int c = min(wave + 4 * j, NK - 1);  // (the last one several times over, with the same values)
+        const Pack<float, KV> p = mine[j];
         Pack<TC, KV> part[3];
 #pragma unroll
         for (int i = 0; i < KV; ++i) {
@@ -399,33 +430,30 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
             for (int c = 0; c < NV; ++c) t.v[r][c] = load_row<TC, VV, R>(vrow, (n16 + 16 * c) * VV, a.dim);
         }
     };
-    Entry next = {};
-    if (tiles > 0) {
-        place(0, look_up(0));
-        if (tiles > 4) next = look_up(1);
-    }
+    Entry e0 = {}, next = {};
+    if (tiles > 0) e0 = look_up(0);
+    if (tiles > 4) next = look_up(1);
+    if constexpr (QP == 3) split_queries<TC, DC, R>(a, seg, lds);
+    if (tiles > 0) place(0, e0);
 
     // The queries, in the layout of the K loads.  (Lanes without a head take
-    // the last one's, and give nothing.)
-    Pack<std::conditional_t<QP == 3, TC, TQ>, KV> q[QP][NK];
+    // the last one's, and give nothing.)  Those in parts stay in LDS: beside the tiles
+    // they would not fit the registers.
+    Pack<TQ, KV> q[QP == 3 ? 1 : NK];
     float unscale = 1.f;  // f16 parts of 32-bit queries are those of the queries over this
     if constexpr (QP == 3) {
         unscale = lds.unscale[n16];
-#pragma unroll
-        for (int n = 0; n < 3; ++n)
-#pragma unroll
-            for (int c = 0; c < NK; ++c) q[n][c] = lds.q[n][c][lane];
     } else {
         const TQ *row = (const TQ *)a.q + (int64_t)seq * a.q_row + ((int64_t)seg.kvh * a.group + min(in_group, a.group - 1)) * a.q_head;
         if (a.q_pieces) {
 #pragma unroll
-            for (int c = 0; c < NK; ++c) q[0][c] = load_row<TQ, KV, R == kAny ? kPieces : R>(row, (g + 4 * c) * KV, a.dim);
+            for (int c = 0; c < NK; ++c) q[c] = load_row<TQ, KV, R == kAny ? kPieces : R>(row, (g + 4 * c) * KV, a.dim);
         } else {
 #pragma unroll
-            for (int c = 0; c < NK; ++c) q[0][c] = load_row<TQ, KV, kAny>(row, (g + 4 * c) * KV, a.dim);
+            for (int c = 0; c < NK; ++c) q[c] = load_row<TQ, KV, kAny>(row, (g + 4 * c) * KV, a.dim);
         }
 #pragma unroll
-        for (int c = 0; c < NK; ++c) q[0][c] = cleared<TQ, KV, R>(q[0][c], (g + 4 * c) * KV, a.dim);
+        for (int c = 0; c < NK; ++c) q[c] = cleared<TQ, KV, R>(q[c], (g + 4 * c) * KV, a.dim);
     }
 
     floatx4 o[NO], ol[C16 ? NO : 1];  // (ol: of the probabilities' small parts)
@@ -441,17 +469,21 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
                 const Pack<TC, KV> k = cleared<TC, KV, R>(t.k[c], (g + 4 * c) * KV, a.dim);
 #pragma unroll
                 for (int i = 0; i < KV; ++i)
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32((float)k.v[i], (float)q[0][c].v[i], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32((float)k.v[i], (float)q[c].v[i], s, 0, 0, 0);
             }
         } else {
             floatx4 low = s;
+            int ql = lane;
+            if constexpr (QP == 3) asm volatile("" : "+v"(ql));  // (read for each tile, not kept)
 #pragma unroll
             for (int c = 0; c < NK; ++c) {
                 const Pack<TC, KV> k = cleared<TC, KV, R>(t.k[c], (g + 4 * c) * KV, a.dim);
-                s = mfma_scores(k, q[0][c], s);
                 if constexpr (QP == 3) {
-                    low = mfma_scores(k, q[1][c], low);
-                    low = mfma_scores(k, q[2][c], low);
+                    s = mfma_scores(k, lds.q[0][c][ql], s);
+                    low = mfma_scores(k, lds.q[1][c][ql], low);
+                    low = mfma_scores(k, lds.q[2][c][ql], low);
+                } else {
+                    s = mfma_scores(k, q[c], s);
                 }
             }
             if constexpr (QP == 3) {
@@ -584,7 +616,8 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
 
     const int units = units_of(a), wg = blockIdx.x;
     Share share = {0, 0, true};
-    if (a.split) share = find_share(a, wg, lds.found);
+    Begin begin;
+    if (a.split) share = find_share(a, wg, lds.found, &begin);
 
     // This workgroup's place: a unit, its tiles, and how far into its length the share has come.
     int seq, unit, tiles_all, x0 = 0;
@@ -599,9 +632,9 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
         if ((int64_t)wg * share.size >= share.total) return;
         at = wg * share.size;
         last = (int)min((int64_t)at + share.size, (int64_t)share.total);
-        seq = uniform(lds.found.seq);
-        tiles_all = uniform(lds.found.tiles);
-        const int in = at - uniform(lds.found.before);
+        seq = begin.seq;
+        tiles_all = begin.tiles;
+        const int in = at - begin.before;
         unit = in / (tiles_all + kUnitCost);
         x0 = in - unit * (tiles_all + kUnitCost);
     }
@@ -618,7 +651,6 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
         visible_range(a, uniform(a.lengths[seq]), &first, &end);
         seg.k0 = first + tile0 * 16;
         seg.k1 = (int)min((int64_t)end, (int64_t)seg.k0 + (int64_t)seg_tiles * 16);
-        if constexpr (Cfg::QP == 3) split_queries<TC, DC, R>(a, seg, lds);
         attn_segment<TC, Q16, DC, R>(a, seg, lds);
         __syncthreads();
 
@@ -641,8 +673,9 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             TQ *out = (TQ *)a.out + (int64_t)seq * a.o_row + (int64_t)(head0 + h) * a.o_head;
             float *po = a.part_o + (part + h) * a.dim;
-#pragma unroll 1
-            for (int d = lane; d < a.dim; d += 64) {
+#pragma unroll
+            for (int d = lane; d < (DC + 63) / 64 * 64; d += 64) {
+                if (d >= a.dim) continue;
                 const float v = (lds.o[0][h][d] * f[0] + lds.o[1][h][d] * f[1]) + (lds.o[2][h][d] * f[2] + lds.o[3][h][d] * f[3]);
                 if (all) out[d] = (TQ)(v * inv);
                 else po[d] = v;

@@ -88,7 +88,7 @@ template <int V, int T> __global__ __launch_bounds__(256) void attn_join(AttnArg
 
 }  // namespace
 
-// Sequences that cannot have more keys than two smallest shares go a unit to a
+// Sequences that cannot have more than kWholeTiles tiles go a unit to a
 // workgroup; else as many workgroups share all tiles as the card holds, or as
 // there are smallest shares.
 size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
@@ -98,7 +98,7 @@ size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
     const int64_t keys = a->window > 0 ? std::min(max_len, a->window) : max_len, tiles = std::max<int64_t>(1, (keys + 15) / 16);
     // (Tiles are counted in 32 bits.  Where a table could name more, there are units enough without a split.)
     const int64_t most = (((int64_t)a->capacity + 15) / 16 + kUnitCost) * units;
-    a->split = tiles > 2 * kMinShare && units > 0 && (most < INT_MAX || units == 1);
+    a->split = tiles > kWholeTiles && units > 0 && (most < INT_MAX || units == 1);
     if (!a->split) {
         a->grid = (int)units;
         return 0;
