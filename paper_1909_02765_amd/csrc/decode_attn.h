@@ -116,10 +116,18 @@ template <typename T, int N, Rows R> __device__ inline Pack<T, N> load_row(const
     return p;
 }
 
-// p with what lies beyond `dim` cleared.
+// p with what lies beyond `dim` cleared (of pieces all or nothing).
 template <typename T, int N, Rows R> __device__ inline Pack<T, N> cleared(Pack<T, N> p, int d, int dim)
 {
-    if constexpr (R != kWhole) {
+    if constexpr (R == kPieces) {
+        struct Words {
+            unsigned w[sizeof(p) / 4];
+        } words = __builtin_bit_cast(Words, p);
+        const unsigned keep = d < dim ? 0xffffffffu : 0u;
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(p) / 4; ++i) words.w[i] &= keep;
+        p = __builtin_bit_cast(Pack<T, N>, words);
+    } else if constexpr (R == kAny) {
 #pragma unroll
         for (int i = 0; i < N; ++i) p.v[i] = d + i < dim ? p.v[i] : (T)0.f;
     }
@@ -230,8 +238,8 @@ __device__ inline Share share_of(const AttnArgs &a, int total, int top)
     Share s;
     s.total = total * units_of(a);
     const int even = (int)(((unsigned)s.total + gridDim.x - 1) / gridDim.x);
-    s.size = max(kMinShare + kUnitCost, even);
-    s.whole = s.size == kMinShare + kUnitCost && top <= kWholeTiles;
+    s.size = max(kMinShare, even);
+    s.whole = s.size == kMinShare && top <= kWholeTiles;
     return s;
 }
 
@@ -322,7 +330,7 @@ template <typename TC, int DC, Rows R, typename Lds> __device__ __forceinline__ 
     auto get = [&](int c) {
         const int d = (g + 4 * c) * KV;
         const Pack<float, KV> p = a.q_pieces ? load_row<float, KV, kPieces>(row, d, a.dim) : load_row<float, KV, kAny>(row, d, a.dim);
-        return cleared<float, KV, kPieces>(p, d, a.dim);
+        return cleared<float, KV, R>(p, d, a.dim);
     };
     float f = 1.f, back = 1.f;
     if constexpr (__is_same(TC, _Float16)) {
@@ -614,7 +622,11 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
     using TQ = std::conditional_t<Q16, TC, float>;
     __shared__ AttnLds<Cfg, TC> lds;
 
-    const int units = units_of(a), wg = blockIdx.x;
+    // Workgroups go round the card's eight dies, each with a cache of its own.
+    // Neighbouring shares, which often hold neighbouring heads of the same
+    // tokens, stay on one die, so that a line of two heads' rows is fetched once.
+    const int die = blockIdx.x & 7, dies = gridDim.x >> 3;
+    const int units = units_of(a), wg = die * dies + min(die, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
     Share share = {0, 0, true};
     Begin begin;
     if (a.split) share = find_share(a, wg, lds.found, &begin);

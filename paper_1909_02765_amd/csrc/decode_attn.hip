@@ -106,7 +106,7 @@ size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
     const int card = cache_dtype == ILPM_F32   ? attn_card_f32(a->dim)
                      : cache_dtype == ILPM_F16 ? (q32 ? attn_card_f16_q32(a->dim) : attn_card_f16(a->dim))
                                                : (q32 ? attn_card_bf16_q32(a->dim) : attn_card_bf16(a->dim));
-    a->grid = (int)std::min<int64_t>({card, kMaxParts, units * ((tiles + kMinShare - 1) / kMinShare)});
+    a->grid = (int)std::min<int64_t>({card, kMaxParts, units * ((tiles + kUnitCost + kMinShare - 1) / kMinShare)});
     a->part_heads = std::min(a->group, kAttnHeads);
     return (size_t)a->grid * (sizeof(AttnPart) + 2 * a->part_heads * (size_t)(a->dim + 2) * sizeof(float));
 }
