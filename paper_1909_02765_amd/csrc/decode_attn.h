@@ -34,6 +34,7 @@
 #pragma once
 
 #include <climits>
+#include <type_traits>
 
 #include "decode.h"
 
@@ -155,8 +156,11 @@ __device__ inline floatx4 mfma_values(uint2 v, const Pack<_Float16, 4> &p, float
 }
 
 // TC: the cache's type.  Q16: queries and outputs are of that same 16-bit type
-// (else f32).  DC: the head size's class (64, 96, 128, 192 or 256).
-template <typename TC, bool Q16, int DC, Rows R> struct AttnKernel {
+// (else f32).  DC: the head size's class (64, 96, 128, 192 or 256).  SHORT: for
+// calls whose sequences are all short, a unit to a workgroup: one tile at a
+// time, in half the registers and instructions (an instruction that runs once
+// costs its fetching, and more workgroups fit a compute unit).
+template <typename TC, bool Q16, int DC, Rows R, bool SHORT> struct AttnKernel {
     static constexpr bool C16 = sizeof(TC) == 2;
     static constexpr int KV = 16 / (int)sizeof(TC);          // elements of a K load
     static constexpr int NK = DC / (4 * KV);                 // K loads of a lane
@@ -171,7 +175,7 @@ template <typename TC, bool Q16, int DC, Rows R> struct AttnKernel {
     static constexpr int SHIFT = __is_same(TC, _Float16) ? 15 : 0;
     // Workgroups that a compute unit holds at once (waves of a SIMD): what the
     // registers of two tiles, the queries and the output leave.
-    static constexpr int PER_CU = DC == 64 ? (QP == 3 ? 3 : 4) : DC <= 128 ? 2 : 1;
+    static constexpr int PER_CU = SHORT ? (DC == 64 ? 5 : DC <= 128 ? 3 : 2) : DC == 64 ? (QP == 3 ? 3 : 4) : DC <= 128 ? 2 : 1;
     // A tile of 16 keys: lane (n, g) holds pieces g, g + 4, ... of key n's K row,
     // and pieces n, n + 16, ... of the V rows of keys 4g..4g+3.
     struct Tile {
@@ -320,9 +324,10 @@ template <typename Cfg, typename TC> struct AttnLds {
 
 // The workgroup splits a unit's 32-bit queries into their parts (once for its
 // four waves, and in a loop: instructions that run once cost their fetching).
-template <typename TC, int DC, Rows R, typename Lds> __device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &seg, Lds &lds)
+template <typename TC, int DC, Rows R, typename Lds>
+__device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &seg, Lds &lds)
 {
-    using Cfg = AttnKernel<TC, false, DC, R>;
+    using Cfg = AttnKernel<TC, false, DC, R, false>;
     constexpr int KV = Cfg::KV, NK = Cfg::NK;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), n16 = lane & 15, g = lane >> 4;
     const int in_group = min(seg.hb * kAttnHeads + n16, a.group - 1);
@@ -372,10 +377,10 @@ template <typename TC, int DC, Rows R, typename Lds> __device__ __forceinline__ 
 }
 
 // A wave's part of a segment, every fourth tile of it, its results left in LDS.
-template <typename TC, bool Q16, int DC, Rows R>
-__device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &seg, AttnLds<AttnKernel<TC, Q16, DC, R>, TC> &lds)
+template <typename TC, bool Q16, int DC, Rows R, bool SHORT>
+__device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &seg, AttnLds<AttnKernel<TC, Q16, DC, R, SHORT>, TC> &lds)
 {
-    using Cfg = AttnKernel<TC, Q16, DC, R>;
+    using Cfg = AttnKernel<TC, Q16, DC, R, SHORT>;
     using Tile = typename Cfg::Tile;
     using TQ = std::conditional_t<Q16, TC, float>;
     constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
@@ -440,7 +445,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
     };
     Entry e0 = {}, next = {};
     if (tiles > 0) e0 = look_up(0);
-    if (tiles > 4) next = look_up(1);
+    if (!SHORT && tiles > 4) next = look_up(1);
     if constexpr (QP == 3) split_queries<TC, DC, R>(a, seg, lds);
     if (tiles > 0) place(0, e0);
 
@@ -577,17 +582,26 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
         o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
         if constexpr (C16) ol[i] = o[i];
     }
-    Tile buf[2];
-    if (tiles > 0) load(0, buf[0]);
-    for (int j = 0; j < tiles; j += 2) {
-        if ((j & 3) == 2 && j + 2 < tiles) {
-            place(j / 4 + 1, next);
-            if (j + 6 < tiles) next = look_up(j / 4 + 2);
+    Tile buf[SHORT ? 1 : 2];
+    if constexpr (SHORT) {
+#pragma unroll 1
+        for (int j = 0; j < tiles; ++j) {
+            if (j > 0 && (j & 3) == 0) place(j / 4, look_up(j / 4));
+            load(j, buf[0]);
+            compute(buf[0]);
         }
-        if (j + 1 < tiles) load(j + 1, buf[1]);
-        compute(buf[0]);
-        if (j + 2 < tiles) load(j + 2, buf[0]);
-        if (j + 1 < tiles) compute(buf[1]);
+    } else {
+        if (tiles > 0) load(0, buf[0]);
+        for (int j = 0; j < tiles; j += 2) {
+            if ((j & 3) == 2 && j + 2 < tiles) {
+                place(j / 4 + 1, next);
+                if (j + 6 < tiles) next = look_up(j / 4 + 2);
+            }
+            if (j + 1 < tiles) load(j + 1, buf[1]);
+            compute(buf[0]);
+            if (j + 2 < tiles) load(j + 2, buf[0]);
+            if (j + 1 < tiles) compute(buf[1]);
+        }
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -615,10 +629,10 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
     }
 }
 
-template <typename TC, bool Q16, int DC, Rows R>
-__global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void attn_split(AttnArgs a)
+template <typename TC, bool Q16, int DC, Rows R, bool SHORT>
+__global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) void attn_split(AttnArgs a)
 {
-    using Cfg = AttnKernel<TC, Q16, DC, R>;
+    using Cfg = AttnKernel<TC, Q16, DC, R, SHORT>;
     using TQ = std::conditional_t<Q16, TC, float>;
     __shared__ AttnLds<Cfg, TC> lds;
 
@@ -629,7 +643,8 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
     const int units = units_of(a), wg = die * dies + min(die, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
     Share share = {0, 0, true};
     Begin begin;
-    if (a.split) share = find_share(a, wg, lds.found, &begin);
+    if constexpr (!SHORT)
+        if (a.split) share = find_share(a, wg, lds.found, &begin);
 
     // This workgroup's place: a unit, its tiles, and how far into its length the share has come.
     int seq, unit, tiles_all, x0 = 0;
@@ -663,7 +678,7 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R>::PER_CU)) void att
         visible_range(a, uniform(a.lengths[seq]), &first, &end);
         seg.k0 = first + tile0 * 16;
         seg.k1 = (int)min((int64_t)end, (int64_t)seg.k0 + (int64_t)seg_tiles * 16);
-        attn_segment<TC, Q16, DC, R>(a, seg, lds);
+        attn_segment<TC, Q16, DC, R, SHORT>(a, seg, lds);
         __syncthreads();
 
         // Join the four waves; each writes a head at a time.
@@ -734,9 +749,14 @@ template <typename TC, bool Q16, int DC> hipError_t attn_split_launch(const Attn
     AttnArgs args = a;
     const int64_t qs = Q16 ? sizeof(TC) : 4, qstep = 16 / qs;
     args.q_pieces = a.dim % step == 0 && (uintptr_t)a.q % 16 == 0 && (a.q_row | a.q_head) % qstep == 0;
-    if (pieces && a.dim == DC) hipLaunchKernelGGL((attn_split<TC, Q16, DC, kWhole>), dim3(a.grid), dim3(256), 0, stream, args);
-    else if (pieces) hipLaunchKernelGGL((attn_split<TC, Q16, DC, kPieces>), dim3(a.grid), dim3(256), 0, stream, args);
-    else hipLaunchKernelGGL((attn_split<TC, Q16, DC, kAny>), dim3(a.grid), dim3(256), 0, stream, args);
+    auto launch = [&](auto rows) {
+        constexpr Rows R = decltype(rows)::value;
+        if (a.split) hipLaunchKernelGGL((attn_split<TC, Q16, DC, R, false>), dim3(a.grid), dim3(256), 0, stream, args);
+        else hipLaunchKernelGGL((attn_split<TC, Q16, DC, R, true>), dim3(a.grid), dim3(256), 0, stream, args);
+    };
+    if (pieces && a.dim == DC) launch(std::integral_constant<Rows, kWhole>{});
+    else if (pieces) launch(std::integral_constant<Rows, kPieces>{});
+    else launch(std::integral_constant<Rows, kAny>{});
     return hipGetLastError();
 }
 
@@ -752,11 +772,11 @@ template <typename TC, bool Q16> hipError_t attn_split_by_dim(const AttnArgs &a,
 // Workgroups of the class of a head size that the card holds at once.
 template <typename TC, bool Q16> int attn_card_by_dim(int dim)
 {
-    return kAttnCus * (dim <= 64    ? AttnKernel<TC, Q16, 64, kWhole>::PER_CU
-                       : dim <= 96  ? AttnKernel<TC, Q16, 96, kWhole>::PER_CU
-                       : dim <= 128 ? AttnKernel<TC, Q16, 128, kWhole>::PER_CU
-                       : dim <= 192 ? AttnKernel<TC, Q16, 192, kWhole>::PER_CU
-                                    : AttnKernel<TC, Q16, 256, kWhole>::PER_CU);
+    return kAttnCus * (dim <= 64    ? AttnKernel<TC, Q16, 64, kWhole, false>::PER_CU
+                       : dim <= 96  ? AttnKernel<TC, Q16, 96, kWhole, false>::PER_CU
+                       : dim <= 128 ? AttnKernel<TC, Q16, 128, kWhole, false>::PER_CU
+                       : dim <= 192 ? AttnKernel<TC, Q16, 192, kWhole, false>::PER_CU
+                                    : AttnKernel<TC, Q16, 256, kWhole, false>::PER_CU);
 }
 
 }  // namespace
