@@ -17,7 +17,7 @@ __device__ inline float sum256(float v, float *lds)
 }
 
 // Any width, strides and alignment: a workgroup per row, which reads the row
-// again for each sum it needs.  Each element is written by the thread that
+// again for each sum it needs (very wide rows, and those of less than a pack).  Each element is written by the thread that
 // reads it, in the last pass, so r may be x and z may be y.
 template <typename TX, typename TY, typename TP> __global__ __launch_bounds__(256) void norm_any(NormArgs a)
 {
@@ -88,48 +88,62 @@ template <typename TX, typename TY, typename TP> __global__ __launch_bounds__(25
     });
 }
 
-// A sum over the 64 lanes of a wave, given to all of them: within rows of 16 by
-// lane permutations of the vector unit, then across the rows.
+// Lane permutations within rows of 16, in the vector unit.
 template <int CTRL> __device__ inline float plus_permuted(float v)
 {
     return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 
-__device__ inline float wave_sum(float v)
+// The sum over groups of LANES (16 or 64) lanes.
+template <int LANES> __device__ inline float lanes_sum(float v)
 {
     v = plus_permuted<0xB1>(v);   // lanes 1 0 3 2 of each four
     v = plus_permuted<0x4E>(v);   // lanes 2 3 0 1 of each four
     v = plus_permuted<0x141>(v);  // the other four of eight
     v = plus_permuted<0x140>(v);  // the other eight of sixteen
-    unsigned x = __builtin_bit_cast(unsigned, v);
-    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const unsigned p0 = p[0], p1 = p[1];
-    x = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1));
-    const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    const unsigned q0 = q[0], q1 = q[1];
-    return __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
+    if constexpr (LANES == 64) {
+        unsigned x = __builtin_bit_cast(unsigned, v);
+        const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        const unsigned p0 = p[0], p1 = p[1];
+        x = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1));
+        const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        const unsigned q0 = q[0], q1 = q[1];
+        v = __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
+    }
+    return v;
 }
 
+// N elements from an address that is aligned to one of them: the memory
+// system takes such accesses whole.
+template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+    static constexpr int WORDS = sizeof(T) * N / 16;
+    unsigned __attribute__((ext_vector_type(4))) w[WORDS];
+};
+
 // Rows of up to T * E values: T threads hold a row in registers, E values each,
-// in packs of VEC (16 bytes of y; VEC 1 for any width, stride and alignment),
-// so each input is read once and each output written once.  T = 64 leaves a
-// row to one wave (four rows a workgroup, no barrier).  Weights and biases
-// stay in registers over the rows that a workgroup takes.
+// in packs of VEC, so each input is read once and each output written once.  T
+// up to 64 leaves a row to part of a wave or a wave (no barrier).  Weights and
+// biases stay in registers over the rows that a workgroup takes.
+//
+// LOOSE: rows of any alignment and of any width from VEC on.  The last pack then
+// ends with the row, over some values of the pack before it: these count in no
+// sum, and only the pack that they belong to stores them (the row may be
+// overwritten in place).
 //
 // Mean and variance come from the values in registers, in two steps, so a mean
 // far from zero costs the variance nothing.  What bounds it: the bytes of x, y,
 // gate, r and z.
-template <typename TX, typename TY, typename TP, int T, int E, int VEC>
+template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOOSE>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
 {
-    constexpr int NV = E / VEC, ROWS = T < 256 ? 256 / T : 1, WAVES = T / 64;
+    constexpr int NV = E / VEC, ROWS = T < 256 ? 256 / T : 1, WAVES = T > 64 ? T / 64 : 1;
     constexpr bool HOLD = T * E <= 8192;  // (beyond, they do not fit beside the row: read again for each)
     __shared__ float lds[WAVES > 1 ? 2 * WAVES : 1];
     const int tid = threadIdx.x % T;
     const float inv_n = 1.f / (float)a.width;
     int turn = 0;
     auto total = [&](float v) {
-        v = wave_sum(v);
+        v = lanes_sum<(T < 64 ? T : 64)>(v);
         if constexpr (WAVES > 1) {
             // Two sets of places in turn: what is written now was read before the last barrier.
             float *part = lds + turn * WAVES;
@@ -142,13 +156,36 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
         }
         return v;
     };
+    // Pack i of this thread begins at `at`; its first `skip` values are another's.
+    auto at = [&](int i) { return (tid + i * T) * VEC; };
+    auto skip = [&](int i) { return LOOSE ? max(0, at(i) + VEC - a.width) : 0; };
     auto get = [&](const auto *row, int i) {
         using TD = std::remove_cv_t<std::remove_reference_t<decltype(*row)>>;
         Pack<TD, VEC> p = {};
-        const int at = (tid + i * T) * VEC;
-        if (row && at < a.width) p = *reinterpret_cast<const Pack<TD, VEC> *>(row + at);
+        if (row && at(i) < a.width) {
+            if constexpr (LOOSE) p = __builtin_bit_cast(Pack<TD, VEC>, *reinterpret_cast<const Loose<TD, VEC> *>(row + at(i) - skip(i)));
+            else p = load_pack<TD, VEC>(row + at(i));
+        }
         return p;
     };
+    auto put = [&](auto *row, int i, const float (&v)[VEC]) {
+        using TD = std::remove_reference_t<decltype(*row)>;
+        if (at(i) >= a.width) return;
+        Pack<TD, VEC> p;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) p.v[j] = (TD)v[j];
+        if constexpr (!LOOSE) {
+            store_pack<TD, VEC>(row + at(i), p);
+        } else if (skip(i) == 0) {
+            *reinterpret_cast<Loose<TD, VEC> *>(row + at(i)) = __builtin_bit_cast(Loose<TD, VEC>, p);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (j >= skip(i)) row[at(i) - skip(i) + j] = p.v[j];
+        }
+    };
+    auto live = [&](int i, int j) { return at(i) < a.width && (!LOOSE || j >= skip(i)); };
+
     Pack<TP, VEC> post_w[NV], post_b[NV], pre_w[NV], pre_b[NV];
 #pragma unroll
     for (int i = 0; HOLD && i < NV; ++i) {
@@ -157,27 +194,24 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
         pre_w[i] = get((const TP *)a.pre_w, i);
         pre_b[i] = get((const TP *)a.pre_b, i);
     }
-    // (v - mean) / sqrt(variance + eps) * w + b of the values in v, which are 0
-    // beyond the row's end; `live` says which are not.
+    // (v - mean) / sqrt(variance + eps) * w + b of the values in v.
     auto normed = [&](float (&v)[NV][VEC], int kind, const void *w, const void *b, const auto &wh, const auto &bh) {
         float mean = 0.f, s = 0.f;
         if (kind == ILPM_NORM_LAYER) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) s += v[i][j];
+                for (int j = 0; j < VEC; ++j) s += live(i, j) ? v[i][j] : 0.f;
             mean = total(s) * inv_n;
             s = 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const bool live = (tid + i * T) * VEC < a.width;
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                v[i][j] = live ? v[i][j] - mean : 0.f;
-                s += v[i][j] * v[i][j];
+                v[i][j] -= mean;
+                s += live(i, j) ? v[i][j] * v[i][j] : 0.f;
             }
-        }
         const float rstd = 1.f / sqrtf(total(s) * inv_n + a.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -214,57 +248,45 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
                 for (int j = 0; j < VEC; ++j) u[i][j] = (float)y[i].v[j];
             if (a.post != ILPM_NORM_NONE) normed(u, a.post, a.post_w, a.post_b, post_w, post_b);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const bool live = (tid + i * T) * VEC < a.width;
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
                     if (a.gate) u[i][j] *= (float)gate[i].v[j];
-                    v[i][j] = live ? v[i][j] + a.scale * u[i][j] : 0.f;
+                    v[i][j] += a.scale * u[i][j];
                 }
-            }
         }
         if (a.r) {
-            TX *r = (TX *)a.r + row * a.r_row;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int at = (tid + i * T) * VEC;
-                Pack<TX, VEC> p;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) p.v[j] = (TX)v[i][j];
-                if (at < a.width) *reinterpret_cast<Pack<TX, VEC> *>(r + at) = p;
-            }
+            for (int i = 0; i < NV; ++i) put((TX *)a.r + row * a.r_row, i, v[i]);
         }
         if (a.z) {
             normed(v, a.pre, a.pre_w, a.pre_b, pre_w, pre_b);
-            TY *z = (TY *)a.z + row * a.z_row;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int at = (tid + i * T) * VEC;
-                Pack<TY, VEC> p;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) p.v[j] = (TY)v[i][j];
-                if (at < a.width) *reinterpret_cast<Pack<TY, VEC> *>(z + at) = p;
-            }
+            for (int i = 0; i < NV; ++i) put((TY *)a.z + row * a.z_row, i, v[i]);
         }
     }
 }
 
-template <typename TX, typename TY, typename TP, int T, int E, int VEC>
+template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOOSE>
 void launch_rows(const NormArgs &a, hipStream_t stream)
 {
     constexpr int block = T < 256 ? 256 : T, per = T < 256 ? 256 / T : 1;
     const int groups = std::min(ceil_div(a.rows, per), 256 * 2048 / block);
-    hipLaunchKernelGGL((norm_rows<TX, TY, TP, T, E, VEC>), dim3(groups), dim3(block), 0, stream, a);
+    hipLaunchKernelGGL((norm_rows<TX, TY, TP, T, E, VEC, LOOSE>), dim3(groups), dim3(block), 0, stream, a);
 }
 
-template <typename TX, typename TY, typename TP, int VEC> bool launch_width(const NormArgs &a, hipStream_t stream)
+// By the width: 8 values a thread where that makes a row's group larger but
+// its chain shorter, 16 to reach the next size.
+template <typename TX, typename TY, typename TP, int VEC, bool LOOSE> bool launch_width(const NormArgs &a, hipStream_t stream)
 {
-    if (a.width <= 512) launch_rows<TX, TY, TP, 64, 8, VEC>(a, stream);
-    else if (a.width <= 1024) launch_rows<TX, TY, TP, 64, 16, VEC>(a, stream);
-    else if (a.width <= 2048) launch_rows<TX, TY, TP, 256, 8, VEC>(a, stream);
-    else if (a.width <= 4096) launch_rows<TX, TY, TP, 256, 16, VEC>(a, stream);
-    else if (a.width <= 8192) launch_rows<TX, TY, TP, 1024, 8, VEC>(a, stream);
-    else if (a.width <= 16384) launch_rows<TX, TY, TP, 1024, 16, VEC>(a, stream);
+    if (a.width < VEC) return false;
+    if (a.width <= 128) launch_rows<TX, TY, TP, 16, 8, VEC, LOOSE>(a, stream);
+    else if (a.width <= 512) launch_rows<TX, TY, TP, 64, 8, VEC, LOOSE>(a, stream);
+    else if (a.width <= 1024) launch_rows<TX, TY, TP, 64, 16, VEC, LOOSE>(a, stream);
+    else if (a.width <= 2048) launch_rows<TX, TY, TP, 256, 8, VEC, LOOSE>(a, stream);
+    else if (a.width <= 4096) launch_rows<TX, TY, TP, 256, 16, VEC, LOOSE>(a, stream);
+    else if (a.width <= 8192) launch_rows<TX, TY, TP, 1024, 8, VEC, LOOSE>(a, stream);
+    else if (!LOOSE && a.width <= 16384) launch_rows<TX, TY, TP, 1024, 16, VEC, false>(a, stream);
     else return false;
     return true;
 }
@@ -279,7 +301,7 @@ template <typename TX, typename TY, typename TP> hipError_t launch(const NormArg
     const bool packs = a.width % VEC == 0 && fits(a.x, a.x_row, sx) && fits(a.r, a.r_row, sx) && fits(a.y, a.y_row, sy) &&
                        fits(a.z, a.z_row, sy) && fits(a.gate, a.gate_row, sp) && fits(a.post_w, 0, sp) &&
                        fits(a.post_b, 0, sp) && fits(a.pre_w, 0, sp) && fits(a.pre_b, 0, sp);
-    if (!(packs ? launch_width<TX, TY, TP, VEC>(a, stream) : launch_width<TX, TY, TP, 1>(a, stream)))
+    if (!(packs ? launch_width<TX, TY, TP, VEC, false>(a, stream) : launch_width<TX, TY, TP, VEC, true>(a, stream)))
         hipLaunchKernelGGL((norm_any<TX, TY, TP>), dim3(a.rows), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
