@@ -245,7 +245,10 @@ int attn_decode(const ilpm_kv_cache *cache, const ilpm_heads *q, const int32_t *
     AttnArgs a = {};
     size_t need = 0;
     if ((rc = attn_sizes(cache, q->heads, q->dtype == ILPM_F32, opt->window, opt->max_len, &a, &need)) != ILPM_OK) return rc;
-    if (!std::isfinite(opt->scale) || !(opt->softcap >= 0.f) || !std::isfinite(opt->softcap)) return ILPM_ERR_INVALID_ARG;
+    // (Scores are formed times log2 e, or over softcap.)
+    if (!std::isfinite(opt->scale * 1.5f) || !(opt->softcap >= 0.f) || !std::isfinite(opt->softcap * 1.5f) ||
+        (opt->softcap > 0.f && !std::isfinite(opt->scale / opt->softcap)))
+        return ILPM_ERR_INVALID_ARG;
     if (opt->mask && (opt->mask_len < 0 || !stride_ok(opt->mask_stride))) return ILPM_ERR_INVALID_ARG;
     if (c.n_seqs == 0) return ILPM_OK;
     if ((rc = check_heads(*q)) != ILPM_OK || (rc = check_heads(*out)) != ILPM_OK) return rc;

@@ -56,10 +56,10 @@ enum Rows { kWhole, kPieces, kAny };
 // The keys of a sequence that the window leaves: [first, end).
 __device__ inline void visible_range(const AttnArgs &a, int length, int *first, int *end)
 {
-    const int n = min(max(length, 0), a.capacity);
+    const int own = max(length, 0), n = min(own, a.capacity);
     *end = n;
     // (The window counts from the sequence's own length, also where the table ends before it.)
-    *first = a.window > 0 ? min(n, max(length - a.window, 0)) : 0;
+    *first = a.window > 0 ? min(n, max(own - a.window, 0)) : 0;
 }
 
 // Tiles of 16 keys of a unit of a sequence of this length; 1 for one without
@@ -440,7 +440,8 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
             t.seen[r] = vo >= 0;
             const TC *vrow = vh + max(vo, (int64_t)0);
 #pragma unroll
-            for (int c = 0; c < NV; ++c) t.v[r][c] = load_row<TC, VV, R>(vrow, (n16 + 16 * c) * VV, a.dim);
+            for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
+                t.v[r][c] = load_row<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R>(vrow, (n16 + 16 * c) * VV, a.dim);
         }
     };
     Entry e0 = {}, next = {};

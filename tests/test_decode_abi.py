@@ -104,6 +104,7 @@ def attn(c=None, q=heads(4 * GB, 32), lengths=5 * GB, opt=None, out=heads(6 * GB
     dict(q=heads(4 * GB + 1, 32)), dict(lengths=5 * GB + 1), dict(lse=7 * GB + 2), dict(ws=8 * GB + 128),
     dict(opt=options(window=-1)), dict(opt=options(max_len=-1)), dict(opt=options(scale=math.nan)), dict(opt=options(scale=math.inf)),
     dict(opt=options(cap=-1.0)), dict(opt=options(cap=math.nan)), dict(opt=options(cap=math.inf)),
+    dict(opt=options(scale=3e38)), dict(opt=options(cap=3e38)), dict(opt=options(cap=1e-40)),
     dict(opt=options(mask=9 * GB, mlen=-1)), dict(opt=options(mask=9 * GB, mlen=320, mstride=-320)),
     dict(out=heads(6 * GB, 32, row=0)), dict(out=heads(6 * GB, 32, head=64)),   # outputs that name a place twice
     dict(out=heads(4 * GB + 256, 32)), dict(out=heads(GB, 32)), dict(out=heads(2 * GB, 32)), dict(out=heads(3 * GB, 32)),
