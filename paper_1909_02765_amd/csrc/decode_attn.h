@@ -103,56 +103,47 @@ __device__ inline float tanh_of(float x)
     return fabsf(x) < 0.25f ? near : far;
 }
 
-// N elements of a row from element d on.  Beyond `dim` they are any of the
-// row's own values (cleared where they matter, once they have arrived).
-template <typename T, int N, Rows R> __device__ inline Pack<T, N> load_row(const T *row, int d, int dim)
+// Pieces of rows are held as machine words, whatever they mean: as arrays of
+// 16-bit values the compiler takes them apart when they arrive, which waits
+// for them at once, and puts them together again where they are used.
+template <int BYTES> using Words = typename PackWord<BYTES>::type;
+typedef Words<16> Words16;
+
+__device__ const Words16 attn_zeros = {0, 0, 0, 0};
+
+// N elements of a row from element d on.  What lies beyond `dim` is 0 with
+// ZERO (a piece of zeros is read for it), else any of the row's own values.
+template <typename T, int N, Rows R, bool ZERO> __device__ inline Words<sizeof(T) * N> load_row(const T *row, int d, int dim)
 {
-    Pack<T, N> p;
+    using W = Words<sizeof(T) * N>;
     if constexpr (R == kAny) {
+        Pack<T, N> p;
 #pragma unroll
-        for (int i = 0; i < N; ++i) p.v[i] = row[min(d + i, dim - 1)];
+        for (int i = 0; i < N; ++i) {
+            const T v = row[min(d + i, dim - 1)];
+            p.v[i] = !ZERO || d + i < dim ? v : (T)0.f;
+        }
+        return __builtin_bit_cast(W, p);
+    } else if constexpr (R == kPieces) {
+        return *reinterpret_cast<const W *>(d < dim ? row + d : ZERO ? (const T *)&attn_zeros : row);
     } else {
-        p = *reinterpret_cast<const Pack<T, N> *>(row + (R == kWhole || d < dim ? d : 0));
+        return *reinterpret_cast<const W *>(row + d);
     }
-    return p;
 }
 
-// p with what lies beyond `dim` cleared (of pieces all or nothing).
-template <typename T, int N, Rows R> __device__ inline Pack<T, N> cleared(Pack<T, N> p, int d, int dim)
+template <typename TC> __device__ inline floatx4 mfma_scores(Words16 k, Words16 q, floatx4 c)
 {
-    if constexpr (R == kPieces) {
-        struct Words {
-            unsigned w[sizeof(p) / 4];
-        } words = __builtin_bit_cast(Words, p);
-        const unsigned keep = d < dim ? 0xffffffffu : 0u;
-#pragma unroll
-        for (unsigned i = 0; i < sizeof(p) / 4; ++i) words.w[i] &= keep;
-        p = __builtin_bit_cast(Pack<T, N>, words);
-    } else if constexpr (R == kAny) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) p.v[i] = d + i < dim ? p.v[i] : (T)0.f;
-    }
-    return p;
+    if constexpr (__is_same(TC, __bf16))
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k), __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
 }
-
-__device__ inline floatx4 mfma_scores(const Pack<__bf16, 8> &k, const Pack<__bf16, 8> &q, floatx4 c)
+template <typename TC> __device__ inline floatx4 mfma_values(Words<8> v, Words<8> p, floatx4 c)
 {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
-}
-__device__ inline floatx4 mfma_scores(const Pack<_Float16, 8> &k, const Pack<_Float16, 8> &q, floatx4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k), __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
-}
-// (An f32 cache never comes to these.)
-__device__ inline floatx4 mfma_scores(const Pack<float, 4> &, const Pack<float, 4> &, floatx4 c) { return c; }
-__device__ inline floatx4 mfma_values(uint2, const Pack<float, 4> &, floatx4 c) { return c; }
-__device__ inline floatx4 mfma_values(uint2 v, const Pack<__bf16, 4> &p, floatx4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(shortx4, v), __builtin_bit_cast(shortx4, p), c, 0, 0, 0);
-}
-__device__ inline floatx4 mfma_values(uint2 v, const Pack<_Float16, 4> &p, floatx4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, v), __builtin_bit_cast(f16x4, p), c, 0, 0, 0);
+    if constexpr (__is_same(TC, __bf16))
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(shortx4, v), __builtin_bit_cast(shortx4, p), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, v), __builtin_bit_cast(f16x4, p), c, 0, 0, 0);
 }
 
 // TC: the cache's type.  Q16: queries and outputs are of that same 16-bit type
@@ -179,8 +170,8 @@ template <typename TC, bool Q16, int DC, Rows R, bool SHORT> struct AttnKernel {
     // A tile of 16 keys: lane (n, g) holds pieces g, g + 4, ... of key n's K row,
     // and pieces n, n + 16, ... of the V rows of keys 4g..4g+3.
     struct Tile {
-        Pack<TC, KV> k[NK];
-        Pack<TC, VV> v[4][NV];
+        Words16 k[NK];
+        Words<sizeof(TC) * VV> v[4][NV];
         bool seen[4];
     };
 };
@@ -318,7 +309,7 @@ template <typename Cfg, typename TC> struct AttnLds {
     float o[4][kAttnHeads][Cfg::DO + 4];
     FindShare found;
     // The three parts of 32-bit queries, as the lanes of the first product take them.
-    Pack<TC, Cfg::KV> q[Cfg::QP == 3 ? 3 : 1][Cfg::QP == 3 ? Cfg::NK : 1][Cfg::QP == 3 ? 64 : 1];
+    Words16 q[Cfg::QP == 3 ? 3 : 1][Cfg::QP == 3 ? Cfg::NK : 1][Cfg::QP == 3 ? 64 : 1];
     float unscale[kAttnHeads];
 };
 
@@ -332,10 +323,19 @@ __device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), n16 = lane & 15, g = lane >> 4;
     const int in_group = min(seg.hb * kAttnHeads + n16, a.group - 1);
     const float *row = (const float *)a.q + (int64_t)seg.seq * a.q_row + ((int64_t)seg.kvh * a.group + in_group) * a.q_head;
-    auto get = [&](int c) {
-        const int d = (g + 4 * c) * KV;
-        const Pack<float, KV> p = a.q_pieces ? load_row<float, KV, kPieces>(row, d, a.dim) : load_row<float, KV, kAny>(row, d, a.dim);
-        return cleared<float, KV, R>(p, d, a.dim);
+    struct Values {
+        float v[KV];
+    };
+    auto get = [&](int c) {  // KV = 8 values: two pieces of four
+        struct Halves {
+            Words16 w[2];
+        } h;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int d = (g + 4 * c) * KV + 4 * n;
+            h.w[n] = a.q_pieces ? load_row<float, 4, kPieces, true>(row, d, a.dim) : load_row<float, 4, kAny, true>(row, d, a.dim);
+        }
+        return __builtin_bit_cast(Values, h);
     };
     float f = 1.f, back = 1.f;
     if constexpr (__is_same(TC, _Float16)) {
@@ -343,7 +343,7 @@ __device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &
         float most = 0.f;
 #pragma unroll 2
         for (int c = 0; c < NK; ++c) {
-            const Pack<float, KV> p = get(c);
+            const Values p = get(c);
 #pragma unroll
             for (int i = 0; i < KV; ++i) most = fmaxf(most, fabsf(p.v[i]));
         }
@@ -354,13 +354,13 @@ __device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &
         back = __builtin_ldexpf(1.f, -by);
     }
     if (wave == 0 && g == 0) lds.unscale[n16] = back;
-    Pack<float, KV> mine[(NK + 3) / 4];
+    Values mine[(NK + 3) / 4];
 #pragma unroll
     for (int j = 0; j < (NK + 3) / 4; ++j) mine[j] = get(min(wave + 4 * j, NK - 1));
 #pragma unroll
     for (int j = 0; j < (NK + 3) / 4; ++j) {
         const int c = min(wave + 4 * j, NK - 1);  // (the last one several times over, with the same values)
-        const Pack<float, KV> p = mine[j];
+        const Values p = mine[j];
         Pack<TC, KV> part[3];
 #pragma unroll
         for (int i = 0; i < KV; ++i) {
@@ -371,7 +371,7 @@ __device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &
             part[2].v[i] = (TC)(v - (float)part[1].v[i]);
         }
 #pragma unroll
-        for (int n = 0; n < 3; ++n) lds.q[n][c][lane] = part[n];
+        for (int n = 0; n < 3; ++n) lds.q[n][c][lane] = __builtin_bit_cast(Words16, part[n]);
     }
     __syncthreads();
 }
@@ -433,7 +433,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
         const int i0 = (j & 3) * 16;
         const TC *krow = kh + max(p.k[i0 + n16], (int64_t)0);
 #pragma unroll
-        for (int c = 0; c < NK; ++c) t.k[c] = load_row<TC, KV, R>(krow, (g + 4 * c) * KV, a.dim);
+        for (int c = 0; c < NK; ++c) t.k[c] = load_row<TC, KV, R, true>(krow, (g + 4 * c) * KV, a.dim);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int64_t vo = p.v[i0 + 4 * g + r];
@@ -441,7 +441,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
             const TC *vrow = vh + max(vo, (int64_t)0);
 #pragma unroll
             for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
-                t.v[r][c] = load_row<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R>(vrow, (n16 + 16 * c) * VV, a.dim);
+                t.v[r][c] = load_row<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R, false>(vrow, (n16 + 16 * c) * VV, a.dim);
         }
     };
     Entry e0 = {}, next = {};
@@ -453,7 +453,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
     // The queries, in the layout of the K loads.  (Lanes without a head take
     // the last one's, and give nothing.)  Those in parts stay in LDS: beside the tiles
     // they would not fit the registers.
-    Pack<TQ, KV> q[QP == 3 ? 1 : NK];
+    Words16 q[QP == 3 ? 1 : NK];
     float unscale = 1.f;  // f16 parts of 32-bit queries are those of the queries over this
     if constexpr (QP == 3) {
         unscale = lds.unscale[n16];
@@ -461,13 +461,11 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
         const TQ *row = (const TQ *)a.q + (int64_t)seq * a.q_row + ((int64_t)seg.kvh * a.group + min(in_group, a.group - 1)) * a.q_head;
         if (a.q_pieces) {
 #pragma unroll
-            for (int c = 0; c < NK; ++c) q[c] = load_row<TQ, KV, R == kAny ? kPieces : R>(row, (g + 4 * c) * KV, a.dim);
+            for (int c = 0; c < NK; ++c) q[c] = load_row<TQ, KV, R == kAny ? kPieces : R, true>(row, (g + 4 * c) * KV, a.dim);
         } else {
 #pragma unroll
-            for (int c = 0; c < NK; ++c) q[c] = load_row<TQ, KV, kAny>(row, (g + 4 * c) * KV, a.dim);
+            for (int c = 0; c < NK; ++c) q[c] = load_row<TQ, KV, kAny, true>(row, (g + 4 * c) * KV, a.dim);
         }
-#pragma unroll
-        for (int c = 0; c < NK; ++c) q[c] = cleared<TQ, KV, R>(q[c], (g + 4 * c) * KV, a.dim);
     }
 
     floatx4 o[NO], ol[C16 ? NO : 1];  // (ol: of the probabilities' small parts)
@@ -480,10 +478,9 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
         if constexpr (!C16) {
 #pragma unroll
             for (int c = 0; c < NK; ++c) {
-                const Pack<TC, KV> k = cleared<TC, KV, R>(t.k[c], (g + 4 * c) * KV, a.dim);
 #pragma unroll
                 for (int i = 0; i < KV; ++i)
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32((float)k.v[i], (float)q[c].v[i], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, t.k[c])[i], __builtin_bit_cast(floatx4, q[c])[i], s, 0, 0, 0);
             }
         } else {
             floatx4 low = s;
@@ -491,13 +488,12 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
             if constexpr (QP == 3) asm volatile("" : "+v"(ql));  // (read for each tile, not kept)
 #pragma unroll
             for (int c = 0; c < NK; ++c) {
-                const Pack<TC, KV> k = cleared<TC, KV, R>(t.k[c], (g + 4 * c) * KV, a.dim);
                 if constexpr (QP == 3) {
-                    s = mfma_scores(k, lds.q[0][c][ql], s);
-                    low = mfma_scores(k, lds.q[1][c][ql], low);
-                    low = mfma_scores(k, lds.q[2][c][ql], low);
+                    s = mfma_scores<TC>(t.k[c], lds.q[0][c][ql], s);
+                    low = mfma_scores<TC>(t.k[c], lds.q[1][c][ql], low);
+                    low = mfma_scores<TC>(t.k[c], lds.q[2][c][ql], low);
                 } else {
-                    s = mfma_scores(k, q[c], s);
+                    s = mfma_scores<TC>(t.k[c], q[c], s);
                 }
             }
             if constexpr (QP == 3) {
@@ -536,17 +532,20 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
                 for (int c = 0; c < NV; ++c)
 #pragma unroll
                     for (int i = 0; i < VV; ++i)
-                        o[c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.seen[r] ? (float)t.v[r][c].v[i] : 0.f, p[r],
+                        o[c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.seen[r] ? __builtin_bit_cast(floatx4, t.v[r][c])[i] : 0.f, p[r],
                                                                             o[c * VV + i], 0, 0, 0);
         } else {
-            Pack<TC, 4> part[PP];
+            Words<8> part[PP];
 #pragma unroll
-            for (int i = 0; i < PP; ++i)
+            for (int i = 0; i < PP; ++i) {
+                Pack<TC, 4> h;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    part[i].v[r] = (TC)p[r];
-                    p[r] -= (float)part[i].v[r];
+                    h.v[r] = (TC)p[r];
+                    p[r] -= (float)h.v[r];
                 }
+                part[i] = __builtin_bit_cast(Words<8>, h);
+            }
             // Selectors of the lower and the upper halves of two rows' registers: a byte 0x0c gives 0.
             unsigned lower[2], upper[2];
 #pragma unroll
@@ -559,18 +558,12 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
             for (int c = 0; c < NV; ++c)
 #pragma unroll
                 for (int i = 0; i < VV; ++i) {
-                    struct Words {
-                        unsigned w[VV / 2];
-                    };
-                    unsigned w[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) w[r] = __builtin_bit_cast(Words, t.v[r][c]).w[i / 2];
-                    const uint2 v = {__builtin_amdgcn_perm(w[1], w[0], i & 1 ? upper[0] : lower[0]),
-                                     __builtin_amdgcn_perm(w[3], w[2], i & 1 ? upper[1] : lower[1])};
+                    const Words<8> v = {__builtin_amdgcn_perm(t.v[1][c][i / 2], t.v[0][c][i / 2], i & 1 ? upper[0] : lower[0]),
+                                        __builtin_amdgcn_perm(t.v[3][c][i / 2], t.v[2][c][i / 2], i & 1 ? upper[1] : lower[1])};
 #pragma unroll
                     for (int k = 0; k < PP; ++k) {
                         floatx4 &sum = k == 0 ? o[c * VV + i] : ol[c * VV + i];
-                        sum = mfma_values(v, part[k], sum);
+                        sum = mfma_values<TC>(v, part[k], sum);
                     }
                 }
         }
