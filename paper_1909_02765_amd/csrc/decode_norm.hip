@@ -17,8 +17,9 @@ __device__ inline float sum256(float v, float *lds)
 }
 
 // Any width, strides and alignment: a workgroup per row, which reads the row
-// again for each sum it needs (very wide rows, and those of less than a pack).  Each element is written by the thread that
-// reads it, in the last pass, so r may be x and z may be y.
+// again for each sum it needs (very wide rows, and those of less than a pack).
+// Each element is written by the thread that reads it, in the last pass, so r may
+// be x and z may be y.
 template <typename TX, typename TY, typename TP> __global__ __launch_bounds__(256) void norm_any(NormArgs a)
 {
     __shared__ float lds[4];
@@ -94,13 +95,13 @@ template <int CTRL> __device__ inline float plus_permuted(float v)
     return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 
-// The sum over groups of LANES (16 or 64) lanes.
+// The sum over groups of LANES (2, 4, 8, 16 or 64) lanes.
 template <int LANES> __device__ inline float lanes_sum(float v)
 {
     v = plus_permuted<0xB1>(v);   // lanes 1 0 3 2 of each four
-    v = plus_permuted<0x4E>(v);   // lanes 2 3 0 1 of each four
-    v = plus_permuted<0x141>(v);  // the other four of eight
-    v = plus_permuted<0x140>(v);  // the other eight of sixteen
+    if constexpr (LANES > 2) v = plus_permuted<0x4E>(v);  // lanes 2 3 0 1 of each four
+    if constexpr (LANES > 4) v = plus_permuted<0x141>(v);  // the other four of eight
+    if constexpr (LANES > 8) v = plus_permuted<0x140>(v);  // the other eight of sixteen
     if constexpr (LANES == 64) {
         unsigned x = __builtin_bit_cast(unsigned, v);
         const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
@@ -123,7 +124,8 @@ template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) 
 // Rows of up to T * E values: T threads hold a row in registers, E values each,
 // in packs of VEC, so each input is read once and each output written once.  T
 // up to 64 leaves a row to part of a wave or a wave (no barrier).  Weights and
-// biases stay in registers over the rows that a workgroup takes.
+// biases stay in registers over the rows that a workgroup takes, and a row is
+// read while the one before it is worked on (7512 f32 rows of 2247 59 -> 47 us).
 //
 // LOOSE: rows of any alignment and of any width from VEC on.  The last pack then
 // ends with the row, over some values of the pack before it: these count in no
@@ -132,12 +134,16 @@ template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) 
 //
 // Mean and variance come from the values in registers, in two steps, so a mean
 // far from zero costs the variance nothing.  What bounds it: the bytes of x, y,
-// gate, r and z.
+// gate, r and z (16381 rows of 4096, f32 over bf16: 201 us, 5.3 TB/s).  Of 16-bit
+// rows of several thousand values it is the vector unit's work on them and on the
+// sums, which one row a compute unit does not hide (6556 bf16 rows of 6723: 106 us,
+// 3.3 TB/s).
 template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOOSE>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
+__global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
 {
-    constexpr int NV = E / VEC, ROWS = T < 256 ? 256 / T : 1, WAVES = T > 64 ? T / 64 : 1;
-    constexpr bool HOLD = T * E <= 8192;  // (beyond, they do not fit beside the row: read again for each)
+    constexpr int NV = E / VEC, ROWS = T <= 64 ? 256 / T : 1, WAVES = T > 64 ? T / 64 : 1;
+    // Beyond, neither weights nor a second row fit beside the row: read for each, when it comes.
+    constexpr bool HOLD = T * E <= 8192;
     __shared__ float lds[WAVES > 1 ? 2 * WAVES : 1];
     const int tid = threadIdx.x % T;
     const float inv_n = 1.f / (float)a.width;
@@ -150,9 +156,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
             turn ^= 1;
             if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
             __syncthreads();
-            v = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) v += part[w];
+            v = lanes_sum<WAVES>(part[threadIdx.x % WAVES]);
         }
         return v;
     };
@@ -186,6 +190,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
     };
     auto live = [&](int i, int j) { return at(i) < a.width && (!LOOSE || j >= skip(i)); };
 
+    // Of most waves all values count.
+    const bool full = __all(at(NV - 1) + VEC <= a.width);
     Pack<TP, VEC> post_w[NV], post_b[NV], pre_w[NV], pre_b[NV];
 #pragma unroll
     for (int i = 0; HOLD && i < NV; ++i) {
@@ -196,23 +202,33 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
     }
     // (v - mean) / sqrt(variance + eps) * w + b of the values in v.
     auto normed = [&](float (&v)[NV][VEC], int kind, const void *w, const void *b, const auto &wh, const auto &bh) {
-        float mean = 0.f, s = 0.f;
+        // The sum of term(v) over the row.
+        auto sum = [&](auto term) {
+            float s = 0.f;
+            if (full) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) s += term(v[i][j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float t = term(v[i][j]);
+                        s += live(i, j) ? t : 0.f;
+                    }
+            }
+            return total(s);
+        };
         if (kind == ILPM_NORM_LAYER) {
+            const float mean = sum([](float x) { return x; }) * inv_n;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) s += live(i, j) ? v[i][j] : 0.f;
-            mean = total(s) * inv_n;
-            s = 0.f;
+                for (int j = 0; j < VEC; ++j) v[i][j] -= mean;
         }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                v[i][j] -= mean;
-                s += live(i, j) ? v[i][j] * v[i][j] : 0.f;
-            }
-        const float rstd = 1.f / sqrtf(total(s) * inv_n + a.eps);
+        const float rstd = rsqrtf(sum([](float x) { return x * x; }) * inv_n + a.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const Pack<TP, VEC> wp = HOLD ? wh[i] : get((const TP *)w, i), bp = HOLD ? bh[i] : get((const TP *)b, i);
@@ -225,18 +241,32 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
         }
     };
 
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
-        float v[NV][VEC], u[NV][VEC];
+    struct Row {
         Pack<TX, VEC> x[NV];
         Pack<TY, VEC> y[NV];
         Pack<TP, VEC> gate[NV];
+    };
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    auto load = [&](Row &t, int64_t row) {
         const TP *grow = a.gate ? (const TP *)a.gate + row * a.gate_row : nullptr;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) y[i] = get(a.y ? (const TY *)a.y + row * a.y_row : (const TY *)nullptr, i);
+        for (int i = 0; i < NV; ++i) t.y[i] = get(a.y ? (const TY *)a.y + row * a.y_row : (const TY *)nullptr, i);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) x[i] = get((const TX *)a.x + row * a.x_row, i);
+        for (int i = 0; i < NV; ++i) t.x[i] = get((const TX *)a.x + row * a.x_row, i);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) gate[i] = get(grow, i);
+        for (int i = 0; i < NV; ++i) t.gate[i] = get(grow, i);
+    };
+    Row next;
+    int64_t row = (int64_t)blockIdx.x * ROWS + (T < 64 ? (int)threadIdx.x / T : __builtin_amdgcn_readfirstlane((int)threadIdx.x / T));
+    if (HOLD && row < a.rows) load(next, row);
+    for (; row < a.rows; row += step) {
+        float v[NV][VEC], u[NV][VEC];
+        if (!HOLD) load(next, row);
+        const Row t = next;
+        const auto &x = t.x;
+        const auto &y = t.y;
+        const auto &gate = t.gate;
+        if (HOLD && row + step < a.rows) load(next, row + step);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -267,24 +297,32 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_rows(NormArgs a)
     }
 }
 
+// As many workgroups as the 256 compute units hold at once, with the same number
+// of rows each, give or take one: more would read the weights again (9116 f32 rows
+// of 1015 23.0 -> 22.2 us).  By their registers that is 16 waves a unit, of 16-bit
+// rows in workgroups of up to four waves 20 (3822 bf16 rows of 1732 14.1 -> 13.2 us).
 template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOOSE>
 void launch_rows(const NormArgs &a, hipStream_t stream)
 {
-    constexpr int block = T < 256 ? 256 : T, per = T < 256 ? 256 / T : 1;
-    const int groups = std::min(ceil_div(a.rows, per), 256 * 2048 / block);
+    constexpr int block = T <= 64 ? 256 : T, per = T <= 64 ? 256 / T : 1;
+    constexpr int waves = sizeof(TX) == 2 && T <= 256 ? 20 : 16;
+    const int rows = ceil_div(a.rows, per), turns = ceil_div(rows, 256 * 64 * waves / block);
+    const int groups = ceil_div(rows, turns);
     hipLaunchKernelGGL((norm_rows<TX, TY, TP, T, E, VEC, LOOSE>), dim3(groups), dim3(block), 0, stream, a);
 }
 
-// By the width: 8 values a thread where that makes a row's group larger but
-// its chain shorter, 16 to reach the next size.
+// By the width: 8 values a thread.  With 16 too few waves fit a compute unit to cover
+// each other's waits (13447 bf16 rows of 675 28.8 -> 23.6 us with two waves for
+// one, 14016 f16 rows of 3651 135 -> 92 with eight for four); rows beyond 8192 have
+// no more threads to go to.
 template <typename TX, typename TY, typename TP, int VEC, bool LOOSE> bool launch_width(const NormArgs &a, hipStream_t stream)
 {
     if (a.width < VEC) return false;
     if (a.width <= 128) launch_rows<TX, TY, TP, 16, 8, VEC, LOOSE>(a, stream);
     else if (a.width <= 512) launch_rows<TX, TY, TP, 64, 8, VEC, LOOSE>(a, stream);
-    else if (a.width <= 1024) launch_rows<TX, TY, TP, 64, 16, VEC, LOOSE>(a, stream);
+    else if (a.width <= 1024) launch_rows<TX, TY, TP, 128, 8, VEC, LOOSE>(a, stream);
     else if (a.width <= 2048) launch_rows<TX, TY, TP, 256, 8, VEC, LOOSE>(a, stream);
-    else if (a.width <= 4096) launch_rows<TX, TY, TP, 256, 16, VEC, LOOSE>(a, stream);
+    else if (a.width <= 4096) launch_rows<TX, TY, TP, 512, 8, VEC, LOOSE>(a, stream);
     else if (a.width <= 8192) launch_rows<TX, TY, TP, 1024, 8, VEC, LOOSE>(a, stream);
     else if (!LOOSE && a.width <= 16384) launch_rows<TX, TY, TP, 1024, 16, VEC, false>(a, stream);
     else return false;

@@ -476,6 +476,15 @@ def test_norm_alone_and_in_place():
         check_norm(c, "in place", cuda=dict(x=x, r=x, y=y, z=y))
 
 
+@pytest.mark.parametrize("rows,width", [(33000, 20), (5001, 130), (2100, 515), (1030, 2001), (600, 4090), (300, 7001), (300, 9000)])
+def test_norm_in_place_over_many_rows(rows, width):
+    """More rows than run at once: a row is read while the one before it is written, over itself."""
+    for types in ((F32, BF16, F32), (F16, F16, F16)):
+        c = norm_case(gen(width), rows, width, *types, "rms", "layer", "rows", True, True)
+        x, y = c["x"].cuda(), c["y"].cuda()
+        check_norm(c, f"{types} {rows}x{width}", cuda=dict(x=x, r=x, y=y, z=y))
+
+
 def test_norm_strided():
     g = gen(14)
     for width, shift in ((512, 0), (512, 8), (512, 1), (1000, 0), (77, 3)):
