@@ -27,23 +27,31 @@ template <> struct PackWord<8> { typedef unsigned type __attribute__((ext_vector
 template <> struct PackWord<4> { typedef unsigned type; };
 template <> struct PackWord<2> { typedef unsigned short type; };
 
-template <typename T, int N> __device__ inline Pack<T, N> load_pack(const T *p)
+// (ALIGN: of the address, in bytes.  The memory system takes words on any
+// element's boundary whole as well.)
+template <int ALIGN, typename T, int N> __device__ inline Pack<T, N> load_words(const T *p)
 {
     using W = typename PackWord<(int)sizeof(Pack<T, N>)>::type;
+    typedef W At __attribute__((aligned(ALIGN)));
     struct Words { W w[sizeof(Pack<T, N>) / sizeof(W)]; } words;
 #pragma unroll
-    for (unsigned i = 0; i < sizeof(words) / sizeof(W); ++i) words.w[i] = reinterpret_cast<const W *>(p)[i];
+    for (unsigned i = 0; i < sizeof(words) / sizeof(W); ++i) words.w[i] = reinterpret_cast<const At *>(p)[i];
     return __builtin_bit_cast(Pack<T, N>, words);
 }
-
-template <typename T, int N> __device__ inline void store_pack(T *p, const Pack<T, N> &v)
+template <int ALIGN, typename T, int N> __device__ inline void store_words(T *p, const Pack<T, N> &v)
 {
     using W = typename PackWord<(int)sizeof(Pack<T, N>)>::type;
+    typedef W At __attribute__((aligned(ALIGN)));
     struct Words { W w[sizeof(Pack<T, N>) / sizeof(W)]; };
     const Words words = __builtin_bit_cast(Words, v);
 #pragma unroll
-    for (unsigned i = 0; i < sizeof(words) / sizeof(W); ++i) reinterpret_cast<W *>(p)[i] = words.w[i];
+    for (unsigned i = 0; i < sizeof(words) / sizeof(W); ++i) reinterpret_cast<At *>(p)[i] = words.w[i];
 }
+// Of a pack that is aligned as one, and of one that is aligned to an element only.
+template <typename T, int N> __device__ inline Pack<T, N> load_pack(const T *p) { return load_words<alignof(Pack<T, N>), T, N>(p); }
+template <typename T, int N> __device__ inline Pack<T, N> load_loose(const T *p) { return load_words<sizeof(T), T, N>(p); }
+template <typename T, int N> __device__ inline void store_pack(T *p, const Pack<T, N> &v) { store_words<alignof(Pack<T, N>), T, N>(p, v); }
+template <typename T, int N> __device__ inline void store_loose(T *p, const Pack<T, N> &v) { store_words<sizeof(T), T, N>(p, v); }
 
 // ---- kv_append ----
 struct AppendArgs {

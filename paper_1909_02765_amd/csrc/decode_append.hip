@@ -8,22 +8,32 @@
 // in place.
 #include "decode.h"
 
-#include <algorithm>
-
 namespace ilpm {
 namespace {
+
+// Division of 0 <= n < 2^31 by d >= 1 as a product: with 2^(s-1) < d <= 2^s and
+// m = floor(2^32 (2^s - d) / d) + 1, n / d = (floor(n m / 2^32) + n) >> s.
+struct Divisor {
+    unsigned m, s;
+    explicit Divisor(unsigned d) : s(0)
+    {
+        while ((1ull << s) < d) ++s;
+        m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+    }
+    __device__ int of(int n) const { return (int)((__umulhi((unsigned)n, m) + (unsigned)n) >> s); }
+};
 
 // Where a token goes: its page and slot, -1 where it is not written.
 struct Place {
     int page, slot;
 };
 
-__device__ inline Place place_of(const AppendArgs &a, int t, int pos)
+template <typename F> __device__ inline Place place_of(const AppendArgs &a, int t, int pos, F page_of)
 {
     Place p = {-1, 0};
     const int seq = a.seq_ids[t];
     if (seq < 0 || seq >= a.n_seqs || pos < 0) return p;
-    const int at = pos / a.page_size;
+    const int at = page_of(pos);
     if (at >= a.max_pages) return p;
     const int page = a.table[(int64_t)seq * a.table_stride + at];
     if (page < 0 || page >= a.n_pages) return p;
@@ -39,7 +49,7 @@ template <typename TX, typename TC> __global__ __launch_bounds__(256) void appen
     const int t = blockIdx.x;
     const int pos = a.positions[t];
     const bool turn = a.rot_dim > 0 && pos >= 0 && pos < a.n_positions;
-    Place at = place_of(a, t, pos);
+    Place at = place_of(a, t, pos, [&](int n) { return n / a.page_size; });
     if (a.rot_dim > 0 && !turn) at.page = -1;
     const int half = a.rot_dim / 2, units = a.dim - half;  // of a rotated head: pairs, then single elements
     const float *cos = a.cos + (turn ? (int64_t)pos * half : 0), *sin = a.sin + (turn ? (int64_t)pos * half : 0);
@@ -79,48 +89,56 @@ template <typename TX, typename TC> __global__ __launch_bounds__(256) void appen
     }
 }
 
-// Rows that divide into packs of VEC elements (of pairs: both halves do): a
-// thread takes one pack of a token's head, or one of each half.  What bounds
-// it: the bytes of queries, keys and values, read and written once.  (Threads
-// that took several heads, to read the angles once for them, were slower: 16381
-// tokens of 40 + 8 heads of 128 in bf16 90 us with one head a thread, 5.3 TB/s,
-// 92 with two, 108 with four.)
-template <typename TX, typename TC, int VEC> __global__ __launch_bounds__(256) void append_packs(AppendArgs a)
+// The packs of VEC that cover n elements: where they do not divide, the last one
+// ends with them, over some of the one before it.  Both then write the same
+// values there (which a rotation in place would not, see packs_fit).
+template <int VEC> __host__ __device__ inline int packs(int n) { return (n + VEC - 1) / VEC; }
+template <int VEC> __device__ inline int pack_at(int u, int n) { return min(u * VEC, n - VEC); }
+
+// A thread takes one pack of VEC elements of a token's head or, where halves
+// turn, one of each half; packs may have any alignment.  What bounds it: the
+// bytes of queries, keys and values, read and written once.  (Threads that took
+// several heads, to read the angles once for them, were slower: 16381 tokens of
+// 40 + 8 heads of 128 in bf16 90 us with one head a thread, 5.3 TB/s, 92 with
+// two, 108 with four.)
+template <typename TX, typename TC, int VEC>
+__global__ __launch_bounds__(256) void append_packs(AppendArgs a, Divisor by_per, Divisor by_units, Divisor by_vunits, Divisor by_page)
 {
-    const int half = a.rot_dim / 2;
+    const int half = a.rot_dim / 2, rest = a.dim - a.rot_dim, turns = a.pairs ? a.rot_dim : half;
     // Packs of a rotated head (the first `turned` of them with their partners, or
     // in pairs of neighbours), and of a value head.
-    const int turned = (a.pairs ? a.rot_dim : half) / VEC, units = a.dim / VEC - (a.pairs ? 0 : half / VEC);
-    const int vunits = a.dim / VEC, rotated_heads = a.q_heads + a.kv_heads;
-    const unsigned per = rotated_heads * units + a.kv_heads * vunits;
-    const unsigned id = blockIdx.x * 256u + threadIdx.x;  // (at most 2^24 workgroups)
-    const int t = (int)(id / per);
+    const int turned = packs<VEC>(turns), units = turned + packs<VEC>(rest);
+    const int vunits = packs<VEC>(a.dim), rotated_heads = a.q_heads + a.kv_heads;
+    const int per = rotated_heads * units + a.kv_heads * vunits;
+    const int id = (int)(blockIdx.x * 256u + threadIdx.x);  // (fewer than 2^23 workgroups)
+    const int t = by_per.of(id);
     if (t >= a.n_tokens) return;
-    const int i = (int)(id - t * per);
+    const int i = id - t * per;
+    auto page_of = [&](int n) { return by_page.of(n); };
     const int pos = a.positions[t];
     const bool known = a.rot_dim > 0 && pos >= 0 && pos < a.n_positions;
 
     if (i >= rotated_heads * units) {  // of a value
-        const int j = i - rotated_heads * units, h = j / vunits, e = (j - h * vunits) * VEC;
-        const Pack<TX, VEC> p = load_pack<TX, VEC>((const TX *)a.v + (int64_t)t * a.v_row + h * a.v_head + e);
-        const Place at = place_of(a, t, pos);
+        const int j = i - rotated_heads * units, h = by_vunits.of(j), e = pack_at<VEC>(j - h * vunits, a.dim);
+        const Pack<TX, VEC> p = load_loose<TX, VEC>((const TX *)a.v + (int64_t)t * a.v_row + h * a.v_head + e);
+        const Place at = place_of(a, t, pos, page_of);
         if (at.page < 0 || (a.rot_dim > 0 && !known)) return;
         Pack<TC, VEC> o;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) o.v[j] = (TC)(float)p.v[j];
-        store_pack<TC, VEC>((TC *)a.vc + (int64_t)at.page * a.vc_page + (int64_t)at.slot * a.vc_slot + h * a.vc_head + e, o);
+        store_loose<TC, VEC>((TC *)a.vc + (int64_t)at.page * a.vc_page + (int64_t)at.slot * a.vc_slot + h * a.vc_head + e, o);
         return;
     }
 
-    const int h = i / units, u = i - h * units;
+    const int h = by_units.of(i), u = i - h * units;
     const bool rotated = u < turned, two = rotated && !a.pairs, turn = rotated && known, query = h < a.q_heads;
     // Elements e.. and, of halves, their partners from e2.
-    const int e = a.pairs || rotated ? u * VEC : half + u * VEC, e2 = e + half;
+    const int e = rotated ? pack_at<VEC>(u, turns) : a.rot_dim + pack_at<VEC>(u - turned, rest), e2 = e + half;
     const TX *src = query ? (const TX *)a.q + (int64_t)t * a.q_row + h * a.q_head
                           : (const TX *)a.k + (int64_t)t * a.k_row + (h - a.q_heads) * a.k_head;
-    const Pack<TX, VEC> p = load_pack<TX, VEC>(src + e);
+    const Pack<TX, VEC> p = load_loose<TX, VEC>(src + e);
     Pack<TX, VEC> p2 = {};
-    if (two) p2 = load_pack<TX, VEC>(src + e2);
+    if (two) p2 = load_loose<TX, VEC>(src + e2);
     // VEC angles for halves, VEC / 2 for pairs.
     constexpr int HV = VEC / 2;
     float c[VEC], s[VEC];
@@ -129,8 +147,8 @@ template <typename TX, typename TC, int VEC> __global__ __launch_bounds__(256) v
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             if (n == 1 && !two) break;
-            const Pack<float, HV> cp = load_pack<float, HV>(a.cos + first + n * HV);
-            const Pack<float, HV> sp = load_pack<float, HV>(a.sin + first + n * HV);
+            const Pack<float, HV> cp = load_loose<float, HV>(a.cos + first + n * HV);
+            const Pack<float, HV> sp = load_loose<float, HV>(a.sin + first + n * HV);
 #pragma unroll
             for (int j = 0; j < HV; ++j) c[n * HV + j] = cp.v[j], s[n * HV + j] = sp.v[j];
         }
@@ -138,7 +156,7 @@ template <typename TX, typename TC, int VEC> __global__ __launch_bounds__(256) v
     // (The queries of a token are turned wherever its keys go.)
     Place at = {-1, 0};
     if (!query) {
-        at = place_of(a, t, pos);
+        at = place_of(a, t, pos, page_of);
         if (at.page < 0 || (a.rot_dim > 0 && !known)) return;
     }
     float x[VEC], y[VEC];
@@ -164,40 +182,36 @@ template <typename TX, typename TC, int VEC> __global__ __launch_bounds__(256) v
         Pack<TD, VEC> o;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) o.v[j] = (TD)x[j];
-        store_pack<TD, VEC>(dst + e, o);
+        store_loose<TD, VEC>(dst + e, o);
         if (!two) return;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) o.v[j] = (TD)y[j];
-        store_pack<TD, VEC>(dst + e2, o);
+        store_loose<TD, VEC>(dst + e2, o);
     };
     if (query) put((TX *)a.q_out + (int64_t)t * a.qo_row + h * a.qo_head);
     else put((TC *)a.kc + (int64_t)at.page * a.kc_page + (int64_t)at.slot * a.kc_slot + (h - a.q_heads) * a.kc_head);
 }
 
-// Whether everything divides into packs of `vec` elements, aligned to 16
-// bytes or the pack's size.
-bool packs_fit(const AppendArgs &a, int vec, int sx, int sc)
+// Whether everything falls into packs of VEC: what turns, what does not, and
+// values have one pack at least; packs of queries that are turned in place do not
+// overlap, nor do those of 32 bytes (11864 tokens of 68 f32 heads of 72 turned by
+// halves of 36: 104 us in overlapping packs of eight, 88 in packs of four).
+template <int VEC> bool packs_fit(const AppendArgs &a, int element)
 {
-    auto at = [&](const void *p, int size) { return (uintptr_t)p % std::min(16, vec * size) == 0; };
-    const int half = a.rot_dim / 2;
-    if (a.dim % vec || (a.pairs ? a.rot_dim : half) % vec) return false;
-    // (Half of a pack of angles is the unit in which they are read.)
-    if (a.rot_dim > 0 && (half % (vec / 2) || !((uintptr_t)a.cos % std::min(16, vec / 2 * 4) == 0 && (uintptr_t)a.sin % std::min(16, vec / 2 * 4) == 0)))
-        return false;
-    for (int64_t s : {a.k_row, a.k_head, a.v_row, a.v_head, a.q_row, a.q_head, a.qo_row, a.qo_head, a.kc_page, a.kc_slot, a.kc_head,
-                      a.vc_page, a.vc_slot, a.vc_head})
-        if (s % vec) return false;
-    return at(a.k, sx) && at(a.v, sx) && at(a.q, sx) && at(a.q_out, sx) && at(a.kc, sc) && at(a.vc, sc);
+    const int turns = a.pairs ? a.rot_dim : a.rot_dim / 2, rest = a.dim - a.rot_dim;
+    if ((turns > 0 && turns < VEC) || (rest > 0 && rest < VEC) || a.dim < VEC) return false;
+    return (VEC * element <= 16 && (!a.q || a.q != a.q_out)) || (turns % VEC == 0 && rest % VEC == 0);
 }
 
 template <typename TX, typename TC, int VEC> bool launch_packs(const AppendArgs &a, hipStream_t stream)
 {
-    if (!packs_fit(a, VEC, sizeof(TX), sizeof(TC))) return false;
-    const int units = a.dim / VEC - (a.pairs ? 0 : a.rot_dim / 2 / VEC);
-    const int64_t per = (int64_t)(a.q_heads + a.kv_heads) * units + (int64_t)a.kv_heads * (a.dim / VEC);
+    if (!packs_fit<VEC>(a, sizeof(TX))) return false;
+    const int units = packs<VEC>(a.pairs ? a.rot_dim : a.rot_dim / 2) + packs<VEC>(a.dim - a.rot_dim), vunits = packs<VEC>(a.dim);
+    const int64_t per = (int64_t)(a.q_heads + a.kv_heads) * units + (int64_t)a.kv_heads * vunits;
     const int64_t groups = (per * a.n_tokens + 255) / 256;
-    if (groups > (1 << 24) - 1) return false;
-    hipLaunchKernelGGL((append_packs<TX, TC, VEC>), dim3((unsigned)groups), dim3(256), 0, stream, a);
+    if (groups >= 1 << 23) return false;
+    hipLaunchKernelGGL((append_packs<TX, TC, VEC>), dim3((unsigned)groups), dim3(256), 0, stream, a, Divisor((unsigned)per),
+                       Divisor((unsigned)units), Divisor((unsigned)vunits), Divisor((unsigned)a.page_size));
     return true;
 }
 

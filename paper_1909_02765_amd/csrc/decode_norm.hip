@@ -114,13 +114,6 @@ template <int LANES> __device__ inline float lanes_sum(float v)
     return v;
 }
 
-// N elements from an address that is aligned to one of them: the memory
-// system takes such accesses whole.
-template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Loose {
-    static constexpr int WORDS = sizeof(T) * N / 16;
-    unsigned __attribute__((ext_vector_type(4))) w[WORDS];
-};
-
 // Rows of up to T * E values: T threads hold a row in registers, E values each,
 // in packs of VEC, so each input is read once and each output written once.  T
 // up to 64 leaves a row to part of a wave or a wave (no barrier).  Weights and
@@ -167,7 +160,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
         using TD = std::remove_cv_t<std::remove_reference_t<decltype(*row)>>;
         Pack<TD, VEC> p = {};
         if (row && at(i) < a.width) {
-            if constexpr (LOOSE) p = __builtin_bit_cast(Pack<TD, VEC>, *reinterpret_cast<const Loose<TD, VEC> *>(row + at(i) - skip(i)));
+            if constexpr (LOOSE) p = load_loose<TD, VEC>(row + at(i) - skip(i));
             else p = load_pack<TD, VEC>(row + at(i));
         }
         return p;
@@ -181,7 +174,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
         if constexpr (!LOOSE) {
             store_pack<TD, VEC>(row + at(i), p);
         } else if (skip(i) == 0) {
-            *reinterpret_cast<Loose<TD, VEC> *>(row + at(i)) = __builtin_bit_cast(Loose<TD, VEC>, p);
+            store_loose<TD, VEC>(row + at(i), p);
         } else {
 #pragma unroll
             for (int j = 0; j < VEC; ++j)

@@ -91,6 +91,19 @@ def test_append(x, cache, tokens, seqs, hq, hk, d, rot, page, pairs):
     check_append(c, pairs, f"{x}->{cache} {tokens}x({hq},{hk})x{d} rot {rot} page {page} pairs {pairs}")
 
 
+@pytest.mark.parametrize("x,cache", PAIRS, ids=str)
+@pytest.mark.parametrize("pairs", [False, True])
+def test_append_heads_that_do_not_divide(x, cache, pairs):
+    """What turns, what does not and whole heads of every remainder to a multiple of eight: copied and in place."""
+    g = gen(17)
+    for d, rot in [(d, rot) for d in (8, 9, 15, 21, 36, 75) for rot in range(0, d + 1, 2)]:
+        c = append_case(g, 5, 2, 3, 1, d, rot, x, cache, 16, 2)
+        check_append(c, pairs, f"d {d} rot {rot}")
+        if rot and rot % 6 == 0:
+            q = c["q"].cuda()
+            check_append(c, pairs, f"d {d} rot {rot} in place", cuda=dict(q=q), q_out=q)
+
+
 def test_append_without_queries_and_many_tokens():
     for d, rot in ((128, 128), (64, 32)):
         c = append_case(gen(d), 4000, 3, 2, 2, d, rot, BF16, BF16, 16, 100)
