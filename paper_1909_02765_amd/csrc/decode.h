@@ -79,9 +79,10 @@ constexpr int kMinShare = 4;    // tiles of 16 keys: a workgroup's smallest shar
 constexpr int kWholeTiles = 16; // a unit of so many is not split where the card is not full
 constexpr int kUnitCost = 6;    // what a unit costs beside its tiles, in tiles
 
-// A unit (key head x block of its query heads) that `count` workgroups share.
+// A unit (key head x block of its query heads) that `count` workgroups share,
+// from `first` on; count 0: none.
 struct AttnPart {
-    int seq, unit, count, pad;
+    int seq, unit, first, count;
 };
 
 struct AttnArgs {
@@ -109,10 +110,12 @@ struct AttnArgs {
     int grid;
     bool split;  // the workgroups share all tiles out (else each takes a unit)
     int part_heads;  // heads of a part
-    // The workspace of a split call: for each workgroup the unit that it began
-    // and others went on with; its two parts (the one that goes on with a unit,
-    // the one that begins one), each its sums [part_heads][dim] and its maximum
-    // and sum [part_heads][2].
+    // The workspace of a split call: the shared units, each at its own place
+    // (part_of_unit) or, where they are more than the workgroups, at the place of the
+    // workgroup that began it; for each workgroup its two parts (the one that goes on
+    // with a unit, the one that begins one), each its sums [part_heads][dim] and
+    // its maximum and sum [part_heads][2].
+    bool part_of_unit;
     AttnPart *parts;
     float *part_o, *part_ml;
 };

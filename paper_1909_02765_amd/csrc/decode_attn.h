@@ -167,6 +167,12 @@ template <typename TC, bool Q16, int DC, Rows R, bool SHORT> struct AttnKernel {
     // Workgroups that a compute unit holds at once (waves of a SIMD): what the
     // registers of two tiles, the queries and the output leave.
     static constexpr int PER_CU = SHORT ? (DC == 64 ? 5 : DC <= 128 ? 3 : 2) : DC == 64 ? (QP == 3 ? 3 : 4) : DC <= 128 ? 2 : 1;
+    // Whether a tile is loaded where there is none (the pool's first row for it).
+    // Loads behind a condition the compiler cannot count, and waits for all of them
+    // before it goes on.  Where one wave has a vector unit for itself that shows (7
+    // f32 heads of 192 over 2 x 57306 keys 131 us, without the condition 105);
+    // where several have, a call of few tiles a wave is 1 us longer without it.
+    static constexpr bool ALWAYS = !SHORT && !C16 && DC >= 192;
     // A tile of 16 keys: lane (n, g) holds pieces g, g + 4, ... of key n's K row,
     // and pieces n, n + 16, ... of the V rows of keys 4g..4g+3.
     struct Tile {
@@ -197,7 +203,7 @@ __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v);
 
 struct FindShare {
     int sum[4], top[4];
-    int seq, tiles, before;
+    int seq, length, before;
 };
 
 // The sum over the workgroup of a value of each thread; *up_to: the sum up to
@@ -221,11 +227,10 @@ __device__ inline int scan256(int v, int *up_to, FindShare &f)
 // Units of a sequence (key heads x blocks of up to 16 of their query heads).
 __device__ inline int units_of(const AttnArgs &a) { return a.kv_heads * a.blocks; }
 
-// The shares of this call, and the sequence in which share `wg` begins, the
-// tiles of its units, and the length of all units before it (0 tiles where the
-// share is beyond the row's end).
+// Where a share begins: in this sequence of this length, with units that take
+// `before` of the row before it.
 struct Begin {
-    int seq, tiles, before;
+    int seq, length, before;
 };
 
 __device__ inline Share share_of(const AttnArgs &a, int total, int top)
@@ -238,13 +243,15 @@ __device__ inline Share share_of(const AttnArgs &a, int total, int top)
     return s;
 }
 
+// The shares of this call, and where share `wg` begins (if it lies in the row).
 __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f, Begin *begin)
 {
     const int tid = threadIdx.x, units = units_of(a);
     *begin = Begin{0, 0, 0};
     if (a.n_seqs <= 64) {  // each wave for itself
         const int lane = tid & 63;
-        const int t = lane < a.n_seqs ? tiles_of(a, a.lengths[lane]) : 0, cost = t > 0 ? t + kUnitCost : 0;
+        const int length = lane < a.n_seqs ? a.lengths[lane] : 0;
+        const int t = lane < a.n_seqs ? tiles_of(a, length) : 0, cost = t > 0 ? t + kUnitCost : 0;
         int top = t, up_to = cost;
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
@@ -260,8 +267,8 @@ __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f, Begi
         const int want = (int)at / units;
         const int seq = __builtin_ctzll(__builtin_amdgcn_ballot_w64(want < up_to));
         begin->seq = seq;
-        begin->tiles = __builtin_amdgcn_readlane(t, seq);
-        begin->before = (__builtin_amdgcn_readlane(up_to, seq) - begin->tiles - kUnitCost) * units;
+        begin->length = __builtin_amdgcn_readlane(length, seq);
+        begin->before = __builtin_amdgcn_readlane(up_to - cost, seq) * units;
         return s;
     }
     int mine = 0, top = 0, up_to;
@@ -280,19 +287,20 @@ __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f, Begi
     const int want = (int)at / units;
     int carry = 0;
     for (int i0 = 0; i0 < a.n_seqs && want >= carry; i0 += 256) {
-        const int t = i0 + tid < a.n_seqs ? tiles_of(a, a.lengths[i0 + tid]) + kUnitCost : 0;
+        const int length = i0 + tid < a.n_seqs ? a.lengths[i0 + tid] : 0;
+        const int t = i0 + tid < a.n_seqs ? tiles_of(a, length) + kUnitCost : 0;
         // (Up to 256 sequences the sums are there.)
         const int sum = a.n_seqs <= 256 ? total : scan256(t, &up_to, f);
         const int to = carry + up_to;
         if (want >= to - t && want < to) {
             f.seq = i0 + tid;
-            f.tiles = t - kUnitCost;
+            f.length = length;
             f.before = (to - t) * units;
         }
         carry += sum;
     }
     __syncthreads();
-    *begin = Begin{uniform(f.seq), uniform(f.tiles), uniform(f.before)};
+    *begin = Begin{uniform(f.seq), uniform(f.length), uniform(f.before)};
     return s;
 }
 
@@ -431,14 +439,15 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
     auto load = [&](int j, Tile &t) {
         const Places &p = lds.places[wave][(j >> 2) & 1];
         const int i0 = (j & 3) * 16;
-        const TC *krow = kh + max(p.k[i0 + n16], (int64_t)0);
+        const bool real = !Cfg::ALWAYS || j < tiles;
+        const TC *krow = kh + (real ? max(p.k[i0 + n16], (int64_t)0) : 0);
 #pragma unroll
         for (int c = 0; c < NK; ++c) t.k[c] = load_row<TC, KV, R, true>(krow, (g + 4 * c) * KV, a.dim);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int64_t vo = p.v[i0 + 4 * g + r];
             t.seen[r] = vo >= 0;
-            const TC *vrow = vh + max(vo, (int64_t)0);
+            const TC *vrow = vh + (real ? max(vo, (int64_t)0) : 0);
 #pragma unroll
             for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
                 t.v[r][c] = load_row<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R, false>(vrow, (n16 + 16 * c) * VV, a.dim);
@@ -591,9 +600,9 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
                 place(j / 4 + 1, next);
                 if (j + 6 < tiles) next = look_up(j / 4 + 2);
             }
-            if (j + 1 < tiles) load(j + 1, buf[1]);
+            if (Cfg::ALWAYS || j + 1 < tiles) load(j + 1, buf[1]);
             compute(buf[0]);
-            if (j + 2 < tiles) load(j + 2, buf[0]);
+            if (Cfg::ALWAYS || j + 2 < tiles) load(j + 2, buf[0]);
             if (j + 1 < tiles) compute(buf[1]);
         }
     }
@@ -640,21 +649,24 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
     if constexpr (!SHORT)
         if (a.split) share = find_share(a, wg, lds.found, &begin);
 
-    // This workgroup's place: a unit, its tiles, and how far into its length the share has come.
-    int seq, unit, tiles_all, x0 = 0;
+    // This workgroup's place: a sequence, its length and its units' tiles, a unit
+    // of it, and how far into the unit's length the share has come.
+    int seq, length, unit, tiles_all, x0 = 0;
     int at = 0, last = 0;
-    if (a.split && threadIdx.x == 0) a.parts[wg] = AttnPart{-1, 0, 0, 0};  // (whatever follows, attn_join reads it)
+    if (a.split && !a.part_of_unit && threadIdx.x == 0) a.parts[wg] = AttnPart{0, 0, 0, 0};  // (whatever follows, attn_join reads it)
     if (share.whole) {
         if (wg >= a.n_seqs * units) return;
         seq = wg / units;
         unit = wg - seq * units;
-        tiles_all = tiles_of(a, uniform(a.lengths[seq]));
+        length = uniform(a.lengths[seq]);
+        tiles_all = tiles_of(a, length);
     } else {
         if ((int64_t)wg * share.size >= share.total) return;
         at = wg * share.size;
         last = (int)min((int64_t)at + share.size, (int64_t)share.total);
         seq = begin.seq;
-        tiles_all = begin.tiles;
+        length = begin.length;
+        tiles_all = tiles_of(a, length);
         const int in = at - begin.before;
         unit = in / (tiles_all + kUnitCost);
         x0 = in - unit * (tiles_all + kUnitCost);
@@ -669,45 +681,72 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
         seg.kvh = unit / a.blocks;
         seg.hb = unit - seg.kvh * a.blocks;
         int first, end;
-        visible_range(a, uniform(a.lengths[seq]), &first, &end);
+        visible_range(a, length, &first, &end);
         seg.k0 = first + tile0 * 16;
         seg.k1 = (int)min((int64_t)end, (int64_t)seg.k0 + (int64_t)seg_tiles * 16);
+        const bool all = seg_tiles == tiles_all;  // of the unit's tiles
         attn_segment<TC, Q16, DC, R, SHORT>(a, seg, lds);
         __syncthreads();
 
-        // Join the four waves; each writes a head at a time.
-        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-        const bool all = seg_tiles == tiles_all;  // of the unit's tiles
+        // Join the four waves, four values of a head at a time.
+        const int heads = min(kAttnHeads, a.group - seg.hb * kAttnHeads), head0 = seg.kvh * a.group + seg.hb * kAttnHeads;
         // The part that begins a unit, or the one that goes on with it.
         const int64_t part = ((int64_t)wg * 2 + (tile0 == 0 ? 1 : 0)) * a.part_heads;
-        const int heads = min(kAttnHeads, a.group - seg.hb * kAttnHeads), head0 = seg.kvh * a.group + seg.hb * kAttnHeads;
-        for (int h = wave; h < heads; h += 4) {
-            float top = lds.m[0][h], sum = 0.f, f[4];
-#pragma unroll
-            for (int w = 1; w < 4; ++w) top = fmaxf(top, lds.m[w][h]);
-            const float base = top == -INFINITY ? 0.f : top;
+        constexpr int PER = DC / 4;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < heads * PER; i += 256) {
+            const int h = i / PER, d = (i - h * PER) * 4;
+            if (d >= a.dim) continue;
+            floatx4 o[4];
+            float m[4], l[4];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                f[w] = __builtin_amdgcn_exp2f(lds.m[w][h] - base);
-                sum += lds.l[w][h] * f[w];
+                o[w] = *reinterpret_cast<const floatx4 *>(&lds.o[w][h][d]);
+                m[w] = lds.m[w][h];
+                l[w] = lds.l[w][h];
             }
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            TQ *out = (TQ *)a.out + (int64_t)seq * a.o_row + (int64_t)(head0 + h) * a.o_head;
-            float *po = a.part_o + (part + h) * a.dim;
+            const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int d = lane; d < (DC + 63) / 64 * 64; d += 64) {
-                if (d >= a.dim) continue;
-                const float v = (lds.o[0][h][d] * f[0] + lds.o[1][h][d] * f[1]) + (lds.o[2][h][d] * f[2] + lds.o[3][h][d] * f[3]);
-                if (all) out[d] = (TQ)(v * inv);
-                else po[d] = v;
+            for (int w = 0; w < 4; ++w) {
+                const float f = __builtin_amdgcn_exp2f(m[w] - base);
+                o[w] *= f;
+                l[w] *= f;
             }
-            if (lane == 0 && all && a.lse)
-                a.lse[(int64_t)seq * a.q_heads + head0 + h] =
-                    sum == 0.f ? -INFINITY : (top + (__builtin_amdgcn_logf(sum) - (float)Cfg::SHIFT)) * kLn2;
-            if (lane == 0 && !all) {
-                a.part_ml[(part + h) * 2] = top - (float)Cfg::SHIFT;
-                a.part_ml[(part + h) * 2 + 1] = sum;
+            const float sum = (l[0] + l[1]) + (l[2] + l[3]);
+            floatx4 v = (o[0] + o[1]) + (o[2] + o[3]);
+            auto put = [&](auto *to) {
+                using TO = std::remove_reference_t<decltype(*to)>;
+                Pack<TO, 4> p;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) p.v[k] = (TO)v[k];
+                if (d + 4 <= a.dim) {
+                    store_loose<TO, 4>(to + d, p);
+                    return;
+                }
+                to[d] = p.v[0];
+                if (d + 1 < a.dim) to[d + 1] = p.v[1];
+                if (d + 2 < a.dim) to[d + 2] = p.v[2];
+            };
+            if (all) {
+                v *= sum == 0.f ? 0.f : 1.f / sum;
+                put((TQ *)a.out + (int64_t)seq * a.o_row + (int64_t)(head0 + h) * a.o_head);
+                if (d == 0 && a.lse)
+                    a.lse[(int64_t)seq * a.q_heads + head0 + h] =
+                        sum == 0.f ? -INFINITY : (top + (__builtin_amdgcn_logf(sum) - (float)Cfg::SHIFT)) * kLn2;
+            } else {
+                put(a.part_o + (part + h) * a.dim);
+                if (d == 0) {
+                    a.part_ml[(part + h) * 2] = top - (float)Cfg::SHIFT;
+                    a.part_ml[(part + h) * 2 + 1] = sum;
+                }
             }
+        }
+        // Who begins a unit says whether others go on with it.
+        if (a.split && threadIdx.x == 0 && tile0 == 0) {
+            const int rest = tiles_all - seg_tiles;
+            const int count = all ? 0 : 1 + (int)(((unsigned)rest + share.size - 1) / (unsigned)share.size);
+            if (a.part_of_unit) a.parts[seq * units + unit] = AttnPart{seq, unit, wg, count};
+            else if (!all) a.parts[wg] = AttnPart{seq, unit, wg, count};
         }
         if (share.whole) {
             // (Long before 2^31: units are at most 2^24, workgroups too.)
@@ -715,14 +754,10 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
             if (!a.split || u >= a.n_seqs * units) return;
             seq = u / units;
             unit = u - seq * units;
-            tiles_all = tiles_of(a, uniform(a.lengths[seq]));
+            length = uniform(a.lengths[seq]);
+            tiles_all = tiles_of(a, length);
             __syncthreads();  // the LDS that the next unit's waves write has been read
             continue;
-        }
-        // Who begins a unit that others go on with says so.
-        if (threadIdx.x == 0 && !all && tile0 == 0) {
-            const int rest = tiles_all - seg_tiles;
-            a.parts[wg] = AttnPart{seq, unit, 1 + (int)(((unsigned)rest + share.size - 1) / (unsigned)share.size), 0};
         }
         at += x1 - x0;
         if (at >= last) return;
@@ -730,7 +765,8 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
         x0 = 0;
         if (++unit == units) {
             unit = 0;
-            tiles_all = tiles_of(a, uniform(a.lengths[++seq]));
+            length = uniform(a.lengths[++seq]);
+            tiles_all = tiles_of(a, length);
         }
     }
 }
