@@ -284,6 +284,17 @@ def test_attention_without_a_key_anywhere():
     assert (out == 0).all() and (lse == -math.inf).all()
 
 
+@pytest.mark.parametrize("seqs,hq,hk,d", [(600, 4, 2, 64), (70, 17, 1, 72), (90, 5, 5, 33), (1300, 1, 1, 64)])
+def test_attention_of_many_sequences(seqs, hq, hk, d):
+    """More units than workgroups and fewer, some of which begin in one workgroup and end in another."""
+    g = gen(seqs)
+    lengths = torch.randint(0, 300, (seqs,), generator=g).tolist()
+    lengths[seqs // 2], lengths[-1] = 3001, 1777
+    c = attn_case(g, lengths, hq, hk, d, F32, BF16, 64)
+    check_attn(c, f"{seqs} sequences")
+    check_attn(c, f"{seqs} sequences, window", window=290)
+
+
 def test_attention_length_beyond_the_table():
     c = attn_case(gen(4), [48, 48], 4, 2, 64, BF16, BF16, 16)
     c["lengths"] = torch.tensor([1000, 2 ** 31 - 1], dtype=torch.int32)
