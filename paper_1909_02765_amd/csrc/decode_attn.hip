@@ -123,7 +123,11 @@ size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
     const int card = cache_dtype == ILPM_F32   ? attn_card_f32(a->dim)
                      : cache_dtype == ILPM_F16 ? (q32 ? attn_card_f16_q32(a->dim) : attn_card_f16(a->dim))
                                                : (q32 ? attn_card_bf16_q32(a->dim) : attn_card_bf16(a->dim));
-    a->grid = (int)std::min<int64_t>({card, kMaxParts, units * ((tiles + kUnitCost + kMinShare - 1) / kMinShare)});
+    // (Shares of few tiles are better off larger: 8 key heads of 2445 x 10 f16 keys of
+    // 80 15.2 us on 768 workgroups, 14.3 on 512.)
+    int grid = card;
+    while (grid > 2 * kAttnCus && units * tiles < 18 * (int64_t)grid) grid -= kAttnCus;
+    a->grid = (int)std::min<int64_t>({grid, kMaxParts, units * ((tiles + kUnitCost + kMinShare - 1) / kMinShare)});
     a->part_heads = std::min(a->group, kAttnHeads);
     a->part_of_unit = units <= a->grid;
     return (size_t)a->grid * (sizeof(AttnPart) + 2 * a->part_heads * (size_t)(a->dim + 2) * sizeof(float));
