@@ -127,7 +127,7 @@ template <int LANES> __device__ inline float lanes_sum(float v)
 //
 // Mean and variance come from the values in registers, in two steps, so a mean
 // far from zero costs the variance nothing.  What bounds it: the bytes of x, y,
-// gate, r and z (16381 rows of 4096, f32 over bf16: 201 us, 5.3 TB/s).  Of 16-bit
+// gate, r and z (16381 rows of 4096, f32 over bf16: 190 us, 5.7 TB/s).  Of 16-bit
 // rows of several thousand values it is the vector unit's work on them and on the
 // sums, which one row a compute unit does not hide (6556 bf16 rows of 6723: 106 us,
 // 3.3 TB/s).
@@ -293,12 +293,19 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
 // As many workgroups as the 256 compute units hold at once, with the same number
 // of rows each, give or take one: more would read the weights again (9116 f32 rows
 // of 1015 23.0 -> 22.2 us).  By their registers that is 16 waves a unit, of 16-bit
-// rows in workgroups of up to four waves 20 (3822 bf16 rows of 1732 14.1 -> 13.2 us).
+// rows in workgroups of up to four waves 20 (3822 bf16 rows of 1732 14.1 -> 13.2
+// us).  Calls whose bytes come from memory and not from the 256 MB cache before it, in
+// rows that fill eight waves, do better with one workgroup a unit (us with two and
+// one: 16000 f32 rows of 4096 over bf16 204 and 186, of 3584 179 and 162, bf16 ones of
+// 4096 128 and 118; but 16000 of 3584 110 and 112, and of 262 MB 8000 of 4096 44 and 48).
 template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOOSE>
 void launch_rows(const NormArgs &a, hipStream_t stream)
 {
     constexpr int block = T <= 64 ? 256 : T, per = T <= 64 ? 256 / T : 1;
-    constexpr int waves = sizeof(TX) == 2 && T <= 256 ? 20 : 16;
+    const int64_t bytes = (int64_t)a.rows * a.width *
+                          (sizeof(TX) * (1 + !!a.r) + sizeof(TY) * (!!a.y + !!a.z) + sizeof(TP) * (a.gate && a.gate_row > 0));
+    const bool alone = T == 512 && a.width >= T * E / 8 * 7 && bytes > 320000000;
+    const int waves = alone ? 8 : sizeof(TX) == 2 && T <= 256 ? 20 : 16;
     const int rows = ceil_div(a.rows, per), turns = ceil_div(rows, 256 * 64 * waves / block);
     const int groups = ceil_div(rows, turns);
     hipLaunchKernelGGL((norm_rows<TX, TY, TP, T, E, VEC, LOOSE>), dim3(groups), dim3(block), 0, stream, a);
