@@ -509,6 +509,19 @@ def test_norm_in_place_over_many_rows(rows, width):
         check_norm(c, f"{types} {rows}x{width}", cuda=dict(x=x, r=x, y=y, z=y))
 
 
+def test_norm_of_rows_that_come_from_memory():
+    """So many bytes that workgroups are launched by another rule: the rows are those of calls of a few of them."""
+    ilpm = lib()
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, y = (torch.randn((11000, 4088), generator=g, device="cuda").to(BF16) for _ in range(2))
+    w = torch.randn(4088, generator=g, device="cuda").to(BF16)
+    r, z = ilpm.residual_norm(x, y, post="rms", pre="layer", post_w=w, pre_b=w)
+    for i in (0, 511, 5300, 10990):
+        some_r, some_z = ilpm.residual_norm(x[i:i + 10], y[i:i + 10], post="rms", pre="layer", post_w=w, pre_b=w)
+        assert torch.equal(r[i:i + 10], some_r) and torch.equal(z[i:i + 10], some_z)
+    assert torch.isfinite(r).all() and torch.isfinite(z).all()
+
+
 def test_norm_strided():
     g = gen(14)
     for width, shift in ((512, 0), (512, 8), (512, 1), (1000, 0), (77, 3)):
