@@ -503,7 +503,7 @@ typedef struct ilpm_attn_options {
     int mask_len;
     int window;          /* > 0: only the last `window` tokens are seen; 0: all */
     int max_len;         /* no sequence is longer, as far as the caller knows; 0: unknown.  Only the
-                            split over the length goes by it, the result does not depend on it */
+                            split over the length goes by it, the result only in its rounding */
 } ilpm_attn_options;
 
 /*
@@ -520,8 +520,8 @@ typedef struct ilpm_attn_options {
  *        as 0 below 0, and as the table's end beyond it
  *   out  as q (may be q itself);  lse  fp32 [n_seqs][q_heads] contiguous, or NULL
  * head_dim is at most 256 (ILPM_ERR_UNSUPPORTED above).
- * Long sequences are split over their length into chunks whose partial
- * results are joined in their order, in a workspace of
+ * Long sequences are split over their length into parts whose results are
+ * joined in their order, in a workspace of
  * ilpm_attn_decode_workspace_size bytes: `workspace` (256-byte aligned; its
  * contents do not matter) if it is not NULL, else the one of the split plans (see
  * ilpm_conv2d_fwd), whose rules then hold.  Calls with workspaces of their own

@@ -30,7 +30,12 @@
 // card holds at once (see Share).  A workgroup takes its share unit by unit; a
 // unit that spans workgroups leaves partial results, which attn_join adds.
 //
-// What bounds it: the cache's bytes.
+// What bounds it: the cache's bytes (131071 keys of 8 bf16 heads of 128 under 32
+// query heads 106 us, 64 ragged sequences of up to 8191 of them 211 us, 5.0 TB/s
+// with the join); of single heads with window, mask and soft cap the vector unit
+// (24 sequences of 12 f16 heads of 80, window 1000: 27 us, 2.6 TB/s); of calls with a tile or
+// two a wave the accesses that wait for each other (lengths, pages, rows, the
+// join: f32 queries over 16 shared bf16 heads of 256, 8 sequences of up to 2049, 15 us).
 #pragma once
 
 #include <climits>
@@ -643,7 +648,8 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
 
     // Workgroups go round the card's eight dies, each with a cache of its own.
     // Neighbouring shares, which often hold neighbouring heads of the same
-    // tokens, stay on one die, so that a line of two heads' rows is fetched once.
+    // tokens, stay on one die, so that a line of two heads' rows is fetched once
+    // (131071 keys of 8 bf16 heads of 128 111 -> 108 us).
     const int die = blockIdx.x & 7, dies = gridDim.x >> 3;
     const int units = units_of(a), wg = die * dies + min(die, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
     Share share = {0, 0, true};
