@@ -76,7 +76,7 @@ hipError_t append_launch(const AppendArgs &a, int x_dtype, int cache_dtype, hipS
 constexpr int kAttnHeads = 16;  // query heads of a workgroup
 constexpr int kAttnCus = 256;   // compute units of the card
 constexpr int kMinShare = 4;    // tiles of 16 keys: a workgroup's smallest share (a tile a wave)
-constexpr int kWholeTiles = 16; // a unit of so many is not split where the card is not full
+constexpr int kWholeTiles = 16; // units of so many are never split (see attn_plan)
 constexpr int kUnitCost = 6;    // what a unit costs beside its tiles, in tiles
 
 // A unit (key head x block of its query heads) that `count` workgroups share,

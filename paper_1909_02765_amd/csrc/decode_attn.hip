@@ -105,9 +105,13 @@ template <int V> __global__ __launch_bounds__(256) void attn_join(AttnArgs a)
 
 }  // namespace
 
-// Sequences that cannot have more than kWholeTiles tiles go a unit to a
-// workgroup; else as many workgroups share all tiles as the card holds, or as
-// there are smallest shares.
+// Either a unit goes to a workgroup, or as many workgroups as the card holds (or
+// as there are smallest shares) share all tiles.  The first takes about 5 us and
+// `round` for every four tiles of the longest sequence; the second 12 us for its
+// two kernels and one more for every 36 units (fitted to 64 calls of 17 to 64 tiles
+// and 60 to 1425 units: 1386 units of 48 tiles, f16 heads of 80, 114 us shared and
+// 66 by units; 65 such units under f32 queries 15 and 20).  Beyond 64 tiles units
+// differ too much in length (207 of up to 321 tiles 56 us shared and 134 by units).
 size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
 {
     a->blocks = ceil_div(a->group, kAttnHeads);
@@ -115,7 +119,9 @@ size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
     const int64_t keys = a->window > 0 ? std::min(max_len, a->window) : max_len, tiles = std::max<int64_t>(1, (keys + 15) / 16);
     // (Tiles are counted in 32 bits.  Where a table could name more, there are units enough without a split.)
     const int64_t most = (((int64_t)a->capacity + 15) / 16 + kUnitCost) * units;
-    a->split = tiles > kWholeTiles && units > 0 && (most < INT_MAX || units == 1);
+    const double round = cache_dtype == ILPM_F32 ? 0.2 + a->dim / 55. : 0.7 + a->dim / 250. + (q32 ? 0.35 : 0.);
+    const bool by_units = tiles <= kWholeTiles || (tiles <= 4 * kWholeTiles && 5. + (double)tiles / 4. * round <= 12. + (double)units / 36.);
+    a->split = !by_units && units > 0 && (most < INT_MAX || units == 1);
     if (!a->split) {
         a->grid = (int)units;
         return 0;
