@@ -111,7 +111,8 @@ template <int V> __global__ __launch_bounds__(256) void attn_join(AttnArgs a)
 // two kernels and one more for every 36 units (fitted to 64 calls of 17 to 64 tiles
 // and 60 to 1425 units: 1386 units of 48 tiles, f16 heads of 80, 114 us shared and
 // 66 by units; 65 such units under f32 queries 15 and 20).  Beyond 64 tiles units
-// differ too much in length (207 of up to 321 tiles 56 us shared and 134 by units).
+// differ too much in length (207 of up to 321 tiles 56 us shared and 134 by units),
+// and fewer than 60 would leave most of the card idle.
 size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
 {
     a->blocks = ceil_div(a->group, kAttnHeads);
@@ -120,7 +121,7 @@ size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
     // (Tiles are counted in 32 bits.  Where a table could name more, there are units enough without a split.)
     const int64_t most = (((int64_t)a->capacity + 15) / 16 + kUnitCost) * units;
     const double round = cache_dtype == ILPM_F32 ? 0.2 + a->dim / 55. : 0.7 + a->dim / 250. + (q32 ? 0.35 : 0.);
-    const bool by_units = tiles <= kWholeTiles || (tiles <= 4 * kWholeTiles && 5. + (double)tiles / 4. * round <= 12. + (double)units / 36.);
+    const bool by_units = tiles <= kWholeTiles || (tiles <= 4 * kWholeTiles && units >= 60 && 5. + (double)tiles / 4. * round <= 12. + (double)units / 36.);
     a->split = !by_units && units > 0 && (most < INT_MAX || units == 1);
     if (!a->split) {
         a->grid = (int)units;
