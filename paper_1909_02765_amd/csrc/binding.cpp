@@ -6,7 +6,7 @@
 // all arguments by position, from the wrappers in __init__.py, and return what
 // those return, or the negative status of the C call.
 #include <ATen/ATen.h>
-#include <ATen/EmptyTensor.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -138,8 +138,7 @@ ilpm_kv_cache cache_of(PyObject *k_pages, PyObject *v_pages, PyObject *page_tabl
 // dispatch a tensor costs 0.35 us more.)
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType type)
 {
-    static c10::Allocator *allocator = c10::GetAllocator(c10::DeviceType::CUDA);
-    return at::detail::empty_generic(shape, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
+    return at::Tensor(at::detail::empty_cuda(shape, type, c10::Device(c10::DeviceType::CUDA, c10::hip::current_device()), std::nullopt));
 }
 
 hipStream_t current_stream() { return c10::hip::getCurrentHIPStream().stream(); }
