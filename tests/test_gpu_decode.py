@@ -569,6 +569,27 @@ def test_norm_of_rows_that_are_not_finite():
         assert torch.isfinite(z[0]).all() and torch.isfinite(z[3]).all()
 
 
+def test_outputs_are_ordinary_tensors():
+    ilpm = lib()
+    x = torch.randn((4, 64), device="cuda")
+    for mode in (torch.enable_grad, torch.no_grad, torch.inference_mode):
+        with mode():
+            r, z = ilpm.residual_norm(x, x.half(), post="rms")
+            for t, dtype in ((r, F32), (z, F16)):
+                assert t.device == x.device and t.dtype == dtype and t.is_contiguous() and not t.requires_grad
+                assert t.untyped_storage().device == x.device and t.is_inference() == (mode is torch.inference_mode)
+                assert torch.equal(t.clone(), t) and torch.isfinite(t * 2).all()
+    w = torch.ones(64, device="cuda", requires_grad=True)
+    (ilpm.residual_norm(x, x)[0] * w).sum().backward()
+    assert torch.isfinite(w.grad).all()
+    del r, z, t
+    held = torch.cuda.memory_allocated()
+    r, z = ilpm.residual_norm(x, x)
+    assert torch.cuda.memory_allocated() == held + 2 * 4 * 64 * 4
+    del r, z
+    assert torch.cuda.memory_allocated() == held
+
+
 def test_norm_nothing():
     r, z = lib().residual_norm(torch.empty((0, 64), device="cuda"), torch.empty((0, 64), device="cuda"))
     assert r.shape == z.shape == (0, 64)
