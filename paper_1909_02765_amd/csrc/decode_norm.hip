@@ -116,9 +116,10 @@ template <int LANES> __device__ inline float lanes_sum(float v)
 
 // Rows of up to T * E values: T threads hold a row in registers, E values each,
 // in packs of VEC, so each input is read once and each output written once.  T
-// up to 64 leaves a row to part of a wave or a wave (no barrier).  Weights and
-// biases stay in registers over the rows that a workgroup takes, and a row is
-// read while the one before it is worked on (7512 f32 rows of 2247 59 -> 47 us).
+// is 16 or 64, part of a wave or a wave (no barrier), or 1024: of these a
+// workgroup has as many waves as the row fills.  Weights and biases stay in
+// registers over the rows that a workgroup takes, and a row is read while the one
+// before it is worked on (7512 f32 rows of 2247 59 -> 47 us).
 //
 // LOOSE: rows of any alignment and of any width from VEC on.  The last pack then
 // ends with the row, over some values of the pack before it: these count in no
@@ -135,10 +136,11 @@ template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOO
 __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
 {
     constexpr int NV = E / VEC, ROWS = T <= 64 ? 256 / T : 1, WAVES = T > 64 ? T / 64 : 1;
+    const int threads = T <= 64 ? T : (int)blockDim.x;  // of a row
     // Beyond, neither weights nor a second row fit beside the row: read for each, when it comes.
     constexpr bool HOLD = T * E <= 8192;
     __shared__ float lds[WAVES > 1 ? 2 * WAVES : 1];
-    const int tid = threadIdx.x % T;
+    const int tid = T <= 64 ? threadIdx.x % T : threadIdx.x;
     const float inv_n = 1.f / (float)a.width;
     int turn = 0;
     auto total = [&](float v) {
@@ -149,12 +151,13 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
             turn ^= 1;
             if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
             __syncthreads();
-            v = lanes_sum<WAVES>(part[threadIdx.x % WAVES]);
+            const int wave = threadIdx.x % WAVES;
+            v = lanes_sum<WAVES>(wave * 64 < threads ? part[wave] : 0.f);
         }
         return v;
     };
     // Pack i of this thread begins at `at`; its first `skip` values are another's.
-    auto at = [&](int i) { return (tid + i * T) * VEC; };
+    auto at = [&](int i) { return (tid + i * threads) * VEC; };
     auto skip = [&](int i) { return LOOSE ? max(0, at(i) + VEC - a.width) : 0; };
     auto get = [&](const auto *row, int i) {
         using TD = std::remove_cv_t<std::remove_reference_t<decltype(*row)>>;
@@ -250,7 +253,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
         for (int i = 0; i < NV; ++i) t.gate[i] = get(grow, i);
     };
     Row next;
-    int64_t row = (int64_t)blockIdx.x * ROWS + (T < 64 ? (int)threadIdx.x / T : __builtin_amdgcn_readfirstlane((int)threadIdx.x / T));
+    int64_t row = (int64_t)blockIdx.x * ROWS + (T < 64 ? (int)threadIdx.x / T : T == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0);
     if (HOLD && row < a.rows) load(next, row);
     for (; row < a.rows; row += step) {
         float v[NV][VEC], u[NV][VEC];
@@ -294,19 +297,25 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
 // of rows each, give or take one: more would read the weights again (9116 f32 rows
 // of 1015 23.0 -> 22.2 us).  By their registers that is 16 waves a unit, of 16-bit
 // rows in workgroups of up to four waves 20 (3822 bf16 rows of 1732 14.1 -> 13.2
-// us).  Calls whose bytes come from memory and not from the 256 MB cache before it, in
-// rows that fill eight waves, do better with one workgroup a unit (us with two and
-// one: 16000 f32 rows of 4096 over bf16 204 and 186, of 3584 179 and 162, bf16 ones of
-// 4096 128 and 118; but 16000 of 3584 110 and 112, and of 262 MB 8000 of 4096 44 and 48).
+// us).  Of f32 rows more of them at once than the next power of two would hold
+// are slower (8000 f32 rows of 2052 over bf16: two workgroups of five waves a unit
+// 57 us, three 65; bf16 rows 55 and 42).  Calls whose bytes come from memory and not
+// from the 256 MB cache before it, in rows that fill eight waves, do better with one
+// workgroup a unit (us with two and one: 16000 f32 rows of 4096 over bf16 204 and 186,
+// of 3584 179 and 162, bf16 ones of 4096 128 and 118; but 16000 of 3584 110 and
+// 112, of 262 MB 8000 of 4096 44 and 48, and 14016 f16 ones of 3651, which are LOOSE, 92
+// and 97).
 template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOOSE>
 void launch_rows(const NormArgs &a, hipStream_t stream)
 {
-    constexpr int block = T <= 64 ? 256 : T, per = T <= 64 ? 256 / T : 1;
+    constexpr int per = T <= 64 ? 256 / T : 1;
+    const int block = T <= 64 ? 256 : ceil_div(a.width, E * 64) * 64, waves = block / 64;
     const int64_t bytes = (int64_t)a.rows * a.width *
                           (sizeof(TX) * (1 + !!a.r) + sizeof(TY) * (!!a.y + !!a.z) + sizeof(TP) * (a.gate && a.gate_row > 0));
-    const bool alone = T == 512 && a.width >= T * E / 8 * 7 && bytes > 320000000;
-    const int waves = alone ? 8 : sizeof(TX) == 2 && T <= 256 ? 20 : 16;
-    const int rows = ceil_div(a.rows, per), turns = ceil_div(rows, 256 * 64 * waves / block);
+    const bool alone = !LOOSE && a.width >= 3584 && a.width <= 4096 && bytes > 320000000;
+    const int full = waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : waves <= 8 ? 8 : 16;
+    const int per_cu = alone ? 1 : sizeof(TX) == 2 ? (waves <= 4 ? 20 : 16) / waves : 16 / full;
+    const int rows = ceil_div(a.rows, per), turns = ceil_div(rows, 256 * per_cu);
     const int groups = ceil_div(rows, turns);
     hipLaunchKernelGGL((norm_rows<TX, TY, TP, T, E, VEC, LOOSE>), dim3(groups), dim3(block), 0, stream, a);
 }
@@ -320,9 +329,6 @@ template <typename TX, typename TY, typename TP, int VEC, bool LOOSE> bool launc
     if (a.width < VEC) return false;
     if (a.width <= 128) launch_rows<TX, TY, TP, 16, 8, VEC, LOOSE>(a, stream);
     else if (a.width <= 512) launch_rows<TX, TY, TP, 64, 8, VEC, LOOSE>(a, stream);
-    else if (a.width <= 1024) launch_rows<TX, TY, TP, 128, 8, VEC, LOOSE>(a, stream);
-    else if (a.width <= 2048) launch_rows<TX, TY, TP, 256, 8, VEC, LOOSE>(a, stream);
-    else if (a.width <= 4096) launch_rows<TX, TY, TP, 512, 8, VEC, LOOSE>(a, stream);
     else if (a.width <= 8192) launch_rows<TX, TY, TP, 1024, 8, VEC, LOOSE>(a, stream);
     else if (!LOOSE && a.width <= 16384) launch_rows<TX, TY, TP, 1024, 16, VEC, false>(a, stream);
     else return false;
