@@ -95,13 +95,13 @@ template <int CTRL> __device__ inline float plus_permuted(float v)
     return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 
-// The sum over groups of LANES (2, 4, 8, 16 or 64) lanes.
+// The sum over groups of LANES (16 or 64) lanes.
 template <int LANES> __device__ inline float lanes_sum(float v)
 {
     v = plus_permuted<0xB1>(v);   // lanes 1 0 3 2 of each four
-    if constexpr (LANES > 2) v = plus_permuted<0x4E>(v);  // lanes 2 3 0 1 of each four
-    if constexpr (LANES > 4) v = plus_permuted<0x141>(v);  // the other four of eight
-    if constexpr (LANES > 8) v = plus_permuted<0x140>(v);  // the other eight of sixteen
+    v = plus_permuted<0x4E>(v);   // lanes 2 3 0 1 of each four
+    v = plus_permuted<0x141>(v);  // the other four of eight
+    v = plus_permuted<0x140>(v);  // the other eight of sixteen
     if constexpr (LANES == 64) {
         unsigned x = __builtin_bit_cast(unsigned, v);
         const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
