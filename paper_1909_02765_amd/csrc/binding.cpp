@@ -230,8 +230,11 @@ PyObject *attn_decode(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     int rc = ilpm_attn_decode_workspace_size(&c, hq.heads, o.window, o.max_len, &need);
     if (rc != ILPM_OK) return PyLong_FromLong(rc);
     at::Tensor ws;
-    if (given(args[13])) ws = tensor(args[13], "workspace");
-    else if (need > 0) ws = empty({(int64_t)need}, at::kByte);
+    if (given(args[13])) {
+        ws = tensor(args[13], "workspace");
+        // (Of a view the bytes between its elements are not the caller's to give, nor are there nbytes() behind an expanded one.)
+        if (!ws.is_contiguous()) value_error("workspace must be contiguous");
+    } else if (need > 0) ws = empty({(int64_t)need}, at::kByte);
     rc = ilpm_attn_decode(&c, &hq, lengths_p, &o, &ho, lse.defined() ? (float *)floats_of(lse, "lse") : nullptr,
                           ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.nbytes() : 0, current_stream());
     if (rc != ILPM_OK) return PyLong_FromLong(rc);

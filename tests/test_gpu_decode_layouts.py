@@ -1,0 +1,34 @@
+"""GPU: workspaces whose elements do not lie together are refused before anything is launched."""
+import pytest
+import torch
+
+from gpu_common import note, torch_cuda
+
+pytestmark = pytest.mark.gpu
+
+
+def test_attention_refuses_a_workspace_that_is_not_contiguous():
+    """Rows of a wider buffer, every other byte, and one byte named many times: each has the bytes by its count of
+    elements, and a write of so many from its first one on would reach what is not its own."""
+    torch_cuda()
+    import paper_1909_02765_amd as ilpm
+    bf16 = dict(dtype=torch.bfloat16, device="cuda")
+    kp, vp = torch.zeros((100, 16, 2, 128), **bf16), torch.zeros((100, 16, 2, 128), **bf16)
+    table = torch.arange(100, dtype=torch.int32, device="cuda").view(1, 100)
+    q, lengths = torch.zeros((1, 8, 128), **bf16), torch.tensor([1500], dtype=torch.int32, device="cuda")
+    need = ilpm.attn_decode_workspace_size(kp, vp, table, 8)
+    assert need > 0
+    rows = -(-need // 256)
+    wide = torch.full((rows, 1024), 7, dtype=torch.uint8, device="cuda")
+    strided = torch.full((2 * need,), 7, dtype=torch.uint8, device="cuda")
+    for what, ws in (("rows", wide[:, :256]), ("every other byte", strided[::2]),
+                     ("expanded", torch.zeros(1, dtype=torch.uint8, device="cuda").expand(need))):
+        assert ws.nbytes >= need
+        note(f"[attn] workspace: {what}")
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            ilpm.attn_decode(q, kp, vp, table, lengths, workspace=ws)
+    torch.cuda.synchronize()
+    assert (wide == 7).all() and (strided == 7).all()
+    out = ilpm.attn_decode(q, kp, vp, table, lengths, workspace=wide.view(-1)[:need])
+    torch.cuda.synchronize()
+    assert (out == 0).all()
