@@ -231,11 +231,13 @@ def workspace_size(c_in, h, w, c_out, k, stride=1, pad=0) -> int:
 
 
 def set_workspace(buf=None, stream=None):
-    """Register a caller-owned device buffer (a CUDA tensor, 256-byte aligned) as
-    the current device's workspace, or unregister it with None."""
+    """Register a caller-owned device buffer (a contiguous CUDA tensor, 256-byte aligned)
+    as the current device's workspace, or unregister it with None."""
     if buf is None:
         _check(lib.ilpm_set_workspace(None, 0, _stream_handle(stream)), "ilpm_set_workspace")
         return
+    if not isinstance(buf, torch.Tensor) or not buf.is_cuda or not buf.is_contiguous():
+        raise TypeError("buf must be a contiguous CUDA tensor")
     nbytes = buf.numel() * buf.element_size()
     _check(lib.ilpm_set_workspace(ctypes.c_void_p(buf.data_ptr()), nbytes, _stream_handle(stream)),
            "ilpm_set_workspace")

@@ -32,3 +32,17 @@ def test_attention_refuses_a_workspace_that_is_not_contiguous():
     out = ilpm.attn_decode(q, kp, vp, table, lengths, workspace=wide.view(-1)[:need])
     torch.cuda.synchronize()
     assert (out == 0).all()
+
+
+def test_set_workspace_refuses_what_is_not_contiguous():
+    """The library's workspace, which convolutions and attention without one of their own write to."""
+    torch_cuda()
+    import paper_1909_02765_amd as ilpm
+    wide = torch.zeros((256, 1024), dtype=torch.uint8, device="cuda")
+    try:
+        for buf in (wide[:, :256], wide[:1, :1].expand(256, 256), wide.t()):
+            with pytest.raises(TypeError, match="contiguous"):
+                ilpm.set_workspace(buf)
+        ilpm.set_workspace(wide)
+    finally:
+        ilpm.set_workspace(None)
