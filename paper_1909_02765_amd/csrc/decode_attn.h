@@ -168,8 +168,10 @@ template <typename TC, bool Q16, int DC, Rows R, bool SHORT> struct AttnKernel {
     static constexpr int DO = NO * 16;                       // values that they hold
     static constexpr int QP = C16 && !Q16 ? 3 : 1;           // parts of a query
     static constexpr int PP = __is_same(TC, __bf16) && !Q16 ? 3 : 2;  // parts of a probability (16-bit caches)
-    // f16: probabilities go in times 2^SHIFT.
-    static constexpr int SHIFT = __is_same(TC, _Float16) ? 15 : 0;
+    // f16: probabilities go into the second product times this, and its sums come out so.
+    // (Not by 2^(score + 15), which rounds the score at a magnitude of 15: probabilities
+    // kept 21 bits that way.)
+    static constexpr float UP = __is_same(TC, _Float16) ? 0x1p15f : 1.f;
     // Workgroups that a compute unit holds at once (waves of a SIMD): what the
     // registers of two tiles, the queries and the output leave.  (16-bit heads of up
     // to 96 keep up to nine of their registers in memory for the third: 4 key heads over
@@ -540,7 +542,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
         }
         float p[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - base + (float)Cfg::SHIFT);
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - base);
         l += (p[0] + p[1]) + (p[2] + p[3]);
         if constexpr (!C16) {
 #pragma unroll
@@ -553,6 +555,11 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, const Segment &s
                                                                             o[c * VV + i], 0, 0, 0);
         } else {
             Words<8> part[PP];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[r] *= Cfg::UP;
+                if constexpr (Cfg::UP != 1.f) asm("" : "+v"(p[r]));  // (one product, not one for each of its uses)
+            }
 #pragma unroll
             for (int i = 0; i < PP; ++i) {
                 Pack<TC, 4> h;
@@ -737,15 +744,16 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
                 if (d + 2 < a.dim) to[d + 2] = p.v[2];
             };
             if (all) {
-                v *= sum == 0.f ? 0.f : 1.f / sum;
+                v *= sum == 0.f ? 0.f : 1.f / (sum * Cfg::UP);
                 put((TQ *)a.out + (int64_t)seq * a.o_row + (int64_t)(head0 + h) * a.o_head);
                 if (d == 0 && a.lse)
                     a.lse[(int64_t)seq * a.q_heads + head0 + h] =
-                        sum == 0.f ? -INFINITY : (top + (__builtin_amdgcn_logf(sum) - (float)Cfg::SHIFT)) * kLn2;
+                        sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
             } else {
+                v *= 1.f / Cfg::UP;
                 put(a.part_o + (part + h) * a.dim);
                 if (d == 0) {
-                    a.part_ml[(part + h) * 2] = top - (float)Cfg::SHIFT;
+                    a.part_ml[(part + h) * 2] = top;
                     a.part_ml[(part + h) * 2 + 1] = sum;
                 }
             }
