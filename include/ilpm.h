@@ -430,9 +430,9 @@ int ilpm_maxpool2x2(const float *in, int C, int H, int W, float *out, hipStream_
  * as stated (strides in elements, not negative; the innermost dimension is
  * contiguous).  What a call writes must not overlap what it reads or else
  * writes, except where a comment allows it, and must not overlap itself.
- * Arithmetic and sums are fp32 or more; each output is rounded to its type
- * once, to nearest even.  Sizes of zero tokens, sequences or rows are valid
- * and launch nothing.
+ * Arithmetic and sums are fp32 or more (ilpm_attn_decode states what it holds in
+ * fewer bits); each output is rounded to its type once, to nearest even.  Sizes
+ * of zero tokens, sequences or rows are valid and launch nothing.
  *
  * What lies in device memory cannot be checked before a launch.  The kernels
  * check lengths, positions, sequence numbers and page numbers themselves and
@@ -519,6 +519,11 @@ typedef struct ilpm_attn_options {
  *   lengths  int32 [n_seqs]: tokens in the cache, the new one among them; taken
  *        as 0 below 0, and as the table's end beyond it
  *   out  as q (may be q itself);  lse  fp32 [n_seqs][q_heads] contiguous, or NULL
+ * Over 16-bit caches the exponentials that weigh the values are rounded (those in l
+ * are not): to 2^-17 of themselves under bf16 queries; over f16 to 2^-23, or by up to
+ * 2^-40 where that is more, so that an infinite v_j under a smaller one gives NaN;
+ * under fp32 queries over bf16 not at all.  Of fp32 queries over f16 what is below
+ * 2^-39 of a row's largest value is lost.
  * head_dim is at most 256 (ILPM_ERR_UNSUPPORTED above).
  * Long sequences are split over their length into parts whose results are
  * joined in their order, in a workspace of

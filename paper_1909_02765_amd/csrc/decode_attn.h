@@ -16,14 +16,19 @@
 //   16-bit cache: 16x16x32 for the scores; for the second product 16x16x16, whose
 //     operand of four keys comes together from four rows by byte permutations,
 //     and in them keys that are not seen become 0.  Probabilities, and queries
-//     of 32 bits, go in as 16-bit parts whose sum keeps their bits (hi = the value
-//     rounded, the next part what is left): queries in three; probabilities in two
-//     (16 bits of bf16, 22 of f16, more than an output of the type keeps), or
-//     three under 32-bit queries over bf16.  f16 parts are scaled by powers of two
-//     so that none of their bits fall below f16's smallest values.  The first part
+//     of 32 bits, go in as 16-bit parts (hi = the value rounded, the next part what
+//     is left, rounded).  Queries: three, which keep all their bits (over f16 those
+//     above 2^-39 of the largest's).  Probabilities: two under 16-bit queries, which
+//     hold bf16 ones to 2^-17 of them and f16 ones to 2^-23, for outputs of 8 and 11
+//     bits; three under 32-bit queries over bf16, which keep all bits; two there over
+//     f16, whose 2^-23 is a unit of the last place of 32 bits, as much as the
+//     exponential itself may be off (a third costs up to 11%: 8 ragged sequences of up
+//     to 30001 keys of 8 heads of 64 58.2 -> 64.8 us).  f16 parts are scaled by powers
+//     of two so that they keep what is above 2^-40 of the largest.  The first part
 //     has an accumulator of its own: an infinity in the cache makes infinities or
-//     NaN of it as the definition does, while the products with the small parts may
-//     be NaN where it has none (0 times infinity), and are left out if so.
+//     NaN of it as the definition does (of f16 probabilities below 2^-40, whose first
+//     part is 0, NaN), while the products with the small parts may be NaN where
+//     it has none (0 times infinity), and are left out if so.
 //
 // How the work is divided: the tiles of 16 keys of all (sequence, key head)
 // units lie in one row, which the workgroups share out evenly, as many as the

@@ -71,6 +71,13 @@ def test_probabilities():
     assert out.max() > 1.2 and lse.max() > 1.2
 
 
+@pytest.mark.parametrize("dtype,held", [(torch.bfloat16, 2.0 ** -17), (torch.float16, 2.0 ** -23)], ids=str)
+def test_two_parts_hold_what_the_header_says(dtype, held):
+    p = exact.full_mantissas(torch.Generator().manual_seed(3), (1 << 16,), 0.25, 1.0).abs()
+    off = (in_parts(p * 2.0 ** 15, dtype, 2).double() * 2.0 ** -15 - p.double()).abs() / p.double()
+    assert held / 2 < off.max() <= held
+
+
 @pytest.mark.parametrize("x", [1 / 64, 1 / 32])
 def test_two_keys_by_hand(x):
     out, lse = exact.expected_of_two(torch.tensor(x, dtype=torch.float64))
