@@ -513,11 +513,14 @@ typedef struct ilpm_attn_options {
  *   out = sum exp(x_j - m) v_j / l;  lse = m + ln l
  * over the keys j seen: j < lengths[s], in the window, not masked, in a page
  * of the pool.  Nothing else of the cache has a part in it, whatever it holds.
- * A row that sees no key gives out = 0 and lse = -infinity.
+ * A row that sees no key, or none that scores above -infinity, gives out = 0 and
+ * lse = -infinity.
  *   q    [n_seqs] rows of q_heads heads, a multiple of the cache's kv_heads:
  *        head h reads key head h / (q_heads / kv_heads).  The cache's type or ILPM_F32
- *   lengths  int32 [n_seqs]: tokens in the cache, the new one among them; taken
- *        as 0 below 0, and as the table's end beyond it
+ *   lengths  int32 [n_seqs]: tokens of the sequence, the new one among them; taken
+ *        as 0 below 0.  Of a sequence longer than its table can name only the keys
+ *        in the table are seen, while the window counts from the length itself: the
+ *        keys j >= lengths[s] - window, which may be none of them
  *   out  as q (may be q itself);  lse  fp32 [n_seqs][q_heads] contiguous, or NULL
  * Over 16-bit caches the exponentials that weigh the values are rounded (those in l
  * are not): to 2^-17 of themselves under bf16 queries; over f16 to 2^-23, or by up to

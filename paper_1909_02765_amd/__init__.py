@@ -566,8 +566,9 @@ def attn_decode(q, k_pages, v_pages, page_table, lengths, *, scale: Optional[flo
     softcap > 0: scores x become softcap * tanh(x / softcap); mask bool or uint8 [n_seqs, keys]: a key is seen where it
     is not 0; max_len: an upper bound of the lengths, if known.  Returns out (like q), or (out, lse) with return_lse
     or lse given, lse float32 [n_seqs, q_heads]: the logarithm of the sum of the exponentials of the scores.  A row that
-    sees no key gives 0 and -inf.  workspace: a contiguous CUDA tensor of attn_decode_workspace_size bytes, for calls that must
-    not allocate; by default it comes from torch's allocator.  See ilpm_attn_decode in include/ilpm.h."""
+    sees no key gives 0 and -inf.  Keys beyond the table's end are not seen, and the window counts from lengths itself
+    there too.  workspace: a contiguous CUDA tensor of attn_decode_workspace_size bytes, for calls that must not
+    allocate; by default it comes from torch's allocator.  See ilpm_attn_decode in include/ilpm.h."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return attn_decode(q, k_pages, v_pages, page_table, lengths, scale=scale, window=window, softcap=softcap,

@@ -1,4 +1,4 @@
-"""GPU: workspaces whose elements do not lie together are refused before anything is launched."""
+"""GPU: workspaces whose elements do not lie together are refused before anything is launched; lengths beyond the table."""
 import pytest
 import torch
 
@@ -46,3 +46,19 @@ def test_set_workspace_refuses_what_is_not_contiguous():
         ilpm.set_workspace(wide)
     finally:
         ilpm.set_workspace(None)
+
+
+def test_window_of_a_sequence_longer_than_its_table():
+    """It counts from the sequence's own length: with 48 keys named and values j at key j, of length 60 and a window of
+    20 keys 40 to 47 are seen, of length 68 none."""
+    torch_cuda()
+    import paper_1909_02765_amd as ilpm
+    kp = torch.zeros((3, 16, 1, 64), device="cuda")
+    vp = torch.arange(48.0, device="cuda").view(3, 16, 1, 1).expand(3, 16, 1, 64).contiguous()
+    table = torch.arange(3, dtype=torch.int32, device="cuda").expand(3, 3)
+    lengths = torch.tensor([60, 48, 68], dtype=torch.int32, device="cuda")
+    out, lse = ilpm.attn_decode(torch.zeros((3, 1, 64), device="cuda"), kp, vp, table, lengths, window=20, return_lse=True)
+    torch.cuda.synchronize()
+    want = torch.tensor([43.5, 37.5, 0.0], device="cuda")
+    assert torch.allclose(out, want.view(3, 1, 1).expand(3, 1, 64), rtol=1e-6)
+    assert torch.allclose(lse.flatten(), torch.tensor([8.0, 20.0, 0.0], device="cuda").log())
