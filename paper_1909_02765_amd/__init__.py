@@ -3,7 +3,8 @@
 Argument marshalling only: every step of the convolution runs in the HIP
 kernels behind the C ABI declared in include/ilpm.h.  PyTorch supplies device
 memory and the current stream.  There is no fallback: if the library is not
-built, importing the binding raises.
+built, importing the binding raises, and the decoder-step operators raise if
+their module is not.
 
     import paper_1909_02765_amd as ilpm
     y = ilpm.conv2d(x, w, bias, stride=1, pad=1)   # x [1,C_in,H,W], w [C_out,C_in,K,K]
@@ -66,10 +67,23 @@ import torch  # noqa: E402,F401
 
 lib = ctypes.CDLL(LIBRARY)
 
-if not os.path.exists(os.path.join(PKG, "_binding.so")):
-    raise ImportError(f"{os.path.join(PKG, '_binding.so')} is not built: run `python paper_1909_02765_amd/build.py` "
-                      "(or __graft_entry__.build()) first")
-from . import _binding  # noqa: E402
+
+class _Missing:
+    """In the place of the decoder-step operators' module where it cannot be loaded: it is built on one torch's C++
+    headers, which the convolutions do not need.  Every use raises."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"{os.path.join(PKG, '_binding.so')} is not built for this torch: run `python "
+                          f"paper_1909_02765_amd/build.py` (or __graft_entry__.build()) first ({self._why})")
+
+
+try:
+    from . import _binding  # noqa: E402
+except ImportError as e:
+    _binding = _Missing(e)
 
 
 def _hip_runtimes_mapped():
