@@ -16,7 +16,7 @@
 //   16-bit cache: 16x16x32 for the scores; for the second product 16x16x16, whose
 //     operand of four keys comes together from four rows by byte permutations,
 //     and in them keys that are not seen become 0.  Probabilities, and queries
-//     of 32 bits, go in as 16-bit parts (hi = the value rounded, the next part what
+//     of 32 bits, go in as 16-bit parts (one the value rounded, the next one what
 //     is left, rounded).  Queries: three, which keep all their bits (over f16 those
 //     above 2^-39 of the largest's).  Probabilities: two under 16-bit queries, which
 //     hold bf16 ones to 2^-17 of them and f16 ones to 2^-23, for outputs of 8 and 11
@@ -388,7 +388,14 @@ __device__ __forceinline__ void split_queries(const AttnArgs &a, const Segment &
 #pragma unroll
         for (int i = 0; i < KV; ++i) {
             float v = p.v[i] * f;
-            part[0].v[i] = (TC)v;
+            if constexpr (__is_same(TC, __bf16)) {
+                // Cut off, not rounded, which beyond bf16's largest value gives infinity: the parts
+                // after it hold the rest all the same.  (A NaN keeps a bit of its upper half.)
+                v = __builtin_canonicalizef(v);
+                part[0].v[i] = __builtin_bit_cast(__bf16, (unsigned short)(__builtin_bit_cast(unsigned, v) >> 16));
+            } else {
+                part[0].v[i] = (TC)v;
+            }
             v -= (float)part[0].v[i];
             part[1].v[i] = (TC)v;
             part[2].v[i] = (TC)(v - (float)part[1].v[i]);

@@ -13,7 +13,7 @@ SIZES = [5, 64, 72, 80, 96, 128, 192, 256]
 PAGE = 16
 
 
-def call(q, keys, values, seen, **options):
+def call(q, keys, values, seen, factor=1.0):
     """attn_decode of sequences that share one paged cache [keys][kv_heads][d], sequence s seeing the keys seen[s]."""
     torch_cuda()
     import paper_1909_02765_amd as ilpm
@@ -25,7 +25,7 @@ def call(q, keys, values, seen, **options):
     kp, vp = (t.view(pages, PAGE, *t.shape[1:]).cuda() for t in (kp, vp))
     table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, -1).expand(n, -1)
     lengths = torch.full((n,), keys.shape[0], dtype=torch.int32, device="cuda")
-    out, lse = ilpm.attn_decode(q.cuda(), kp, vp, table, lengths, scale=1.0, mask=mask.cuda(), return_lse=True, **options)
+    out, lse = ilpm.attn_decode(q.cuda(), kp, vp, table, lengths, scale=factor, mask=mask.cuda(), return_lse=True)
     torch.cuda.synchronize()
     return out.double().cpu(), lse.double().cpu()
 
@@ -92,3 +92,22 @@ def test_lse_keeps_32_bits_under_16_bit_queries(x, keys, apart):
     out, lse = call(q, k, v, torch.tensor([[0, apart]]))
     _, want = exact.expected_of_two(-q[:, :, 0].double())
     assert ((lse - want).abs() <= exact.LSE).all() and (out == 1).all()
+
+
+@pytest.mark.parametrize("cache", CACHES, ids=str)
+@pytest.mark.parametrize("keys", [2, 600])
+def test_queries_up_to_the_largest_value(cache, keys):
+    """Finite queries beyond the range of 16-bit types, under a scale that leaves scores of magnitude 256: no part of
+    them is infinite, and a key that is 0 there scores 0."""
+    top = torch.finfo(torch.float32).max
+    rows = torch.tensor([top, -top, 3.3962e38, 3.3961e38, 3.3895314e38, 3.39e38, -3.4e38, 1e38])
+    q = torch.zeros((len(rows), 16, 64))
+    q[:, :, 37] = rows.unsqueeze(1)
+    q[:, :, 11] = 1.0
+    k, v = torch.zeros((keys, 1, 64), dtype=cache), torch.ones((keys, 1, 64), dtype=cache)
+    k[1, 0, 37] = 1.0   # key 1 scores by the large element, key 0 by none
+    note(f"[attn] largest queries, {cache}, {keys} keys")
+    out, lse = call(q, k, v, torch.tensor([[0, 1]]).expand(len(rows), -1), factor=2.0 ** -120)
+    x = rows.double() * 2.0 ** -120
+    want = torch.logsumexp(torch.stack((torch.zeros_like(x), x)), 0).unsqueeze(1)
+    assert ((lse - want).abs() <= exact.SCORE * want.abs().clamp_min(1)).all() and (out == 1).all()
