@@ -56,7 +56,7 @@ class Decoder:
     """One sequence: its weights packed for one token, its cache pages, and how many tokens they hold."""
 
     def __init__(self, weights, most_tokens, cache=torch.float32):
-        self.w, self.length = weights, 0
+        self.w, self.length, self.most = weights, 0, most_tokens
         self.cos, self.sin = angles(most_tokens)
         pages = -(-most_tokens // PAGE)
         # The pages of a sequence lie where the pool had room.
@@ -86,6 +86,8 @@ class Decoder:
     def step(self, x):
         """x [T, WIDTH], the next T tokens' embeddings: their outputs [T, WIDTH]."""
         t = x.shape[0]
+        if self.length + t > self.most:  # (the cache would leave them out)
+            raise ValueError(f"{t} tokens after {self.length} are more than the {self.most} that this decoder was made for")
         pos = torch.arange(self.length, self.length + t, dtype=torch.int32, device="cuda")
         seq, lengths = torch.zeros_like(pos), pos + 1
         rows = self.table.expand(t, -1)  # every token of the call reads the one sequence's pages

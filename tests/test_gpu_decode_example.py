@@ -74,3 +74,19 @@ def test_decoder_agrees_with_dense_layers(cache, bound):
     want = dense(m, dbl, x.double())
     off = (torch.cat(got).double().cpu() - want).abs().max().item()
     assert off <= bound * max(1.0, want.abs().max().item()), off
+
+
+def test_decoder_refuses_more_tokens_than_it_was_made_for():
+    """What its cache and angles have no place for would be left out, and the outputs be those of other tokens."""
+    m = example()
+    d = m.Decoder(m.make_weights(5), 20)
+    x = torch.randn((24, m.WIDTH), generator=torch.Generator().manual_seed(6)).cuda()
+    z = d.step(x[:18])
+    with pytest.raises(ValueError, match="more than the 20"):
+        d.step(x[18:21])
+    last = d.step(x[18:20])   # a refused call changed nothing
+    with pytest.raises(ValueError):
+        d.step(x[20:21])
+    again = m.Decoder(m.make_weights(5), 20).step(x[:20])
+    torch.cuda.synchronize()
+    assert (torch.cat((z, last)) - again).abs().max() < 1e-3
