@@ -4,7 +4,9 @@ Argument marshalling only: every step of the convolution runs in the HIP
 kernels behind the C ABI declared in include/ilpm.h.  PyTorch supplies device
 memory and the current stream.  There is no fallback: if the library is not
 built, importing the binding raises, and the decoder-step operators raise if
-their module is not.
+their module is not.  Everything here is for inference: nothing is recorded for
+autograd, so outputs, and tensors written in place, never require a gradient,
+also where inputs do.
 
     import paper_1909_02765_amd as ilpm
     y = ilpm.conv2d(x, w, bias, stride=1, pad=1)   # x [1,C_in,H,W], w [C_out,C_in,K,K]

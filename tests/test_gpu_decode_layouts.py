@@ -1,4 +1,5 @@
-"""GPU: workspaces whose elements do not lie together are refused before anything is launched; lengths beyond the table."""
+"""GPU: workspaces whose elements do not lie together are refused before anything is launched; lengths beyond the table;
+inputs that require gradients."""
 import pytest
 import torch
 
@@ -62,3 +63,18 @@ def test_window_of_a_sequence_longer_than_its_table():
     want = torch.tensor([43.5, 37.5, 0.0], device="cuda")
     assert torch.allclose(out, want.view(3, 1, 1).expand(3, 1, 64), rtol=1e-6)
     assert torch.allclose(lse.flatten(), torch.tensor([8.0, 20.0, 0.0], device="cuda").log())
+
+
+def test_inputs_that_require_gradients_give_outputs_that_do_not():
+    torch_cuda()
+    import paper_1909_02765_amd as ilpm
+    x, w = torch.randn((4, 64), device="cuda", requires_grad=True), torch.ones(64, device="cuda", requires_grad=True)
+    heads = torch.randn((4, 2, 64), device="cuda", requires_grad=True)
+    kp, vp = torch.zeros((4, 16, 2, 64), device="cuda"), torch.zeros((4, 16, 2, 64), device="cuda")
+    table, zeros = torch.arange(4, dtype=torch.int32, device="cuda").view(4, 1), torch.zeros(4, dtype=torch.int32, device="cuda")
+    q = ilpm.kv_append(heads, heads, kp, vp, table, table.flatten(), zeros, q=heads)
+    got = (q, kp, vp, *ilpm.attn_decode(heads, kp, vp, table, zeros + 1, return_lse=True), *ilpm.residual_norm(x, x, post="rms", post_w=w))
+    assert not any(t.requires_grad for t in got)
+    assert torch.equal(got[3], heads.detach())   # of one key, its value
+    image, filters = torch.randn((1, 8, 5, 5), device="cuda", requires_grad=True), torch.randn((4, 8, 3, 3), device="cuda", requires_grad=True)
+    assert not ilpm.conv2d(image, filters).requires_grad
