@@ -299,12 +299,17 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_rows(NormArgs a)
 // rows in workgroups of up to four waves 20 (3822 bf16 rows of 1732 14.1 -> 13.2
 // us).  Of f32 rows more of them at once than the next power of two would hold
 // are slower (8000 f32 rows of 2052 over bf16: two workgroups of five waves a unit
-// 57 us, three 65; bf16 rows 55 and 42).  Calls whose bytes come from memory and not
-// from the 256 MB cache before it, in rows that fill eight waves, do better with one
-// workgroup a unit (us with two and one: 16000 f32 rows of 4096 over bf16 204 and 186,
-// of 3584 179 and 162, bf16 ones of 4096 128 and 118; but 16000 of 3584 110 and
-// 112, of 262 MB 8000 of 4096 44 and 48, and 14016 f16 ones of 3651, which are LOOSE, 92
-// and 97).
+// 57 us, three 65; bf16 rows 55 and 42).  Rows of 3584 to 4096 values, which are
+// seven and eight waves, otherwise go two workgroups a unit; where more bytes than the
+// 256 MB cache before the memory holds are moved, one is faster (us with two and one:
+// 16000 f32 rows of 3584 over bf16 with f32 gates by rows 175 and 161, of 4096 203 and
+// 190; 8000 of 3584 over bf16 alone, 344 MB, 63 and 61; 16000 bf16 rows of 3584 90 and
+// 90, of 4096 100 and 93, but 8000 of 4096, 262 MB, 42 and 48; 14016 f16 ones of 3651,
+// which are LOOSE, 92 and 97).  Narrower rows of two workgroups a unit are left as they
+// are: there it goes by the types (16000 rows of 2568: f32 over bf16 125 and 116, bf16
+// 69 and 86).
+constexpr int64_t kBeyondCache = 320000000;
+
 template <typename TX, typename TY, typename TP, int T, int E, int VEC, bool LOOSE>
 void launch_rows(const NormArgs &a, hipStream_t stream)
 {
@@ -312,7 +317,7 @@ void launch_rows(const NormArgs &a, hipStream_t stream)
     const int block = T <= 64 ? 256 : ceil_div(a.width, E * 64) * 64, waves = block / 64;
     const int64_t bytes = (int64_t)a.rows * a.width *
                           (sizeof(TX) * (1 + !!a.r) + sizeof(TY) * (!!a.y + !!a.z) + sizeof(TP) * (a.gate && a.gate_row > 0));
-    const bool alone = !LOOSE && a.width >= 3584 && a.width <= 4096 && bytes > 320000000;
+    const bool alone = !LOOSE && a.width >= 3584 && a.width <= 4096 && bytes > kBeyondCache;
     const int full = waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : waves <= 8 ? 8 : 16;
     const int per_cu = alone ? 1 : sizeof(TX) == 2 ? (waves <= 4 ? 20 : 16) / waves : 16 / full;
     const int rows = ceil_div(a.rows, per), turns = ceil_div(rows, 256 * per_cu);
