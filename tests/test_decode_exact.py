@@ -34,6 +34,8 @@ def test_scores():
         assert torch.equal(in_parts(q, dtype, 3), q)
     assert of(in_parts(q, torch.bfloat16, 2)).max() > 10 and (of(in_parts(q, torch.bfloat16, 2)) > 1).float().mean() > 0.5
     assert (of(in_parts(q, torch.float16, 1)) > 1).float().mean() > 0.9
+    # Of f16 the third part holds a last bit alone, which the bound leaves room for and equal bits do not.
+    assert ((in_parts(q, torch.float16, 2) * LOG2E * LN2) != q * LOG2E * LN2).float().mean() > 0.1
 
 
 def of_two(x, probability, kept, shift=0):

@@ -50,6 +50,17 @@ def test_scores_keep_32_bits(cache, d, keys, kv_heads):
     assert (out == 1).all()
 
 
+@pytest.mark.parametrize("d", SIZES)
+def test_scores_are_the_same_bits_over_every_cache(d):
+    """One-hot keys are exact in each type, and three parts hold all of a query: what follows is the same arithmetic.
+    (The last bit of 32 is in the third part of f16 as of bf16.)"""
+    q = exact.full_mantissas(torch.Generator().manual_seed(d), (d, 16, d), 0.5, 2.0)
+    note(f"[attn] the same scores over every cache, d {d}")
+    got = [call(q, exact.one_hot(torch.arange(d), d).unsqueeze(1).to(cache), torch.ones((d, 1, d), dtype=cache),
+                torch.arange(d).unsqueeze(1))[1] for cache in CACHES]
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
 @pytest.mark.parametrize("cache", CACHES, ids=str)
 @pytest.mark.parametrize("d", SIZES)
 # The second key: of the same tile, of another wave's, of another tile of the wave; few keys and many.
