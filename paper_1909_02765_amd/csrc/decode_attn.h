@@ -36,11 +36,15 @@
 // unit that spans workgroups leaves partial results, which attn_join adds.
 //
 // What bounds it: the cache's bytes (131071 keys of 8 bf16 heads of 128 under 32
-// query heads 106 us, 64 ragged sequences of up to 8191 of them 211 us, 5.0 TB/s
-// with the join); of single heads with window, mask and soft cap the vector unit
-// (24 sequences of 12 f16 heads of 80, window 1000: 27 us, 2.6 TB/s); of calls with a tile or
-// two a wave the accesses that wait for each other (lengths, pages, rows, the
-// join: f32 queries over 16 shared bf16 heads of 256, 8 sequences of up to 2049, 15 us).
+// query heads 106 us, 64 ragged sequences of up to 8191 of them 210 us, 5.0 TB/s
+// with the join).  f32 queries over heads of 72 and 80 stay below that (117164 keys
+// of 7 f16 heads of 72 under 84 79 us, 3.0 TB/s; their second product is done over the
+// 128 values that sixteen lanes load), and so do single heads with window, mask and soft
+// cap (24 sequences of 12 f16 heads of 80, window 1000: 27 us, 2.6 TB/s).  In both the
+// vector unit issues in 32 to 40% of the cycles and the matrix cores are busy in 7 to
+// 11%: neither is full, and two waves a SIMD do not cover each other's waits.  Of calls with a tile or two a wave it is the accesses that wait
+// for each other (lengths, pages, rows, the join: f32 queries over 16 shared bf16
+// heads of 256, 8 sequences of up to 2049, 15 us).
 #pragma once
 
 #include <climits>
@@ -60,7 +64,10 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // How rows lie in memory: whole (16-byte pieces, dim is the class's size), in
-// 16-byte pieces, or in no such order (element by element).
+// 16-byte pieces, or in no such order (element by element, for pools that are off
+// that alignment and sizes that are no whole pieces: 131071 keys of 8 bf16 heads of 128
+// under 32 take 573 us so in place of 107, 65000 of 8 heads of 64 under f32 queries 89
+// in place of 33).
 enum Rows { kWhole, kPieces, kAny };
 
 // The keys of a sequence that the window leaves: [first, end).
@@ -180,7 +187,12 @@ template <typename TC, bool Q16, int DC, Rows R, bool SHORT> struct AttnKernel {
     // Workgroups that a compute unit holds at once (waves of a SIMD): what the
     // registers of two tiles, the queries and the output leave.  (16-bit heads of up
     // to 96 keep up to nine of their registers in memory for the third: 4 key heads over
-    // 48 x 14583 bf16 keys of 72 221 us with two, 175 with three.)
+    // 48 x 14583 bf16 keys of 72 221 us with two, 175 with three.)  The bounds of SHORT
+    // kernels are those of 16-bit queries.  Under 32-bit ones they are not reached at
+    // 128 (two for three) and 256 (one for two), and at 64, where they are, up to 50
+    // registers of f16 caches and 17 of bf16 ones lie in memory (1 sequence of 250 keys
+    // of 2 bf16 heads under 8 of 32 bits: 7.4 us).  Rows taken element by element spill
+    // as much as 181.
     static constexpr int PER_CU = SHORT ? (DC == 64 ? 5 : DC <= 128 ? 3 : 2) : DC == 64 ? (QP == 3 ? 3 : 4) : DC == 96 && C16 ? 3 : DC <= 128 ? 2 : 1;
     // Whether a tile is loaded where there is none (the pool's first row for it).
     // Loads behind a condition the compiler cannot count, and waits for all of them

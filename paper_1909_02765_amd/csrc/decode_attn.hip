@@ -111,8 +111,11 @@ template <int V> __global__ __launch_bounds__(256) void attn_join(AttnArgs a)
 // two kernels and one more for every 36 units (fitted to 64 calls of 17 to 64 tiles
 // and 60 to 1425 units: 1386 units of 48 tiles, f16 heads of 80, 114 us shared and
 // 66 by units; 65 such units under f32 queries 15 and 20).  Beyond 64 tiles units
-// differ too much in length (207 of up to 321 tiles 56 us shared and 134 by units),
-// and fewer than 60 would leave most of the card idle.
+// differ too much in length (207 of up to 321 tiles 56 us shared and 134 by units).
+// The fit has no calls of fewer than 60 units, and those are shared beyond 16 tiles: 8
+// and 32 units of bf16 heads of 128 take 9.7 and 10.0 us shared at 19 tiles (8.0 and 8.1
+// by units), 9.8 and 10.7 at 29 (10.1 and 10.2), 9.8 and 11.0 at 44 (12.7 and 12.8), 8
+// units of f32 ones 10.8 at 17 tiles (12.6).
 size_t attn_plan(AttnArgs *a, int cache_dtype, bool q32, int max_len)
 {
     a->blocks = ceil_div(a->group, kAttnHeads);
