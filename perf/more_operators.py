@@ -641,7 +641,7 @@ def _exact_verify(s):
                 if total > 0 and u[i][c] * (1.0 if q is None else q[x].item()) < have / total:
                     taken = c
                     break
-                if q is not None and total <= 0:
+                if total <= 0:
                     continue
                 if q is None:
                     total -= have
