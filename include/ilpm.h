@@ -576,6 +576,167 @@ typedef struct ilpm_residual_norm_args {
 } ilpm_residual_norm_args;
 int ilpm_residual_norm(const ilpm_residual_norm_args *args, hipStream_t stream);
 
+/* ---- a drafted decoder step: trees of guessed tokens over the paged cache ----
+ *
+ * A decoder that drafts runs several guessed tokens of a sequence in one pass
+ * and keeps those that the target's probabilities allow.  The guesses of a
+ * sequence form a tree (or several) of up to ILPM_MAX_NODES nodes: parents[i]
+ * is the node that node i follows, a number below i, or -1 for a node that
+ * follows the sequence itself (a root).  A node with any other parent, or whose
+ * parent is none, is no node (padding: -2).  Node i of a sequence of L tokens
+ * is token L + i of the cache; its place in the text is L + its depth, the
+ * number of nodes above it.
+ *
+ *   ilpm_kv_append_norm  queries and keys normed and rotated, keys and values stored
+ *   ilpm_attn_tree       attention of every node over the cache and the nodes above it
+ *   ilpm_verify_drafts   which nodes are kept, and the token that follows the last
+ *   ilpm_kv_copy         the kept nodes' keys and values moved together, sequences forked
+ *
+ * The conventions of a decoder step, above, hold for them too.
+ */
+#define ILPM_MAX_NODES 64
+
+/* How ilpm_kv_append_norm norms, rotates and places its tokens. */
+typedef struct ilpm_append_options {
+    const int32_t *seq_ids, *positions; /* int32 [n_tokens] */
+    const int32_t *slots;               /* int32 [n_tokens], or NULL: positions */
+    const float *cos, *sin;             /* as ilpm_kv_append's */
+    const void *q_w, *k_w;              /* [head_dim] of param_dtype, or NULL: 1 */
+    int n_positions, rot_dim, pairs;
+    int norm;                           /* ILPM_NORM_*, of each head */
+    int param_dtype;                    /* k's type or ILPM_F32 */
+    float eps;
+} ilpm_append_options;
+
+/*
+ * ilpm_kv_append_norm -- ilpm_kv_append with a norm of every head of the
+ * queries and keys before their rotation, and with slots of their own for the
+ * tokens: token t is rotated by positions[t] and stored as token slots[t] of
+ * sequence seq_ids[t].
+ *   a head h becomes rotated(norm(h)), norm as ilpm_residual_norm's over the
+ *   head's own head_dim values, with weights q_w for queries and k_w for keys;
+ *   ILPM_NORM_NONE leaves it as it is (then q_w and k_w must be NULL).  Values
+ *   are only stored.  What is normed is rotated before it is rounded.
+ * Tokens are left out as ilpm_kv_append leaves them out, their place in the
+ * cache by slots[t]; a query is normed wherever its key goes, and is rotated
+ * where its position is in [0, n_positions).  q_out may be q itself (same data and strides).
+ * head_dim is at most 1024 (ILPM_ERR_UNSUPPORTED above, and for element types
+ * other than ilpm_kv_append's).
+ */
+int ilpm_kv_append_norm(const ilpm_kv_cache *cache, const ilpm_heads *k, const ilpm_heads *v, const ilpm_heads *q,
+                        const ilpm_heads *q_out, const ilpm_append_options *options, int n_tokens, hipStream_t stream);
+
+/* How ilpm_attn_tree scores and which keys it sees. */
+typedef struct ilpm_tree_options {
+    const uint8_t *mask;   /* as ilpm_attn_options', over the tokens of the cache, nodes among them */
+    int64_t mask_stride;
+    float scale, softcap;  /* as there */
+    int mask_len;
+    int window;            /* > 0: a node sees only keys less than `window` places before it; 0: all */
+    int sinks;             /* with a window: keys at places below this are seen all the same */
+    int max_len;           /* no sequence is longer (its nodes not counted), as far as the caller knows;
+                              0: unknown.  Only the split over the length goes by it */
+} ilpm_tree_options;
+
+/*
+ * ilpm_attn_tree -- attention of the nodes of each sequence's trees over the
+ * cache: with x_j, out and lse as ilpm_attn_decode has them, node i of a
+ * sequence of L = lengths[s] tokens (taken as 0 below 0) sees the keys
+ *   j < L          at place j: all tokens of the sequence
+ *   j = L + a      at place L + depth(a), for a = i and every node a above it
+ * that are in a page of the pool, not masked (mask[s][j]), and, with a window,
+ * less than `window` places before the node's own, L + depth(i), or at a place
+ * below `sinks`.  Nothing else of the cache has a part in it.
+ *   q    [n_seqs * n_nodes] rows of q_heads heads, row s * n_nodes + i is node i of
+ *        sequence s; heads and types as ilpm_attn_decode's
+ *   lengths  int32 [n_seqs]: tokens of the sequence without its nodes.  Of keys
+ *        beyond the sequence's table none is seen; places count from lengths itself
+ *   parents  int32 [n_seqs][n_nodes], contiguous; n_nodes at most ILPM_MAX_NODES
+ *        (ILPM_ERR_UNSUPPORTED above)
+ *   out  as q (may be q itself);  lse  fp32 [n_seqs * n_nodes][q_heads] contiguous, or NULL
+ * The rows of what is no node, and of nodes that see no key, give out = 0 and
+ * lse = -infinity.  A chain of n tokens (parents -1, 0, 1, ...) is a prompt's
+ * next part; a single node is ilpm_attn_decode's new token.
+ * Over 16-bit caches the exponentials that weigh the values are rounded (those in
+ * lse are not): under 16-bit queries to 2^-17 of themselves over bf16 and 2^-23 over
+ * f16, or there by up to 2^-40 where that is more; under fp32 queries over bf16 to 2^-24, over f16 as
+ * under 16-bit ones.  An infinite v_j that is seen gives infinity or NaN.  Of fp32
+ * queries over f16 what is below 2^-39 of a row's largest value is lost.
+ * head_dim is at most 256 (ILPM_ERR_UNSUPPORTED above).
+ * The workspace is as ilpm_attn_decode's, of ilpm_attn_tree_workspace_size bytes.
+ */
+int ilpm_attn_tree(const ilpm_kv_cache *cache, const ilpm_heads *q, const int32_t *lengths, const int32_t *parents,
+                   int n_nodes, const ilpm_tree_options *options, const ilpm_heads *out, float *lse, void *workspace,
+                   size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ilpm_attn_tree (0 where it needs none), from the cache's
+ * sizes, q_heads, n_nodes, the window, the sinks and max_len.  Pure host. */
+int ilpm_attn_tree_workspace_size(const ilpm_kv_cache *cache, int q_heads, int n_nodes, int window, int sinks,
+                                  int max_len, size_t *bytes);
+
+/*
+ * ilpm_verify_drafts -- which nodes of each sequence's tree are kept, so that
+ * the tokens follow the target's probabilities whatever was drafted, and the
+ * token that comes after them.  Node 0 is the last token that is certain; the
+ * walk begins there.  From a node with target row p and draft row q, the
+ * distributions of the token after it, its children are tried in their order,
+ * with w = p and Z = 1 at first.  A child with token x is kept, and the walk goes
+ * on from it, if
+ *   with draft rows:  u q(x) Z < w(x), else w becomes max(w / Z - q, 0) and Z its sum
+ *   without:          u Z < w(x),      else Z becomes Z - w(x) and w(x) 0
+ * where u = uniforms[s][child], and only while Z > 0.  (With draft rows the
+ * children of a node are drawn independently from q; without, they may be any,
+ * such as the most likely tokens.)  Behind the last kept node the next token is
+ * the smallest v with w(0) + ... + w(v) > uniforms[s][0] (w(0) + w(1) + ...),
+ * or the last one with w(v) > 0 where there is none; over p in the place of w
+ * where w is 0 everywhere, and -1 where p is as well.
+ * Sums are held in 64 bits.  A probability that is not above 0 (NaN among them)
+ * counts as 0, one above the largest fp32 number as that.  A child whose token is
+ * outside [0, vocab) is not kept and changes nothing.
+ *   tokens, parents  int32 [n_seqs][n_nodes], contiguous, n_nodes in [1, ILPM_MAX_NODES]
+ *   target, draft  [n_seqs][n_nodes][vocab] of dtype, rows strided as given (in
+ *           elements); row i is the distribution after node i.  draft NULL: none
+ *   uniforms  fp32 [n_seqs][n_nodes], contiguous, in [0, 1)
+ *   path    int32 [n_seqs][n_nodes]: the kept nodes from node 0 on, then -1
+ *   counts  int32 [n_seqs]: how many they are;  next_tokens  int32 [n_seqs]
+ * A sequence whose parents[s][0] is not -1 has no tree: its path is all -1, its
+ * count 0 and its next token -1.
+ * The workspace is as ilpm_attn_decode's, of ilpm_verify_drafts_workspace_size bytes.
+ */
+typedef struct ilpm_verify_args {
+    const int32_t *tokens, *parents;
+    const void *target, *draft;
+    int64_t target_seq_stride, target_node_stride, draft_seq_stride, draft_node_stride;
+    const float *uniforms;
+    int32_t *path, *counts, *next_tokens;
+    int n_seqs, n_nodes, vocab;
+    int dtype; /* of target and draft */
+} ilpm_verify_args;
+int ilpm_verify_drafts(const ilpm_verify_args *args, void *workspace, size_t workspace_bytes, hipStream_t stream);
+int ilpm_verify_drafts_workspace_size(int n_seqs, int n_nodes, int vocab, size_t *bytes);
+
+/*
+ * ilpm_kv_copy -- copy tokens' keys and values within the pools: for every row s
+ * and i < min(counts[s], max_count), token dst_start[s] + i of row s of
+ * dst_table becomes token src_start[s] + i of row s of the cache's own table,
+ * or with a path token src_start[s] + path[s][i].
+ *   With a path (int32 [n_seqs], rows path_stride apart, of at least max_count
+ * entries; max_count at most ILPM_MAX_NODES, ILPM_ERR_UNSUPPORTED above) all of a
+ * row's tokens are read before any is written: kept nodes of a tree are moved
+ * together in their own place by equal tables and starts.  A negative entry copies nothing.
+ *   Without one a slot that is written must not be read by the same call, unless
+ * it is copied onto itself: sequences are forked onto pages of their own, whole
+ * shared pages by the tables alone.
+ * Of two rows neither may write what the other reads or writes, except the same
+ * values onto themselves.  A token that is outside its table, or in no page of the
+ * pool, is neither read nor written; counts below 0 are taken as 0.
+ *   dst_table  int32 [n_seqs][dst_max_pages], rows dst_table_stride apart (0: the same pages)
+ *   src_start, dst_start, counts  int32 [n_seqs]
+ */
+int ilpm_kv_copy(const ilpm_kv_cache *cache, const int32_t *dst_table, int64_t dst_table_stride, int dst_max_pages,
+                 const int32_t *src_start, const int32_t *dst_start, const int32_t *counts, const int32_t *path,
+                 int64_t path_stride, int max_count, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -141,6 +141,12 @@ _SIGS = {
     "ilpm_attn_decode": ([_vp] * 7 + [ctypes.c_size_t, _vp], _i),
     "ilpm_attn_decode_workspace_size": ([_vp, _i, _i, _i, ctypes.POINTER(ctypes.c_size_t)], _i),
     "ilpm_residual_norm": ([_vp, _vp], _i),
+    "ilpm_kv_append_norm": ([_vp] * 6 + [_i, _vp], _i),
+    "ilpm_attn_tree": ([_vp] * 4 + [_i] + [_vp] * 4 + [ctypes.c_size_t, _vp], _i),
+    "ilpm_attn_tree_workspace_size": ([_vp] + [_i] * 5 + [ctypes.POINTER(ctypes.c_size_t)], _i),
+    "ilpm_verify_drafts": ([_vp, _vp, ctypes.c_size_t, _vp], _i),
+    "ilpm_verify_drafts_workspace_size": ([_i] * 3 + [ctypes.POINTER(ctypes.c_size_t)], _i),
+    "ilpm_kv_copy": ([_vp, _vp, ctypes.c_int64, _i, _vp, _vp, _vp, _vp, ctypes.c_int64, _i, _vp], _i),
 }
 for _name, (_args, _res) in _SIGS.items():
     _f = getattr(lib, _name)
@@ -613,4 +619,112 @@ def residual_norm(x, y=None, *, post: Optional[str] = None, post_w=None, post_b=
     got = _binding.residual_norm(x, y, NORMS[post], post_w, post_b, gate, scale, NORMS[pre], pre_w, pre_b, eps, r, z)
     if type(got) is int:
         raise IlpmError(got, "ilpm_residual_norm")
+    return got
+
+
+# ---- a drafted decoder step: trees of guessed tokens over the paged cache ----
+
+MAX_NODES = 64  # ILPM_MAX_NODES
+
+
+def kv_append_norm(k, v, k_pages, v_pages, page_table, seq_ids, positions, *, slots=None, q=None,
+                   norm: Optional[str] = "rms", q_w=None, k_w=None, eps: float = 1e-6, cos=None, sin=None,
+                   pairs: bool = False, q_out=None, stream=None):
+    """kv_append with each head of q and k normed before its rotation, and tokens stored at slots of their own.
+
+    Arguments as kv_append's, and: slots int32 [tokens], where in its sequence each token is stored (positions, by which
+    it is rotated, if not given: a drafted node lies at the sequence's length + its number, its position is the length +
+    its depth); norm None, "rms" or "layer", over the head_dim values of a head, with weights q_w and k_w [head_dim] of
+    k's type or float32.  Returns q_out or None.  See ilpm_kv_append_norm in include/ilpm.h."""
+    if norm not in NORMS:
+        raise ValueError('norm must be None, "rms" or "layer"')
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_append_norm(k, v, k_pages, v_pages, page_table, seq_ids, positions, slots=slots, q=q, norm=norm,
+                                  q_w=q_w, k_w=k_w, eps=eps, cos=cos, sin=sin, pairs=pairs, q_out=q_out)
+    got = _binding.kv_append_norm(k, v, k_pages, v_pages, page_table, seq_ids, positions, slots, q, NORMS[norm], q_w, k_w,
+                                  eps, cos, sin, pairs, q_out)
+    if type(got) is int:
+        raise IlpmError(got, "ilpm_kv_append_norm")
+    return got
+
+
+def attn_tree_workspace_size(k_pages, v_pages, page_table, q_heads: int, nodes: int, window: int = 0, sinks: int = 0,
+                             max_len: int = 0) -> int:
+    """Bytes of workspace attn_tree needs for this cache (0 where it needs none)."""
+    got = _binding.attn_tree_workspace_size(k_pages, v_pages, page_table, q_heads, nodes, window, sinks, max_len)
+    if got < 0:
+        raise IlpmError(got, "ilpm_attn_tree_workspace_size")
+    return got
+
+
+def attn_tree(q, k_pages, v_pages, page_table, lengths, parents, *, scale: Optional[float] = None, window: int = 0,
+              sinks: int = 0, softcap: float = 0.0, mask=None, max_len: int = 0, out=None, lse=None,
+              return_lse: bool = False, workspace=None, stream=None):
+    """Attention of trees of drafted tokens over a paged cache.
+
+    parents int32 [n_seqs, nodes], up to 64 nodes: the node that each follows, below its own number; -1 follows the
+    sequence itself; -2 is no node.  q [n_seqs * nodes, q_heads, head_dim]: row s * nodes + i is node i of sequence s,
+    whose key and value are token lengths[s] + i of the cache (lengths int32 [n_seqs], the nodes not counted).  A node
+    sees the sequence, itself and the nodes above it; with window > 0 only what is less than `window` places before its
+    own, lengths[s] + its depth, and the first `sinks` places.  The rest as in attn_decode, mask over the cache's tokens,
+    max_len without the nodes; a single node is attn_decode's token.  Returns out (like q), or (out, lse).
+    See ilpm_attn_tree in include/ilpm.h."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attn_tree(q, k_pages, v_pages, page_table, lengths, parents, scale=scale, window=window, sinks=sinks,
+                             softcap=softcap, mask=mask, max_len=max_len, out=out, lse=lse, return_lse=return_lse,
+                             workspace=workspace)
+    got = _binding.attn_tree(q, k_pages, v_pages, page_table, lengths, parents, scale, window, sinks, softcap, mask, max_len,
+                             out, lse, return_lse, workspace)
+    if type(got) is int:
+        raise IlpmError(got, "ilpm_attn_tree")
+    return got
+
+
+def verify_drafts_workspace_size(n_seqs: int, n_nodes: int, vocab: int) -> int:
+    """Bytes of workspace verify_drafts needs."""
+    got = _binding.verify_drafts_workspace_size(n_seqs, n_nodes, vocab)
+    if got < 0:
+        raise IlpmError(got, "ilpm_verify_drafts_workspace_size")
+    return got
+
+
+def verify_drafts(tokens, parents, target, uniforms, *, draft=None, path=None, counts=None, next_tokens=None,
+                  workspace=None, stream=None):
+    """Which drafted nodes are kept, and the token after the last of them, so that tokens follow the target.
+
+    tokens, parents int32 [n_seqs, nodes] (parents as in attn_tree; node 0 is the last token that is certain); target
+    [n_seqs, nodes, vocab]: row i is the distribution after node i; draft, if given, of the same sizes and type: the
+    distributions that each node's children were drawn from, independently (without it the children may be any tokens);
+    uniforms float32 [n_seqs, nodes] in [0, 1): number i tests node i, number 0 draws the next token.  Returns (path,
+    counts, next_tokens), int32 [n_seqs, nodes], [n_seqs], [n_seqs]: the kept nodes from node 0 on, then -1; how many;
+    the next token.  See ilpm_verify_drafts in include/ilpm.h."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return verify_drafts(tokens, parents, target, uniforms, draft=draft, path=path, counts=counts,
+                                 next_tokens=next_tokens, workspace=workspace)
+    got = _binding.verify_drafts(tokens, parents, target, uniforms, draft, path, counts, next_tokens, workspace)
+    if type(got) is int:
+        raise IlpmError(got, "ilpm_verify_drafts")
+    return got
+
+
+def kv_copy(k_pages, v_pages, src_table, dst_table, src_start, dst_start, counts, *, path=None,
+            max_count: Optional[int] = None, stream=None):
+    """Copy tokens' keys and values within the pools, in place.
+
+    For every row s of the tables and i < counts[s]: token dst_start[s] + i of dst_table's row becomes token
+    src_start[s] + i of src_table's row, or with a path (int32 [n_seqs, up to 64]) token src_start[s] + path[s, i].
+    With a path a row is read whole before it is written: kv_copy(k, v, table, table, lengths, lengths, counts,
+    path=path) moves the nodes that verify_drafts kept together behind the sequence.  Without one, what is written must
+    not be read by the call: sequences fork onto pages of their own.  max_count: a bound of counts, if known.
+    See ilpm_kv_copy in include/ilpm.h."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_copy(k_pages, v_pages, src_table, dst_table, src_start, dst_start, counts, path=path,
+                           max_count=max_count)
+    got = _binding.kv_copy(k_pages, v_pages, src_table, dst_table, src_start, dst_start, counts, path, max_count)
+    if type(got) is int:
+        raise IlpmError(got, "ilpm_kv_copy")
     return got

@@ -53,6 +53,18 @@ template <typename T, int N> __device__ inline Pack<T, N> load_loose(const T *p)
 template <typename T, int N> __device__ inline void store_pack(T *p, const Pack<T, N> &v) { store_words<alignof(Pack<T, N>), T, N>(p, v); }
 template <typename T, int N> __device__ inline void store_loose(T *p, const Pack<T, N> &v) { store_words<sizeof(T), T, N>(p, v); }
 
+// Division of 0 <= n < 2^31 by d >= 1 as a product: with 2^(s-1) < d <= 2^s and
+// m = floor(2^32 (2^s - d) / d) + 1, n / d = (floor(n m / 2^32) + n) >> s.
+struct Divisor {
+    unsigned m, s;
+    explicit Divisor(unsigned d) : s(0)
+    {
+        while ((1ull << s) < d) ++s;
+        m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+    }
+    __device__ int of(int n) const { return (int)((__umulhi((unsigned)n, m) + (unsigned)n) >> s); }
+};
+
 // ---- kv_append ----
 struct AppendArgs {
     // rows of heads: [token][head][dim], strides in elements

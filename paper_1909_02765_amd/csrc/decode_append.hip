@@ -11,18 +11,6 @@
 namespace ilpm {
 namespace {
 
-// Division of 0 <= n < 2^31 by d >= 1 as a product: with 2^(s-1) < d <= 2^s and
-// m = floor(2^32 (2^s - d) / d) + 1, n / d = (floor(n m / 2^32) + n) >> s.
-struct Divisor {
-    unsigned m, s;
-    explicit Divisor(unsigned d) : s(0)
-    {
-        while ((1ull << s) < d) ++s;
-        m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
-    }
-    __device__ int of(int n) const { return (int)((__umulhi((unsigned)n, m) + (unsigned)n) >> s); }
-};
-
 // Where a token goes: its page and slot, -1 where it is not written.
 struct Place {
     int page, slot;

@@ -1,0 +1,67 @@
+// What the operators of a drafted decoder step share: their arguments as the
+// kernels take them, and their launchers (the entry points check the
+// arguments, draft_api.hip).
+#pragma once
+
+#include "decode.h"
+
+namespace ilpm {
+
+// ---- kv_append_norm ----
+struct AppendNormArgs {
+    AppendArgs a;  // (positions turn, slots place)
+    const int32_t *slots;
+    const void *q_w, *k_w;
+    int norm;
+    float eps;
+};
+hipError_t append_norm_launch(const AppendNormArgs &n, int x_dtype, int cache_dtype, int param_dtype, hipStream_t stream);
+
+// ---- verify_drafts ----
+constexpr int kVerifyChunk = 4096;  // probabilities that a workgroup sums
+
+// Where a sequence's walk ended, and what is left of that node's row: a p - b q, or p
+// without the tokens gone[0..n_gone).
+struct VerifyEnd {
+    int node, n_gone;  // node -1: no tree
+    double a, b;
+    int gone[ILPM_MAX_NODES];
+};
+struct VerifySum {
+    double left, all;  // of a chunk: of what is left of the row, of the row
+};
+struct VerifyArgs {
+    ilpm_verify_args v;
+    int chunks;  // of a row
+    VerifyEnd *ends;
+    VerifySum *sums;  // [n_seqs][chunks]
+};
+size_t verify_plan(VerifyArgs *a);
+void verify_workspace(VerifyArgs *a, void *ws);
+hipError_t verify_launch(const VerifyArgs &a, hipStream_t stream);
+
+// ---- kv_copy ----
+struct CopyArgs {
+    void *k, *v;
+    int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;  // in bytes
+    int row_bytes, kv_heads, n_pages, page_size;
+    const int32_t *src_table, *dst_table;
+    int64_t src_table_stride, dst_table_stride;
+    int src_max_pages, dst_max_pages, n_seqs;
+    const int32_t *src_start, *dst_start, *counts, *path;
+    int64_t path_stride;
+    int max_count;
+};
+hipError_t copy_launch(const CopyArgs &a, hipStream_t stream);
+
+// ---- attn_tree ----
+struct TreeArgs {
+    AttnArgs a;  // (lengths without the nodes; q_heads, group: of a node)
+    const int32_t *parents;
+    int n_nodes, sinks;
+};
+size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len);
+void tree_workspace(TreeArgs *t, void *ws);
+hipError_t tree_launch(const TreeArgs &t, int cache_dtype, hipStream_t stream);
+
+}  // namespace ilpm
