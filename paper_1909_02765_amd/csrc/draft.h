@@ -55,10 +55,15 @@ struct CopyArgs {
 hipError_t copy_launch(const CopyArgs &a, hipStream_t stream);
 
 // ---- attn_tree ----
+// (Of AttnArgs: lengths without the nodes; group, blocks and part_heads count the rows
+// of a key head, its nodes' heads: row r is head r % group of node r / group.)
 struct TreeArgs {
-    AttnArgs a;  // (lengths without the nodes; q_heads, group: of a node)
+    AttnArgs a;
     const int32_t *parents;
     int n_nodes, sinks;
+    int rows;        // of a key head: n_nodes * group
+    int row_blocks;  // of 16 rows that a workgroup takes
+    bool pieces;     // heads are whole pieces of 16 bytes
 };
 size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len);
 void tree_workspace(TreeArgs *t, void *ws);

@@ -1,0 +1,744 @@
+// attn_tree's kernel: attention of the nodes of drafted trees over a paged
+// cache, in one pass over the keys with the running maximum and sum of the
+// softmax.  A key head's rows are its query heads of all nodes of a sequence.
+//
+// As attn_decode's (decode_attn.h) it runs both products on the matrix cores
+// with keys along their rows, S[key][row] = K Q and O[d][row] = V P, so that
+// probabilities stay in the lane that found them, and a wave takes keys of its
+// own.  Here a wave holds several blocks of 16 rows: a tile of 16 keys is
+// loaded once, and its V operands are put together once, for all of them.
+//
+// Which keys a row sees differs between the rows only where nodes lie, and
+// where a window begins; tiles that hold neither go without a test for each
+// row.  In the others a value that is not finite must not reach a row that does
+// not see its key (0 times it is NaN): there such values are taken out of the
+// product, and the rows that see them get NaN by a product of flags.
+#pragma once
+
+#include "decode_attn.h"
+#include "draft.h"
+
+namespace ilpm {
+namespace {
+
+// The nodes that each node sees (itself and those above it), as bits; 0: no
+// node.  Lane i holds node i.  Whoever is above whom is followed by doubling.
+__device__ inline unsigned long long seen_nodes(int parent, int lane, int n)
+{
+    bool ok = lane < n && parent >= -1 && parent < lane;
+    int up = ok ? parent : -1;
+    unsigned lo = lane < 32 ? 1u << lane : 0, hi = lane >= 32 ? 1u << (lane - 32) : 0;
+#pragma unroll 1
+    for (int d = 1; d < n; d <<= 1) {
+        const int from = up < 0 ? lane : up;
+        const unsigned l = __shfl(lo, from), h = __shfl(hi, from);
+        const int u = __shfl(up, from), k = __shfl((int)ok, from);
+        lo |= l;
+        hi |= h;
+        ok = ok && k;
+        up = up < 0 ? -1 : u;
+    }
+    return ok ? (unsigned long long)hi << 32 | lo : 0ull;
+}
+
+// The keys of a sequence that any of its nodes may see: the first `sinks` of
+// them, and [first, end); the nodes begin at `length`.
+struct TreeRange {
+    int64_t length;
+    int sinks, first, end;
+};
+
+__device__ inline TreeRange tree_range(const TreeArgs &t, int length)
+{
+    const AttnArgs &a = t.a;
+    TreeRange r;
+    r.length = max(length, 0);
+    r.end = (int)min((int64_t)a.capacity, r.length + t.n_nodes);
+    r.first = a.window > 0 ? (int)min((int64_t)r.end, max((int64_t)0, r.length + 1 - a.window)) : 0;
+    r.sinks = min(t.sinks, r.first);
+    if (r.sinks >= r.first - 15) r.sinks = r.first = 0;  // (they would share a tile)
+    return r;
+}
+
+__device__ inline int tree_tiles(const TreeArgs &t, int length)
+{
+    const TreeRange r = tree_range(t, length);
+    return max(1, (r.sinks + 15) / 16 + (int)(((unsigned)(r.end - r.first) + 15) / 16));
+}
+
+// N elements of a row from element d on, as load_row (decode_attn.h) takes them but
+// in pieces of any alignment: kPieces for head sizes of whole pieces.
+template <typename T, int N, Rows R, bool ZERO> __device__ inline Words<sizeof(T) * N> load_piece(const T *row, int d, int dim)
+{
+    using W = Words<sizeof(T) * N>;
+    if constexpr (R == kAny) return load_row<T, N, kAny, ZERO>(row, d, dim);
+    const T *at = d < dim ? row + d : ZERO ? (const T *)&attn_zeros : row;
+    return __builtin_bit_cast(W, load_loose<T, N>(at));
+}
+
+// A head size's class, and what of AttnKernel's does not hold here.
+template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeKernel : AttnKernel<TC, Q16, DC, R, false> {
+    using Base = AttnKernel<TC, Q16, DC, R, false>;
+    static constexpr int ROWS = 16 * MA;
+    // Workgroups that a compute unit holds at once.
+    static constexpr int PER_CU = DC >= 192 ? 1 : 2;
+};
+
+template <typename Cfg, int MA> struct TreeLds {
+    Places places[4][2];
+    FindShare found;
+    // Of each row: the nodes that it sees, and the first place (a row of no node: 0 bits).
+    unsigned long long bits[16 * MA];
+    int low[16 * MA];
+    float unscale[16 * MA];
+    int top_low;  // the largest of low
+    union {
+        // The queries, as the lanes of the first product take them, in parts those of 32 bits.
+        Words16 q[Cfg::QP][Cfg::NK][MA][64];
+        // Of 16 rows each wave's maxima, sums and outputs (the rows 4 banks apart).
+        struct {
+            float o[4][16][Cfg::DO + 4];
+            float m[4][16], l[4][16];
+        } j;
+    };
+};
+
+// A unit's tiles [tile0, tile1), as a workgroup takes them.
+struct TreeSegment {
+    int seq, kvh, block;
+    int tile0, tile1;
+    TreeRange range;
+};
+
+// Where row r of a segment's block lies in q, out and lse: its sequence's node and head.
+__device__ inline int row_in_unit(const TreeSegment &seg, int rows_of_block, int r) { return seg.block * rows_of_block + r; }
+
+// Rows' bits and lows, and the queries in their layout, into LDS.
+template <typename TC, bool Q16, int DC, Rows R, int MA, typename Lds>
+__device__ __forceinline__ void tree_rows(const TreeArgs &t, const TreeSegment &seg, Lds &lds)
+{
+    using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
+    using TQ = std::conditional_t<Q16, TC, float>;
+    constexpr int KV = Cfg::KV, NK = Cfg::NK, QP = Cfg::QP;
+    const AttnArgs &a = t.a;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), n16 = lane & 15, g = lane >> 4;
+    if (wave == 0) {
+        unsigned long long bits = seen_nodes(lane < t.n_nodes ? t.parents[(int64_t)seg.seq * t.n_nodes + lane] : -2, lane, t.n_nodes);
+        const int depth = __builtin_popcountll(bits) - 1;
+        int low = 0;
+        if (a.window > 0) {
+            const unsigned long long above = bits;
+            for (int n = 0; n < t.n_nodes; ++n) {
+                const int dn = __builtin_amdgcn_readlane(depth, n);
+                if (((above >> n) & 1) && depth - dn >= a.window && seg.range.length + dn >= t.sinks) bits &= ~(1ull << n);
+            }
+            low = (int)min((int64_t)INT_MAX, max((int64_t)0, seg.range.length + depth + 1 - a.window));
+        }
+        int top = low;
+#pragma unroll 1
+        for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
+        if (lane == 0) lds.top_low = top;
+        for (int r0 = 0; r0 < 16 * MA; r0 += 64) {
+            const int r = r0 + lane, row = row_in_unit(seg, 16 * MA, r), node = min(row / a.group, t.n_nodes - 1);
+            const unsigned b0 = __shfl((unsigned)bits, node), b1 = __shfl((unsigned)(bits >> 32), node);
+            const int l = __shfl(low, node);
+            if (r < 16 * MA) {
+                lds.bits[r] = row < t.rows ? (unsigned long long)b1 << 32 | b0 : 0ull;
+                lds.low[r] = l;
+            }
+        }
+    }
+    // Wave w takes block w % MA, and of it every (4 / MA)-th piece.
+    constexpr int STEP = 4 / MA;
+    const int ma = wave % MA, c0 = wave / MA;
+    const int in_unit = min(row_in_unit(seg, 16 * MA, ma * 16 + n16), t.rows - 1), node = in_unit / a.group;
+    const TQ *row = (const TQ *)a.q + ((int64_t)seg.seq * t.n_nodes + node) * a.q_row +
+                    ((int64_t)seg.kvh * a.group + (in_unit - node * a.group)) * a.q_head;
+    if constexpr (QP == 1) {
+#pragma unroll 2
+        for (int c = c0; c < NK; c += STEP)
+            lds.q[0][c][ma][lane] = load_piece<TQ, KV, R, true>(row, (g + 4 * c) * KV, a.dim);
+    } else {
+        struct Values {
+            float v[KV];
+        };
+        auto get = [&](int c) {  // KV = 8 values: two pieces of four
+            struct Halves {
+                Words16 w[2];
+            } h;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int d = (g + 4 * c) * KV + 4 * n;
+                h.w[n] = load_piece<float, 4, R, true>(row, d, a.dim);
+            }
+            return __builtin_bit_cast(Values, h);
+        };
+        float f = 1.f, back = 1.f;
+        if constexpr (__is_same(TC, _Float16)) {
+            // The largest becomes 2^14 to 2^15: parts keep what is above 2^-39 of it.
+            float most = 0.f;
+#pragma unroll 2
+            for (int c = 0; c < NK; ++c) {
+                const Values p = get(c);
+#pragma unroll
+                for (int i = 0; i < KV; ++i) most = fmaxf(most, fabsf(p.v[i]));
+            }
+            most = max_of_head(most);
+            const int e = (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127;  // 2^e <= most < 2^(e+1)
+            const int by = most > 0.f && e < 128 ? min(14 - e, 126) : 0;
+            f = __builtin_ldexpf(1.f, by);
+            back = __builtin_ldexpf(1.f, -by);
+        }
+        if (c0 == 0 && g == 0) lds.unscale[ma * 16 + n16] = back;
+#pragma unroll 2
+        for (int c = c0; c < NK; c += STEP) {
+            const Values p = get(c);
+            Pack<TC, KV> part[3];
+#pragma unroll
+            for (int i = 0; i < KV; ++i) {
+                float v = p.v[i] * f;
+                if constexpr (__is_same(TC, __bf16)) {
+                    // (Cut off, not rounded: see decode_attn.h.)
+                    v = __builtin_canonicalizef(v);
+                    part[0].v[i] = __builtin_bit_cast(__bf16, (unsigned short)(__builtin_bit_cast(unsigned, v) >> 16));
+                } else {
+                    part[0].v[i] = (TC)v;
+                }
+                v -= (float)part[0].v[i];
+                part[1].v[i] = (TC)v;
+                part[2].v[i] = (TC)(v - (float)part[1].v[i]);
+            }
+#pragma unroll
+            for (int n = 0; n < 3; ++n) lds.q[n][c][ma][lane] = __builtin_bit_cast(Words16, part[n]);
+        }
+    }
+    __syncthreads();
+}
+
+template <typename TC> __device__ inline floatx4 mfma_values32(Words16 v, Words16 p, floatx4 c) { return mfma_scores<TC>(v, p, c); }
+
+// Of a word of two 16-bit values, ones in the places of those that are not finite.
+template <typename TC> __device__ inline unsigned not_finite(unsigned w)
+{
+    constexpr unsigned E = __is_same(TC, __bf16) ? 0x7f80u : 0x7c00u;
+    return ((w & E) == E ? 0xffffu : 0u) | ((w & (E << 16)) == (E << 16) ? 0xffff0000u : 0u);
+}
+template <typename TC> constexpr unsigned kOnes = __is_same(TC, __bf16) ? 0x3f803f80u : 0x3c003c00u;
+
+// A wave's part of a segment, every fourth tile of it, and the join of the
+// four waves' parts, 16 rows at a time.
+template <typename TC, bool Q16, int DC, Rows R, int MA, typename Put>
+__device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegment &seg, TreeLds<TreeKernel<TC, Q16, DC, R, MA>, MA> &lds, Put put)
+{
+    using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
+    constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
+    constexpr int QP = Cfg::QP, PP = Cfg::PP;
+    constexpr bool C16 = Cfg::C16;
+    const AttnArgs &a = t.a;
+
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int wave = uniform((int)(threadIdx.x >> 6));
+    const int n16 = lane & 15, g = lane >> 4;
+    const int seq = seg.seq;
+    const TreeRange range = seg.range;
+    const int sink_tiles = (range.sinks + 15) / 16;
+    // Tile j of this wave is tile 4j + wave of the segment.
+    const int tiles = max(0, (seg.tile1 - seg.tile0 - wave + 3) / 4);
+    auto start_of = [&](int tile) { return tile < sink_tiles ? tile * 16 : range.first + (tile - sink_tiles) * 16; };
+
+    // Lane (n, g) looks up key n of tile 4*group + g.
+    struct Entry {
+        int page, slot;
+    };
+    auto look_up = [&](int group) {
+        Entry e = {-1, 0};
+        const int tile = seg.tile0 + (group * 4 + g) * 4 + wave;
+        const int64_t key = (int64_t)start_of(tile) + n16;
+        if (tile < seg.tile1 && key < (tile < sink_tiles ? range.sinks : range.end)) {
+            const int p = (int)key / a.page_size;
+            e.slot = (int)key - p * a.page_size;
+            e.page = a.table[(int64_t)seq * a.table_stride + p];
+            if (a.mask && (key >= a.mask_len || !a.mask[(int64_t)seq * a.mask_stride + key])) e.page = -1;
+        }
+        return e;
+    };
+    auto place = [&](int group, Entry e) {
+        const bool ok = e.page >= 0 && e.page < a.n_pages;
+        Places &p = lds.places[wave][group & 1];
+        p.k[lane] = ok ? (int64_t)e.page * a.k_page + (int64_t)e.slot * a.k_slot : -1;
+        p.v[lane] = ok ? (int64_t)e.page * a.v_page + (int64_t)e.slot * a.v_slot : -1;
+        // (Only this wave reads them, and a wave's LDS accesses keep their order.)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    const TC *kh = (const TC *)a.k + (int64_t)seg.kvh * a.k_head;
+    const TC *vh = (const TC *)a.v + (int64_t)seg.kvh * a.v_head;
+    Words16 kt[NK];
+    Words<sizeof(TC) * VV> vt[4][NV];
+    bool seen[4];
+    // A key that is not seen reads the pool's first row, and none of it is used.
+    auto load_k = [&](int j) {
+        const int64_t at = lds.places[wave][(j >> 2) & 1].k[(j & 3) * 16 + n16];
+        const TC *row = kh + (j < tiles ? max(at, (int64_t)0) : 0);
+#pragma unroll
+        for (int c = 0; c < NK; ++c) kt[c] = load_piece<TC, KV, R, true>(row, (g + 4 * c) * KV, a.dim);
+    };
+    auto load_v = [&](int j) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t at = lds.places[wave][(j >> 2) & 1].v[(j & 3) * 16 + 4 * g + r];
+            seen[r] = at >= 0;
+            const TC *row = vh + (j < tiles ? max(at, (int64_t)0) : 0);
+#pragma unroll
+            for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
+                vt[r][c] = load_piece<TC, VV, R, false>(row, (n16 + 16 * c) * VV, a.dim);
+        }
+    };
+
+    Entry e0 = {}, next = {};
+    if (tiles > 0) e0 = look_up(0);
+    if (tiles > 4) next = look_up(1);
+    tree_rows<TC, Q16, DC, R, MA>(t, seg, lds);
+    if (tiles > 0) place(0, e0);
+
+    floatx4 o[MA][NO];
+    float m[MA], l[MA];
+#pragma unroll
+    for (int ma = 0; ma < MA; ++ma) {
+        m[ma] = -INFINITY;
+        l[ma] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) o[ma][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float scale2 = a.softcap > 0.f ? a.scale / a.softcap : a.scale * kLog2e;
+    const float cap2 = a.softcap * kLog2e;
+    const int top_low = uniform(lds.top_low);
+
+    // Selectors that put rows' 16-bit values together; 0 for those of keys that are not seen.
+    auto values = [&](int c, int i, const unsigned *lower, const unsigned *upper) {
+        return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], i & 1 ? upper[0] : lower[0]),
+                        __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], i & 1 ? upper[1] : lower[1])};
+    };
+    // Whether row (ma, n16) sees key j, which is in the cache.
+    auto sees = [&](int ma, int64_t j) {
+        const int r = ma * 16 + n16;
+        if (j >= range.length) return ((lds.bits[r] >> min(j - range.length, (int64_t)63)) & 1) != 0;
+        return j >= lds.low[r] || j < t.sinks;
+    };
+    // Takes values that are not finite out of a tile whose rows do not see the same keys, and gives NaN to the rows
+    // that see them.  (Hardly ever: no need for it to be fast.)
+    auto take_out = [&](int64_t key0) {
+        bool any = false;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                if constexpr (C16) {
+#pragma unroll
+                    for (int i = 0; i < VV / 2; ++i) any |= seen[r] && not_finite<TC>(vt[r][c][i]) != 0;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VV; ++i) any |= seen[r] && (vt[r][c][i] & 0x7f800000u) == 0x7f800000u;
+                }
+            }
+        if (!__builtin_amdgcn_ballot_w64(any)) return;
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) {
+            bool s[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[r] = seen[r] && sees(ma, key0 + 4 * g + r);
+            if constexpr (C16) {
+                unsigned lower[2], upper[2];
+                Words<8> ones;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const unsigned keep = (seen[2 * h] ? 0xffffu : 0u) | (seen[2 * h + 1] ? 0xffff0000u : 0u);
+                    lower[h] = (0x05040100u & keep) | (0x0c0c0c0cu & ~keep);
+                    upper[h] = (0x07060302u & keep) | (0x0c0c0c0cu & ~keep);
+                    ones[h] = kOnes<TC> & ((s[2 * h] ? 0xffffu : 0u) | (s[2 * h + 1] ? 0xffff0000u : 0u));
+                }
+#pragma unroll
+                for (int c = 0; c < NV; ++c)
+#pragma unroll
+                    for (int i = 0; i < VV; ++i) {
+                        Words<8> v = values(c, i, lower, upper);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) v[h] = not_finite<TC>(v[h]) & kOnes<TC>;
+                        const floatx4 n = mfma_values<TC>(v, ones, floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[ma][c * VV + i][r] += n[r] > 0.f ? __builtin_nanf("") : 0.f;
+                    }
+            } else {
+#pragma unroll
+                for (int c = 0; c < NV; ++c)
+#pragma unroll
+                    for (int i = 0; i < VV; ++i) {
+                        floatx4 n = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            n = __builtin_amdgcn_mfma_f32_16x16x4f32(seen[r] && (vt[r][c][i] & 0x7f800000u) == 0x7f800000u ? 1.f : 0.f,
+                                                                     s[r] ? 1.f : 0.f, n, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[ma][c * VV + i][r] += n[r] > 0.f ? __builtin_nanf("") : 0.f;
+                    }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                if constexpr (C16) {
+#pragma unroll
+                    for (int i = 0; i < VV / 2; ++i) vt[r][c][i] &= ~not_finite<TC>(vt[r][c][i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VV; ++i) vt[r][c][i] = (vt[r][c][i] & 0x7f800000u) == 0x7f800000u ? 0u : vt[r][c][i];
+                }
+            }
+    };
+
+    if (tiles > 0) {
+        load_k(0);
+        load_v(0);
+    }
+#pragma unroll 1
+    for (int j = 0; j < tiles; ++j) {
+        if ((j & 3) == 2 && j + 2 < tiles) {
+            place(j / 4 + 1, next);
+            if (j + 6 < tiles) next = look_up(j / 4 + 2);
+        }
+        const int tile = seg.tile0 + 4 * j + wave;
+        const int64_t key0 = start_of(tile);
+        const bool special = key0 + 15 >= range.length || (tile >= sink_tiles && key0 < top_low);
+
+        // The scores of all rows, then the next tile's keys are on their way.
+        floatx4 s[MA];
+        int ql = lane;
+        asm volatile("" : "+v"(ql));  // (read for each tile, not kept)
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) {
+            floatx4 x = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (!C16) {
+#pragma unroll
+                for (int c = 0; c < NK; ++c) {
+                    const floatx4 q = __builtin_bit_cast(floatx4, lds.q[0][c][ma][ql]);
+#pragma unroll
+                    for (int i = 0; i < KV; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, kt[c])[i], q[i], x, 0, 0, 0);
+                }
+            } else {
+                floatx4 low = x;
+#pragma unroll
+                for (int c = 0; c < NK; ++c) {
+                    x = mfma_scores<TC>(kt[c], lds.q[0][c][ma][ql], x);
+                    if constexpr (QP == 3) {
+                        low = mfma_scores<TC>(kt[c], lds.q[1][c][ma][ql], low);
+                        low = mfma_scores<TC>(kt[c], lds.q[2][c][ma][ql], low);
+                    }
+                }
+                if constexpr (QP == 3) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] += low[r] - low[r] == 0.f ? low[r] : 0.f;
+                }
+            }
+            s[ma] = x;
+        }
+        load_k(j + 1);
+
+        if (special) take_out(key0);
+        constexpr int PW = !C16 ? 4 : PP == 3 ? 6 : 4;
+        unsigned part[MA][PW];  // probabilities: hi and lo of four keys, a third part; or 32 bits
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) {
+            float x[4], top = -INFINITY;
+            const float by = QP == 3 ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] = s[ma][r] * by;
+                if (a.softcap > 0.f) x[r] = cap2 * tanh_of(x[r]);
+                x[r] = seen[r] ? x[r] : -INFINITY;
+            }
+            if (special) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = sees(ma, key0 + 4 * g + r) ? x[r] : -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, x[r]);
+            if (__builtin_amdgcn_ballot_w64(top > m[ma])) {  // (most tiles leave all maxima where they are)
+                const float m_new = fmaxf(m[ma], max_of_head(top));
+                const float alpha = __builtin_amdgcn_exp2f(m[ma] - (m_new == -INFINITY ? 0.f : m_new));
+                m[ma] = m_new;
+                l[ma] *= alpha;
+#pragma unroll
+                for (int i = 0; i < NO; ++i) o[ma][i] *= alpha;
+            }
+            const float base = m[ma] == -INFINITY ? 0.f : m[ma];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(x[r] - base);
+            l[ma] += (x[0] + x[1]) + (x[2] + x[3]);
+            if constexpr (!C16) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) part[ma][r] = __builtin_bit_cast(unsigned, x[r]);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[r] *= Cfg::UP;
+                    if constexpr (Cfg::UP != 1.f) asm("" : "+v"(x[r]));  // (one product, not one for each of its uses)
+                }
+#pragma unroll
+                for (int i = 0; i < PP; ++i) {
+                    Pack<TC, 4> h;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        h.v[r] = (TC)x[r];
+                        x[r] -= (float)h.v[r];
+                    }
+                    const Words<8> w = __builtin_bit_cast(Words<8>, h);
+                    part[ma][2 * i] = w[0];
+                    part[ma][2 * i + 1] = w[1];
+                }
+            }
+        }
+
+        if constexpr (!C16) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < NV; ++c)
+#pragma unroll
+                    for (int i = 0; i < VV; ++i) {
+                        const float v = seen[r] ? __builtin_bit_cast(floatx4, vt[r][c])[i] : 0.f;
+#pragma unroll
+                        for (int ma = 0; ma < MA; ++ma)
+                            o[ma][c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __builtin_bit_cast(float, part[ma][r]), o[ma][c * VV + i], 0, 0, 0);
+                    }
+        } else {
+            // Selectors of the lower and the upper halves of two rows' registers: a byte 0x0c gives 0.
+            unsigned lower[2], upper[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned keep = (seen[2 * h] ? 0xffffu : 0u) | (seen[2 * h + 1] ? 0xffff0000u : 0u);
+                lower[h] = (0x05040100u & keep) | (0x0c0c0c0cu & ~keep);
+                upper[h] = (0x07060302u & keep) | (0x0c0c0c0cu & ~keep);
+            }
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int i = 0; i < VV; ++i) {
+                    const Words<8> v = values(c, i, lower, upper);
+                    // The same four keys twice, against the first and second parts of their probabilities.
+                    const Words16 vv = {v[0], v[1], v[0], v[1]};
+#pragma unroll
+                    for (int ma = 0; ma < MA; ++ma) {
+                        floatx4 &sum = o[ma][c * VV + i];
+                        sum = mfma_values32<TC>(vv, Words16{part[ma][0], part[ma][1], part[ma][2], part[ma][3]}, sum);
+                        // (By the same instruction: one of 16x16x16 right after it, on the same registers, found them as
+                        // they were before it.)
+                        if constexpr (PP == 3) sum = mfma_values32<TC>(vv, Words16{part[ma][4], part[ma][5], 0u, 0u}, sum);
+                    }
+                }
+        }
+        load_v(j + 1);
+    }
+
+    // Join the waves: lane (n, g) holds values (4g + r + 16c) * VV + i of row n.
+#pragma unroll
+    for (int ma = 0; ma < MA; ++ma) {
+        float sum = l[ma];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        __syncthreads();  // the queries, or what the last rows left, have been read
+        const bool real = lds.bits[ma * 16 + n16] != 0;  // (what is no node has seen keys of the sequence: none counts)
+        if (g == 0) {
+            lds.j.m[wave][n16] = real ? m[ma] : -INFINITY;
+            lds.j.l[wave][n16] = real ? sum : 0.f;
+        }
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                Pack<float, VV> p;
+#pragma unroll
+                for (int i = 0; i < VV; ++i) p.v[i] = real ? o[ma][c * VV + i][r] : 0.f;
+                *reinterpret_cast<Pack<float, VV> *>(&lds.j.o[wave][n16][(4 * g + r + 16 * c) * VV]) = p;
+            }
+        __syncthreads();
+        constexpr int PER = DC / 4;
+        const int row0 = row_in_unit(seg, 16 * MA, ma * 16), rows = min(16, t.rows - row0);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < rows * PER; i += 256) {
+            const int r = i / PER, d = (i - r * PER) * 4;
+            if (d >= a.dim) continue;
+            floatx4 v[4];
+            float mw[4], lw[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                v[w] = *reinterpret_cast<const floatx4 *>(&lds.j.o[w][r][d]);
+                mw[w] = lds.j.m[w][r];
+                lw[w] = lds.j.l[w][r];
+            }
+            const float top = fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3])), base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = __builtin_amdgcn_exp2f(mw[w] - base);
+                v[w] *= f;
+                lw[w] *= f;
+            }
+            put(row0 + r, ma * 16 + r, d, (v[0] + v[1]) + (v[2] + v[3]), top, (lw[0] + lw[1]) + (lw[2] + lw[3]));
+        }
+    }
+}
+
+template <typename TC, bool Q16, int DC, Rows R, int MA>
+__global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void tree_split(TreeArgs t)
+{
+    using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
+    using TQ = std::conditional_t<Q16, TC, float>;
+    __shared__ TreeLds<Cfg, MA> lds;
+    const AttnArgs &a = t.a;
+
+    // (Neighbouring shares stay on one die: see decode_attn.h.)
+    const int die = blockIdx.x & 7, dies = gridDim.x >> 3;
+    const int units = units_of(a), wg = die * dies + min(die, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
+    Share share = {0, 0, true};
+    Begin begin;
+    if (a.split) share = find_share(a, wg, lds.found, &begin, [&](int n) { return tree_tiles(t, n); });
+
+    // This workgroup's place: a sequence, its length and its units' tiles, a unit
+    // of it, and how far into the unit's length the share has come.
+    int seq, length, unit, tiles_all, x0 = 0;
+    int at = 0, last = 0;
+    if (a.split && !a.part_of_unit && threadIdx.x == 0) a.parts[wg] = AttnPart{0, 0, 0, 0};  // (whatever follows, the join reads it)
+    if (share.whole) {
+        if (wg >= a.n_seqs * units) return;
+        seq = wg / units;
+        unit = wg - seq * units;
+        length = uniform(a.lengths[seq]);
+        tiles_all = tree_tiles(t, length);
+    } else {
+        if ((int64_t)wg * share.size >= share.total) return;
+        at = wg * share.size;
+        last = (int)min((int64_t)at + share.size, (int64_t)share.total);
+        seq = begin.seq;
+        length = begin.length;
+        tiles_all = tree_tiles(t, length);
+        const int in = at - begin.before;
+        unit = in / (tiles_all + kUnitCost);
+        x0 = in - unit * (tiles_all + kUnitCost);
+    }
+
+    for (;;) {
+        const int x1 = share.whole ? tiles_all + kUnitCost : min(tiles_all + kUnitCost, x0 + (last - at));
+        const int tile0 = max(0, x0 - kUnitCost), seg_tiles = max(0, x1 - kUnitCost) - tile0;
+        if (seg_tiles == 0) return;  // the share ends before the unit's first tile
+        TreeSegment seg;
+        seg.seq = seq;
+        seg.kvh = unit / a.blocks;
+        seg.block = unit - seg.kvh * a.blocks;
+        seg.tile0 = tile0;
+        seg.tile1 = tile0 + seg_tiles;
+        seg.range = tree_range(t, length);
+        if (seg.range.end == 0) seg.tile1 = tile0;  // (no keys, and perhaps no pool)
+        const bool all = seg_tiles == tiles_all;  // of the unit's tiles
+        // The part that begins a unit, or the one that goes on with it.
+        const int64_t part = ((int64_t)wg * 2 + (tile0 == 0 ? 1 : 0)) * a.part_heads;
+        tree_segment<TC, Q16, DC, R, MA>(t, seg, lds, [&](int row, int r, int d, floatx4 v, float top, float sum) {
+            auto put = [&](auto *to) {
+                using TO = std::remove_reference_t<decltype(*to)>;
+                Pack<TO, 4> p;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) p.v[k] = (TO)v[k];
+                if (d + 4 <= a.dim) {
+                    store_loose<TO, 4>(to + d, p);
+                    return;
+                }
+                to[d] = p.v[0];
+                if (d + 1 < a.dim) to[d + 1] = p.v[1];
+                if (d + 2 < a.dim) to[d + 2] = p.v[2];
+            };
+            if (all) {
+                const int node = row / a.group, head = seg.kvh * a.group + (row - node * a.group);
+                const int64_t at_row = (int64_t)seq * t.n_nodes + node;
+                v *= sum == 0.f ? 0.f : 1.f / (sum * Cfg::UP);
+                put((TQ *)a.out + at_row * a.o_row + (int64_t)head * a.o_head);
+                if (d == 0 && a.lse) a.lse[at_row * a.q_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+            } else {
+                v *= 1.f / Cfg::UP;
+                put(a.part_o + (part + r) * a.dim);
+                if (d == 0) {
+                    a.part_ml[(part + r) * 2] = top;
+                    a.part_ml[(part + r) * 2 + 1] = sum;
+                }
+            }
+        });
+        // Who begins a unit says whether others go on with it.
+        if (a.split && threadIdx.x == 0 && tile0 == 0) {
+            const int rest = tiles_all - seg_tiles;
+            const int count = all ? 0 : 1 + (int)(((unsigned)rest + share.size - 1) / (unsigned)share.size);
+            if (a.part_of_unit) a.parts[seq * units + unit] = AttnPart{seq, unit, wg, count};
+            else if (!all) a.parts[wg] = AttnPart{seq, unit, wg, count};
+        }
+        __syncthreads();  // the LDS that the next unit's waves write has been read
+        if (share.whole) {
+            const int u = seq * units + unit + (int)gridDim.x;
+            if (!a.split || u >= a.n_seqs * units) return;
+            seq = u / units;
+            unit = u - seq * units;
+            length = uniform(a.lengths[seq]);
+            tiles_all = tree_tiles(t, length);
+            continue;
+        }
+        at += x1 - x0;
+        if (at >= last) return;
+        x0 = 0;
+        if (++unit == units) {
+            unit = 0;
+            length = uniform(a.lengths[++seq]);
+            tiles_all = tree_tiles(t, length);
+        }
+    }
+}
+
+// The largest number of row blocks of a workgroup for a class.
+template <typename TC, int DC> constexpr int kMostBlocks = sizeof(TC) == 4 ? (DC <= 128 ? 2 : 1) : DC <= 128 ? 4 : 2;
+
+template <typename TC, bool Q16, int DC> hipError_t tree_split_launch(const TreeArgs &t, hipStream_t stream)
+{
+    auto launch = [&](auto rows, auto blocks) {
+        hipLaunchKernelGGL((tree_split<TC, Q16, DC, decltype(rows)::value, decltype(blocks)::value>), dim3(t.a.grid), dim3(256), 0, stream, t);
+        return hipGetLastError();
+    };
+    constexpr int MOST = kMostBlocks<TC, DC>;
+    constexpr std::integral_constant<Rows, kPieces> pieces{};
+    if (!t.pieces) return launch(std::integral_constant<Rows, kAny>{}, std::integral_constant<int, 1>{});
+    if constexpr (MOST >= 4)
+        if (t.row_blocks == 4) return launch(pieces, std::integral_constant<int, 4>{});
+    if constexpr (MOST >= 2)
+        if (t.row_blocks == 2) return launch(pieces, std::integral_constant<int, 2>{});
+    return launch(pieces, std::integral_constant<int, 1>{});
+}
+
+template <typename TC, bool Q16> hipError_t tree_split_by_dim(const TreeArgs &t, hipStream_t stream)
+{
+    if (t.a.dim <= 64) return tree_split_launch<TC, Q16, 64>(t, stream);
+    if (t.a.dim <= 96) return tree_split_launch<TC, Q16, 96>(t, stream);
+    if (t.a.dim <= 128) return tree_split_launch<TC, Q16, 128>(t, stream);
+    if (t.a.dim <= 192) return tree_split_launch<TC, Q16, 192>(t, stream);
+    return tree_split_launch<TC, Q16, 256>(t, stream);
+}
+
+// Of a head size's class: the most row blocks of a workgroup, and the
+// workgroups that the card holds at once.
+template <typename TC, bool Q16> int tree_most_by_dim(int dim)
+{
+    return dim <= 64 ? kMostBlocks<TC, 64> : dim <= 96 ? kMostBlocks<TC, 96> : dim <= 128 ? kMostBlocks<TC, 128> : dim <= 192 ? kMostBlocks<TC, 192> : kMostBlocks<TC, 256>;
+}
+template <typename TC, bool Q16> int tree_card_by_dim(int dim, int blocks)
+{
+    (void)blocks;
+    return kAttnCus * (dim <= 128 ? 2 : 1);
+}
+
+}  // namespace
+}  // namespace ilpm

@@ -1,124 +1,154 @@
-// attn_tree: attention of drafted nodes over a paged cache and the nodes above
-// them.
+// attn_tree: how a call is shared out over the card, and the join of units that
+// span workgroups (the kernel over the keys is in draft_attn.h).
+#include <algorithm>
 #include <climits>
 
 #include "draft.h"
 
 namespace ilpm {
+
+#define ILPM_TREE_KERNELS(name)                                          \
+    hipError_t tree_split_##name(const TreeArgs &t, hipStream_t stream); \
+    int tree_most_##name(int dim);                                       \
+    int tree_card_##name(int dim, int blocks);
+ILPM_TREE_KERNELS(f32)
+ILPM_TREE_KERNELS(f16)
+ILPM_TREE_KERNELS(f16_q32)
+ILPM_TREE_KERNELS(bf16)
+ILPM_TREE_KERNELS(bf16_q32)
+#undef ILPM_TREE_KERNELS
+
 namespace {
 
-// The nodes that each node sees (itself and those above it), as bits; 0: no
-// node.  Lane i holds node i.  Whoever is above whom is followed by doubling.
-__device__ inline unsigned long long seen_nodes(int parent, int lane, int n)
-{
-    bool ok = lane < n && parent >= -1 && parent < lane;
-    int up = ok ? parent : -1;
-    unsigned lo = lane < 32 ? 1u << lane : 0, hi = lane >= 32 ? 1u << (lane - 32) : 0;
-#pragma unroll 1
-    for (int d = 1; d < 64; d <<= 1) {
-        const int from = up < 0 ? lane : up;
-        const unsigned l = __shfl(lo, from), h = __shfl(hi, from);
-        const int u = __shfl(up, from), k = __shfl((int)ok, from);
-        lo |= l;
-        hi |= h;
-        ok = ok && k;
-        up = up < 0 ? -1 : u;
-    }
-    return ok ? (unsigned long long)hi << 32 | lo : 0ull;
-}
+constexpr int kMaxParts = 4 * kAttnCus;  // of a unit: workgroups of a call
+constexpr float kLn2 = 0.69314718055994530942f;
 
-__device__ inline float read_any(const void *p, int64_t i, int dtype)
-{
-    if (dtype == ILPM_F32) return ((const float *)p)[i];
-    if (dtype == ILPM_F16) return (float)((const _Float16 *)p)[i];
-    return (float)((const __bf16 *)p)[i];
-}
-__device__ inline void write_any(void *p, int64_t i, int dtype, float v)
+__device__ inline void store_f32(void *p, int64_t i, int dtype, float v)
 {
     if (dtype == ILPM_F32) ((float *)p)[i] = v;
     else if (dtype == ILPM_F16) ((_Float16 *)p)[i] = (_Float16)v;
     else ((__bf16 *)p)[i] = (__bf16)v;
 }
 
-// One workgroup for a head of a node, a key a thread and step.
-__global__ __launch_bounds__(256) void tree_plain(TreeArgs t, int cache_dtype)
+// Joins the parts of the unit at place blockIdx.x, for its row blockIdx.y and 64
+// values of it, blockIdx.z, as attn_decode's parts are (attn_join).
+template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
 {
-    __shared__ float query[256], probs[256], red[4];
-    __shared__ int64_t rows[256];
+    constexpr int T = 64 / V, G = 256 / T, AHEAD = 4, OWN = kMaxParts / 256;
+    __shared__ float red[2][4], w[kMaxParts];
+    __shared__ Pack<float, V> sum[G][T];
     const AttnArgs &a = t.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int head = blockIdx.x % a.q_heads, row = blockIdx.x / a.q_heads, seq = row / t.n_nodes, node = row - seq * t.n_nodes;
-    const int kvh = head / a.group;
-    const unsigned long long bits = seen_nodes(lane < t.n_nodes ? t.parents[(int64_t)seq * t.n_nodes + lane] : -2, lane, t.n_nodes);
-    const int my_depth = __builtin_popcountll(bits) - 1;
-    const unsigned long long above = __shfl(bits, node);
-    const int depth = __shfl(my_depth, node);
-    const int64_t length = max(a.lengths[seq], 0), place = length + depth;
-    for (int d = tid; d < a.dim; d += 256) query[d] = read_any(a.q, (int64_t)row * a.q_row + (int64_t)head * a.q_head + d, a.q_dtype);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    const int64_t end = above ? min((int64_t)a.capacity, length + t.n_nodes) : 0;
-    for (int64_t k0 = 0; k0 < end; k0 += 256) {
-        const int64_t key = k0 + tid;
-        bool seen = key < end;
-        int64_t at = key;
-        const int n = (int)min(max(key - length, (int64_t)0), (int64_t)63), dn = __shfl(my_depth, n);  // (lanes' nodes differ: all take part)
-        if (seen && key >= length) {
-            seen = (above >> (key - length)) & 1;
-            at = length + dn;
-        }
-        if (a.window > 0 && at <= place - a.window && at >= t.sinks) seen = false;
-        float x = -INFINITY;
-        int64_t page = -1, slot = 0;
-        if (seen) {
-            const int p = (int)(key / a.page_size);
-            slot = key - (int64_t)p * a.page_size;
-            page = a.table[(int64_t)seq * a.table_stride + p];
-            if (page < 0 || page >= a.n_pages) seen = false;
-            if (a.mask && (key >= a.mask_len || !a.mask[(int64_t)seq * a.mask_stride + key])) seen = false;
-        }
-        if (seen) {
-            const int64_t at_k = page * a.k_page + slot * a.k_slot + (int64_t)kvh * a.k_head;
-            float s = 0.f;
-            for (int d = 0; d < a.dim; ++d) s += query[d] * read_any(a.k, at_k + d, cache_dtype);
-            x = s * a.scale;
-            if (a.softcap > 0.f) x = a.softcap * tanhf(x / a.softcap);
-        }
-        float top = x;
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        __syncthreads();
-        if (lane == 0) red[wave] = top;
-        __syncthreads();
-        const float now = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-        const float base = now == -INFINITY ? 0.f : now, alpha = expf(m - base);
-        m = now;
-        const float p = seen ? expf(x - base) : 0.f;
-        probs[tid] = p;
-        rows[tid] = seen ? page * a.v_page + slot * a.v_slot + (int64_t)kvh * a.v_head : -1;
-        float sum = p;
-        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-        __syncthreads();
-        if (lane == 0) red[wave] = sum;
-        __syncthreads();
-        l = l * alpha + (red[0] + red[1]) + (red[2] + red[3]);
-        o *= alpha;
-        if (tid < a.dim)
-            for (int j = 0; j < 256; ++j)
-                if (rows[j] >= 0) o += probs[j] * read_any(a.v, rows[j] + tid, cache_dtype);
-        __syncthreads();
+    const AttnPart u = a.parts[blockIdx.x];
+    if (u.count == 0) return;
+    const int kvh = u.unit / a.blocks, row = (u.unit - kvh * a.blocks) * 16 * t.row_blocks + (int)blockIdx.y;
+    if (row >= t.rows) return;
+    const int node = row / a.group, head = kvh * a.group + (row - node * a.group), tid = threadIdx.x;
+    const int64_t out_row = (int64_t)u.seq * t.n_nodes + node;
+    auto slot = [&](int i) { return ((((int64_t)u.first + i) * 2 + (i == 0)) * a.part_heads + blockIdx.y); };
+    const int group = tid / T, d = (int)blockIdx.z * 64 + tid % T * V;
+    auto part = [&](int i) {
+        Pack<float, V> p = {};
+        if (i < u.count && d < a.dim) p = load_pack<float, V>(a.part_o + slot(i) * a.dim + d);
+        return p;
+    };
+    float m[OWN], l[OWN], top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+        const int i = tid + k * 256;
+        m[k] = i < u.count ? a.part_ml[slot(i) * 2] : -INFINITY;
+        l[k] = i < u.count ? a.part_ml[slot(i) * 2 + 1] : 0.f;
     }
-    if (tid < a.dim) write_any(a.out, (int64_t)row * a.o_row + (int64_t)head * a.o_head + tid, a.q_dtype, l == 0.f ? 0.f : o / l);
-    if (tid == 0 && a.lse) a.lse[(int64_t)row * a.q_heads + head] = l == 0.f ? -INFINITY : m + logf(l);
+    Pack<float, V> ahead[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) ahead[k] = part(group + k * G);
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) top = fmaxf(top, m[k]);
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) red[0][tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+        const float f = __builtin_amdgcn_exp2f(m[k] - base);
+        total += l[k] * f;
+        if (tid + k * 256 < u.count) w[tid + k * 256] = f;
+    }
+    for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+    if ((tid & 63) == 0) red[1][tid >> 6] = total;
+    __syncthreads();
+    Pack<float, V> v = {};
+    auto add = [&](const Pack<float, V> &p, int i) {
+        if (i >= u.count) return;
+#pragma unroll
+        for (int k = 0; k < V; ++k) v.v[k] += p.v[k] * w[i];
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) add(ahead[k], group + k * G);
+#pragma unroll 4
+    for (int i = group + AHEAD * G; i < u.count; i += G) add(part(i), i);
+    sum[group][tid % T] = v;
+    __syncthreads();
+    total = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const int e = (int)blockIdx.z * 64 + tid;
+    if (tid < 64 && e < a.dim) {
+        float x = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) x += sum[g][tid / V].v[tid % V];
+        store_f32(a.out, out_row * a.o_row + (int64_t)head * a.o_head + e, a.q_dtype, x * inv);
+    }
+    if (e == 0 && a.lse) a.lse[out_row * a.q_heads + head] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 }  // namespace
 
-size_t tree_plan(TreeArgs *, int, bool, int) { return 0; }
-void tree_workspace(TreeArgs *, void *) {}
+// As attn_plan: either a unit (a key head's rows, up to 16 * row_blocks of them) goes
+// to a workgroup, or as many workgroups as the card holds share all tiles.
+size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
+{
+    AttnArgs *a = &t->a;
+    t->rows = t->n_nodes * a->group;
+#define ILPM_TREE_OF(f, ...)                                                 \
+    (cache_dtype == ILPM_F32   ? f##_f32(__VA_ARGS__)                        \
+     : cache_dtype == ILPM_F16 ? (q32 ? f##_f16_q32(__VA_ARGS__) : f##_f16(__VA_ARGS__)) \
+                               : (q32 ? f##_bf16_q32(__VA_ARGS__) : f##_bf16(__VA_ARGS__)))
+    t->pieces = a->dim * element_bytes(cache_dtype) % 16 == 0;
+    const int most = t->pieces ? ILPM_TREE_OF(tree_most, a->dim) : 1;
+    t->row_blocks = std::min(most, t->rows > 32 ? 4 : t->rows > 16 ? 2 : 1);
+    a->blocks = std::max(1, ceil_div(t->rows, 16 * t->row_blocks));
+    const int64_t units = (int64_t)a->n_seqs * a->kv_heads * a->blocks;
+    const int64_t sinks = a->window > 0 ? std::min<int64_t>(t->sinks, max_len) : 0;
+    const int64_t keys = (a->window > 0 ? std::min<int64_t>(max_len, a->window) : max_len) + t->n_nodes;
+    const int64_t tiles = std::max<int64_t>(1, (keys + 15) / 16 + (sinks + 15) / 16);
+    // (Tiles are counted in 32 bits.  Where a table could name more, there are units enough without a split.)
+    const int64_t span = (((int64_t)a->capacity + 15) / 16 + 2 + kUnitCost) * units;
+    a->split = tiles > kWholeTiles && units > 0 && (span < INT_MAX || units == 1);
+    if (!a->split) {
+        a->grid = (int)units;
+        return 0;
+    }
+    const int card = ILPM_TREE_OF(tree_card, a->dim, t->row_blocks);
+#undef ILPM_TREE_OF
+    a->grid = (int)std::min<int64_t>({card, kMaxParts, units * ((tiles + kUnitCost + kMinShare - 1) / kMinShare)});
+    a->part_heads = std::min(t->rows, 16 * t->row_blocks);
+    a->part_of_unit = units <= a->grid;
+    return (size_t)a->grid * (sizeof(AttnPart) + 2 * a->part_heads * (size_t)(a->dim + 2) * sizeof(float));
+}
+
+void tree_workspace(TreeArgs *t, void *ws) { attn_workspace(&t->a, ws); }
 
 hipError_t tree_launch(const TreeArgs &t, int cache_dtype, hipStream_t stream)
 {
-    hipLaunchKernelGGL(tree_plain, dim3((unsigned)(t.a.n_seqs * t.n_nodes * t.a.q_heads)), dim3(256), 0, stream, t, cache_dtype);
+    const AttnArgs &a = t.a;
+    const bool q32 = a.q_dtype == ILPM_F32;
+    const hipError_t e = cache_dtype == ILPM_F32   ? tree_split_f32(t, stream)
+                         : cache_dtype == ILPM_F16 ? (q32 ? tree_split_f16_q32(t, stream) : tree_split_f16(t, stream))
+                                                   : (q32 ? tree_split_bf16_q32(t, stream) : tree_split_bf16(t, stream));
+    if (e != hipSuccess || !a.split) return e;
+    const dim3 grid(a.part_of_unit ? a.n_seqs * a.kv_heads * a.blocks : a.grid, a.part_heads, ceil_div(a.dim, 64));
+    if (a.dim % 4) hipLaunchKernelGGL((tree_join<1>), grid, dim3(256), 0, stream, t);
+    else hipLaunchKernelGGL((tree_join<4>), grid, dim3(256), 0, stream, t);
     return hipGetLastError();
 }
 
