@@ -57,7 +57,7 @@ template <typename T, int N> __device__ inline void store_loose(T *p, const Pack
 // m = floor(2^32 (2^s - d) / d) + 1, n / d = (floor(n m / 2^32) + n) >> s.
 struct Divisor {
     unsigned m, s;
-    explicit Divisor(unsigned d) : s(0)
+    explicit Divisor(unsigned d) : m(0), s(0)
     {
         while ((1ull << s) < d) ++s;
         m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);

@@ -271,15 +271,15 @@ __device__ inline Share share_of(const AttnArgs &a, int total, int top)
 }
 
 // The shares of this call, and where share `wg` begins (if it lies in the row).
-// tiles_in: a unit's tiles in a sequence of a length.
-template <typename Tiles> __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f, Begin *begin, Tiles tiles_in)
+// tiles_in: a unit's tiles in a sequence of a length; unit_cost: what it costs beside them.
+template <typename Tiles> __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f, Begin *begin, Tiles tiles_in, int unit_cost)
 {
     const int tid = threadIdx.x, units = units_of(a);
     *begin = Begin{0, 0, 0};
     if (a.n_seqs <= 64) {  // each wave for itself
         const int lane = tid & 63;
         const int length = lane < a.n_seqs ? a.lengths[lane] : 0;
-        const int t = lane < a.n_seqs ? tiles_in(length) : 0, cost = t > 0 ? t + kUnitCost : 0;
+        const int t = lane < a.n_seqs ? tiles_in(length) : 0, cost = t > 0 ? t + unit_cost : 0;
         int top = t, up_to = cost;
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
@@ -302,7 +302,7 @@ template <typename Tiles> __device__ inline Share find_share(const AttnArgs &a, 
     int mine = 0, top = 0, up_to;
     for (int i = tid; i < a.n_seqs; i += 256) {
         const int t = tiles_in(a.lengths[i]);
-        mine += t + kUnitCost;
+        mine += t + unit_cost;
         top = max(top, t);
     }
 #pragma unroll 1
@@ -316,7 +316,7 @@ template <typename Tiles> __device__ inline Share find_share(const AttnArgs &a, 
     int carry = 0;
     for (int i0 = 0; i0 < a.n_seqs && want >= carry; i0 += 256) {
         const int length = i0 + tid < a.n_seqs ? a.lengths[i0 + tid] : 0;
-        const int t = i0 + tid < a.n_seqs ? tiles_in(length) + kUnitCost : 0;
+        const int t = i0 + tid < a.n_seqs ? tiles_in(length) + unit_cost : 0;
         // (Up to 256 sequences the sums are there.)
         const int sum = a.n_seqs <= 256 ? total : scan256(t, &up_to, f);
         const int to = carry + up_to;
@@ -688,7 +688,7 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
     Share share = {0, 0, true};
     Begin begin;
     if constexpr (!SHORT)
-        if (a.split) share = find_share(a, wg, lds.found, &begin, [&](int n) { return tiles_of(a, n); });
+        if (a.split) share = find_share(a, wg, lds.found, &begin, [&](int n) { return tiles_of(a, n); }, kUnitCost);
 
     // This workgroup's place: a sequence, its length and its units' tiles, a unit
     // of it, and how far into the unit's length the share has come.

@@ -67,19 +67,35 @@ __device__ inline int tree_tiles(const TreeArgs &t, int length)
 }
 
 // N elements of a row from element d on, as load_row (decode_attn.h) takes them but
-// in pieces of any alignment: kPieces for head sizes of whole pieces.
+// in pieces of any alignment: kWhole and kPieces go by the head size alone.  (The
+// address space is named: of a choice between a row and the zeros the compiler
+// does not know it, and the loads that it takes then wait for LDS as well.)
 template <typename T, int N, Rows R, bool ZERO> __device__ inline Words<sizeof(T) * N> load_piece(const T *row, int d, int dim)
 {
     using W = Words<sizeof(T) * N>;
     if constexpr (R == kAny) return load_row<T, N, kAny, ZERO>(row, d, dim);
-    const T *at = d < dim ? row + d : ZERO ? (const T *)&attn_zeros : row;
-    return __builtin_bit_cast(W, load_loose<T, N>(at));
+    typedef W At __attribute__((aligned(sizeof(T))));
+    const T *at = R == kWhole || d < dim ? row + d : ZERO ? (const T *)&attn_zeros : row;
+    return *(const __attribute__((address_space(1))) At *)(uintptr_t)at;
+}
+
+// The kernel's arguments, read anew from where they lie: kept in registers, the
+// many that the loop over the tiles does not need take the place of those that it
+// does (they were moved to and from lanes of vector registers in every tile).
+typedef const __attribute__((address_space(4))) TreeArgs *TreeArgsAt;
+__device__ inline const TreeArgs &args_of(TreeArgsAt at)
+{
+    asm volatile("" : "+s"(at));
+    return *(const TreeArgs *)at;
 }
 
 // A head size's class, and what of AttnKernel's does not hold here.
 template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeKernel : AttnKernel<TC, Q16, DC, R, false> {
     using Base = AttnKernel<TC, Q16, DC, R, false>;
-    static constexpr int ROWS = 16 * MA;
+    // How far, in powers of two, scores may pass the reference of their row before it is
+    // moved up to them, and what f16 probabilities are scaled by so that they still fit.
+    static constexpr float SLACK = __is_same(TC, _Float16) ? 4.f : 8.f;
+    static constexpr float UP = __is_same(TC, _Float16) ? 0x1p11f : 1.f;
     // Workgroups that a compute unit holds at once.
     static constexpr int PER_CU = DC >= 192 ? 1 : 2;
 };
@@ -92,6 +108,9 @@ template <typename Cfg, int MA> struct TreeLds {
     int low[16 * MA];
     float unscale[16 * MA];
     int top_low;  // the largest of low
+    // Values of rows that are not finite for a key that not all rows see.
+    int any_odd;
+    unsigned odd[16 * MA][16];
     union {
         // The queries, as the lanes of the first product take them, in parts those of 32 bits.
         Words16 q[Cfg::QP][Cfg::NK][MA][64];
@@ -113,21 +132,52 @@ struct TreeSegment {
 // Where row r of a segment's block lies in q, out and lse: its sequence's node and head.
 __device__ inline int row_in_unit(const TreeSegment &seg, int rows_of_block, int r) { return seg.block * rows_of_block + r; }
 
-// Rows' bits and lows, and the queries in their layout, into LDS.
-template <typename TC, bool Q16, int DC, Rows R, int MA, typename Lds>
-__device__ __forceinline__ void tree_rows(const TreeArgs &t, const TreeSegment &seg, Lds &lds)
-{
+// What a wave reads for a segment's rows: its lanes' parents, and queries as they
+// lie in memory.  Wave w takes block w % MA, and of it every (4 / MA)-th piece.
+template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeRows {
     using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
     using TQ = std::conditional_t<Q16, TC, float>;
-    constexpr int KV = Cfg::KV, NK = Cfg::NK, QP = Cfg::QP;
-    const AttnArgs &a = t.a;
-    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), n16 = lane & 15, g = lane >> 4;
-    if (wave == 0) {
-        unsigned long long bits = seen_nodes(lane < t.n_nodes ? t.parents[(int64_t)seg.seq * t.n_nodes + lane] : -2, lane, t.n_nodes);
+    static constexpr int KV = Cfg::KV, NK = Cfg::NK, QP = Cfg::QP, STEP = 4 / MA, MINE = (NK + STEP - 1) / STEP;
+    int parent;
+    const TQ *row;
+    Words16 q[QP == 1 ? MINE : 1];
+
+    __device__ __forceinline__ void load(TreeArgsAt args, const TreeSegment &seg, int lane, int wave)
+    {
+        const TreeArgs &t = args_of(args);
+        const AttnArgs &a = t.a;
+        const int n16 = lane & 15, g = lane >> 4, ma = wave % MA, c0 = wave / MA;
+        parent = wave == 0 && lane < t.n_nodes ? t.parents[(int64_t)seg.seq * t.n_nodes + lane] : -2;
+        const int in_unit = min(row_in_unit(seg, 16 * MA, ma * 16 + n16), t.rows - 1), node = t.by_group.of(in_unit);
+        row = (const TQ *)a.q + ((int64_t)seg.seq * t.n_nodes + node) * a.q_row +
+              ((int64_t)seg.kvh * a.group + (in_unit - node * a.group)) * a.q_head;
+        if constexpr (QP == 1) {
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) q[i] = load_piece<TQ, KV, R, true>(row, (g + 4 * min(c0 + i * STEP, NK - 1)) * KV, a.dim);
+        }
+    }
+
+    // Rows' bits and lows, and the queries in their layout, into LDS.
+    template <typename Lds> __device__ __forceinline__ void store(TreeArgsAt args, const TreeSegment &seg, int lane, int wave, Lds &lds)
+    {
+        const TreeArgs &t = args_of(args);
+        const AttnArgs &a = t.a;
+        const int n16 = lane & 15, g = lane >> 4, ma = wave % MA, c0 = wave / MA;
+        for (int i = threadIdx.x; i < 16 * MA * 16; i += 256) lds.odd[i / 16][i % 16] = 0;
+        if (threadIdx.x == 0) lds.any_odd = 0;
+        if constexpr (QP == 1) {
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) lds.q[0][min(c0 + i * STEP, NK - 1)][ma][lane] = q[i];
+        } else {
+            split(t, lane, ma, c0, lds);
+        }
+        if (wave != 0) return;
+        unsigned long long bits = seen_nodes(parent, lane, t.n_nodes);
         const int depth = __builtin_popcountll(bits) - 1;
         int low = 0;
         if (a.window > 0) {
             const unsigned long long above = bits;
+#pragma unroll 1
             for (int n = 0; n < t.n_nodes; ++n) {
                 const int dn = __builtin_amdgcn_readlane(depth, n);
                 if (((above >> n) & 1) && depth - dn >= a.window && seg.range.length + dn >= t.sinks) bits &= ~(1ull << n);
@@ -135,30 +185,21 @@ __device__ __forceinline__ void tree_rows(const TreeArgs &t, const TreeSegment &
             low = (int)min((int64_t)INT_MAX, max((int64_t)0, seg.range.length + depth + 1 - a.window));
         }
         int top = low;
+        if (a.window > 0)
 #pragma unroll 1
-        for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
+            for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
         if (lane == 0) lds.top_low = top;
-        for (int r0 = 0; r0 < 16 * MA; r0 += 64) {
-            const int r = r0 + lane, row = row_in_unit(seg, 16 * MA, r), node = min(row / a.group, t.n_nodes - 1);
-            const unsigned b0 = __shfl((unsigned)bits, node), b1 = __shfl((unsigned)(bits >> 32), node);
-            const int l = __shfl(low, node);
-            if (r < 16 * MA) {
-                lds.bits[r] = row < t.rows ? (unsigned long long)b1 << 32 | b0 : 0ull;
-                lds.low[r] = l;
-            }
-        }
+        const int r = min(lane, 16 * MA - 1), in_block = row_in_unit(seg, 16 * MA, r), node = min(t.by_group.of(in_block), t.n_nodes - 1);
+        const unsigned b0 = __shfl((unsigned)bits, node), b1 = __shfl((unsigned)(bits >> 32), node);
+        const int l = __shfl(low, node);
+        lds.bits[r] = in_block < t.rows ? (unsigned long long)b1 << 32 | b0 : 0ull;
+        lds.low[r] = l;
     }
-    // Wave w takes block w % MA, and of it every (4 / MA)-th piece.
-    constexpr int STEP = 4 / MA;
-    const int ma = wave % MA, c0 = wave / MA;
-    const int in_unit = min(row_in_unit(seg, 16 * MA, ma * 16 + n16), t.rows - 1), node = in_unit / a.group;
-    const TQ *row = (const TQ *)a.q + ((int64_t)seg.seq * t.n_nodes + node) * a.q_row +
-                    ((int64_t)seg.kvh * a.group + (in_unit - node * a.group)) * a.q_head;
-    if constexpr (QP == 1) {
-#pragma unroll 2
-        for (int c = c0; c < NK; c += STEP)
-            lds.q[0][c][ma][lane] = load_piece<TQ, KV, R, true>(row, (g + 4 * c) * KV, a.dim);
-    } else {
+
+    // Queries of 32 bits in three parts (see decode_attn.h).
+    template <typename Lds> __device__ __forceinline__ void split(const TreeArgs &t, int lane, int ma, int c0, Lds &lds)
+    {
+        const int n16 = lane & 15, g = lane >> 4, dim = t.a.dim;
         struct Values {
             float v[KV];
         };
@@ -167,10 +208,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs &t, const TreeSegment &
                 Words16 w[2];
             } h;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int d = (g + 4 * c) * KV + 4 * n;
-                h.w[n] = load_piece<float, 4, R, true>(row, d, a.dim);
-            }
+            for (int n = 0; n < 2; ++n) h.w[n] = load_piece<float, 4, R, true>(row, (g + 4 * c) * KV + 4 * n, dim);
             return __builtin_bit_cast(Values, h);
         };
         float f = 1.f, back = 1.f;
@@ -212,8 +250,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs &t, const TreeSegment &
             for (int n = 0; n < 3; ++n) lds.q[n][c][ma][lane] = __builtin_bit_cast(Words16, part[n]);
         }
     }
-    __syncthreads();
-}
+};
 
 template <typename TC> __device__ inline floatx4 mfma_values32(Words16 v, Words16 p, floatx4 c) { return mfma_scores<TC>(v, p, c); }
 
@@ -223,18 +260,16 @@ template <typename TC> __device__ inline unsigned not_finite(unsigned w)
     constexpr unsigned E = __is_same(TC, __bf16) ? 0x7f80u : 0x7c00u;
     return ((w & E) == E ? 0xffffu : 0u) | ((w & (E << 16)) == (E << 16) ? 0xffff0000u : 0u);
 }
-template <typename TC> constexpr unsigned kOnes = __is_same(TC, __bf16) ? 0x3f803f80u : 0x3c003c00u;
 
 // A wave's part of a segment, every fourth tile of it, and the join of the
 // four waves' parts, 16 rows at a time.
 template <typename TC, bool Q16, int DC, Rows R, int MA, typename Put>
-__device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegment &seg, TreeLds<TreeKernel<TC, Q16, DC, R, MA>, MA> &lds, Put put)
+__device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment &seg, TreeLds<TreeKernel<TC, Q16, DC, R, MA>, MA> &lds, Put put)
 {
     using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
     constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
     constexpr int QP = Cfg::QP, PP = Cfg::PP;
     constexpr bool C16 = Cfg::C16;
-    const AttnArgs &a = t.a;
 
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
@@ -252,6 +287,7 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
         int page, slot;
     };
     auto look_up = [&](int group) {
+        const AttnArgs &a = args_of(args).a;
         Entry e = {-1, 0};
         const int tile = seg.tile0 + (group * 4 + g) * 4 + wave;
         const int64_t key = (int64_t)start_of(tile) + n16;
@@ -264,6 +300,7 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
         return e;
     };
     auto place = [&](int group, Entry e) {
+        const AttnArgs &a = args_of(args).a;
         const bool ok = e.page >= 0 && e.page < a.n_pages;
         Places &p = lds.places[wave][group & 1];
         p.k[lane] = ok ? (int64_t)e.page * a.k_page + (int64_t)e.slot * a.k_slot : -1;
@@ -273,8 +310,12 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
+    const TreeArgs &t = args_of(args);
+    const AttnArgs &a = t.a;
     const TC *kh = (const TC *)a.k + (int64_t)seg.kvh * a.k_head;
     const TC *vh = (const TC *)a.v + (int64_t)seg.kvh * a.v_head;
+    const int dim = a.dim, all_sinks = t.sinks;
+    const float softcap = a.softcap;
     Words16 kt[NK];
     Words<sizeof(TC) * VV> vt[4][NV];
     bool seen[4];
@@ -283,7 +324,7 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
         const int64_t at = lds.places[wave][(j >> 2) & 1].k[(j & 3) * 16 + n16];
         const TC *row = kh + (j < tiles ? max(at, (int64_t)0) : 0);
 #pragma unroll
-        for (int c = 0; c < NK; ++c) kt[c] = load_piece<TC, KV, R, true>(row, (g + 4 * c) * KV, a.dim);
+        for (int c = 0; c < NK; ++c) kt[c] = load_piece<TC, KV, R, true>(row, (g + 4 * c) * KV, dim);
     };
     auto load_v = [&](int j) {
 #pragma unroll
@@ -293,15 +334,23 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
             const TC *row = vh + (j < tiles ? max(at, (int64_t)0) : 0);
 #pragma unroll
             for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
-                vt[r][c] = load_piece<TC, VV, R, false>(row, (n16 + 16 * c) * VV, a.dim);
+                vt[r][c] = load_piece<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R, false>(row, (n16 + 16 * c) * VV, dim);
         }
     };
 
     Entry e0 = {}, next = {};
     if (tiles > 0) e0 = look_up(0);
     if (tiles > 4) next = look_up(1);
-    tree_rows<TC, Q16, DC, R, MA>(t, seg, lds);
-    if (tiles > 0) place(0, e0);
+    // The first tile, the rows' nodes and queries: none waits for another.
+    TreeRows<TC, Q16, DC, R, MA> rows;
+    rows.load(args, seg, lane, wave);
+    if (tiles > 0) {
+        place(0, e0);
+        load_k(0);
+        load_v(0);
+    }
+    rows.store(args, seg, lane, wave, lds);
+    __syncthreads();
 
     floatx4 o[MA][NO];
     float m[MA], l[MA];
@@ -312,8 +361,8 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
 #pragma unroll
         for (int i = 0; i < NO; ++i) o[ma][i] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    const float scale2 = a.softcap > 0.f ? a.scale / a.softcap : a.scale * kLog2e;
-    const float cap2 = a.softcap * kLog2e;
+    const float scale2 = softcap > 0.f ? a.scale / softcap : a.scale * kLog2e;
+    const float cap2 = softcap * kLog2e;
     const int top_low = uniform(lds.top_low);
 
     // Selectors that put rows' 16-bit values together; 0 for those of keys that are not seen.
@@ -321,88 +370,43 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
         return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], i & 1 ? upper[0] : lower[0]),
                         __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], i & 1 ? upper[1] : lower[1])};
     };
-    // Whether row (ma, n16) sees key j, which is in the cache.
-    auto sees = [&](int ma, int64_t j) {
-        const int r = ma * 16 + n16;
+    // Whether row r sees key j, which is in the cache.
+    auto sees = [&](int r, int64_t j) {
         if (j >= range.length) return ((lds.bits[r] >> min(j - range.length, (int64_t)63)) & 1) != 0;
-        return j >= lds.low[r] || j < t.sinks;
+        return j >= lds.low[r] || j < all_sinks;
     };
-    // Takes values that are not finite out of a tile whose rows do not see the same keys, and gives NaN to the rows
-    // that see them.  (Hardly ever: no need for it to be fast.)
+    // Takes values that are not finite out of a tile whose rows do not see the same keys, and marks the rows that see
+    // them: bit c * VV + i of odd[row][n] stands for value (n + 16c) * VV + i.  (Hardly ever.)
     auto take_out = [&](int64_t key0) {
-        bool any = false;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r) {
+            unsigned odd = 0;
 #pragma unroll
             for (int c = 0; c < NV; ++c) {
                 if constexpr (C16) {
 #pragma unroll
-                    for (int i = 0; i < VV / 2; ++i) any |= seen[r] && not_finite<TC>(vt[r][c][i]) != 0;
+                    for (int i = 0; i < VV / 2; ++i) {
+                        const unsigned w = not_finite<TC>(vt[r][c][i]);
+                        vt[r][c][i] &= ~w;
+                        odd |= (w & 1u) << (c * VV + 2 * i) | (w >> 31) << (c * VV + 2 * i + 1);
+                    }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < VV; ++i) any |= seen[r] && (vt[r][c][i] & 0x7f800000u) == 0x7f800000u;
+                    for (int i = 0; i < VV; ++i) {
+                        const bool is = (vt[r][c][i] & 0x7f800000u) == 0x7f800000u;
+                        vt[r][c][i] = is ? 0u : vt[r][c][i];
+                        odd |= (is ? 1u : 0u) << (c * VV + i);
+                    }
                 }
             }
-        if (!__builtin_amdgcn_ballot_w64(any)) return;
-#pragma unroll
-        for (int ma = 0; ma < MA; ++ma) {
-            bool s[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[r] = seen[r] && sees(ma, key0 + 4 * g + r);
-            if constexpr (C16) {
-                unsigned lower[2], upper[2];
-                Words<8> ones;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const unsigned keep = (seen[2 * h] ? 0xffffu : 0u) | (seen[2 * h + 1] ? 0xffff0000u : 0u);
-                    lower[h] = (0x05040100u & keep) | (0x0c0c0c0cu & ~keep);
-                    upper[h] = (0x07060302u & keep) | (0x0c0c0c0cu & ~keep);
-                    ones[h] = kOnes<TC> & ((s[2 * h] ? 0xffffu : 0u) | (s[2 * h + 1] ? 0xffff0000u : 0u));
-                }
-#pragma unroll
-                for (int c = 0; c < NV; ++c)
-#pragma unroll
-                    for (int i = 0; i < VV; ++i) {
-                        Words<8> v = values(c, i, lower, upper);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) v[h] = not_finite<TC>(v[h]) & kOnes<TC>;
-                        const floatx4 n = mfma_values<TC>(v, ones, floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[ma][c * VV + i][r] += n[r] > 0.f ? __builtin_nanf("") : 0.f;
-                    }
-            } else {
-#pragma unroll
-                for (int c = 0; c < NV; ++c)
-#pragma unroll
-                    for (int i = 0; i < VV; ++i) {
-                        floatx4 n = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            n = __builtin_amdgcn_mfma_f32_16x16x4f32(seen[r] && (vt[r][c][i] & 0x7f800000u) == 0x7f800000u ? 1.f : 0.f,
-                                                                     s[r] ? 1.f : 0.f, n, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[ma][c * VV + i][r] += n[r] > 0.f ? __builtin_nanf("") : 0.f;
-                    }
-            }
+            if (!seen[r] || odd == 0) continue;
+            lds.any_odd = 1;
+#pragma unroll 1
+            for (int row = 0; row < 16 * MA; ++row)
+                if (sees(row, key0 + 4 * g + r)) atomicOr(&lds.odd[row][n16], odd);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int c = 0; c < NV; ++c) {
-                if constexpr (C16) {
-#pragma unroll
-                    for (int i = 0; i < VV / 2; ++i) vt[r][c][i] &= ~not_finite<TC>(vt[r][c][i]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < VV; ++i) vt[r][c][i] = (vt[r][c][i] & 0x7f800000u) == 0x7f800000u ? 0u : vt[r][c][i];
-                }
-            }
     };
 
-    if (tiles > 0) {
-        load_k(0);
-        load_v(0);
-    }
 #pragma unroll 1
     for (int j = 0; j < tiles; ++j) {
         if ((j & 3) == 2 && j + 2 < tiles) {
@@ -449,23 +453,36 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
         if (special) take_out(key0);
         constexpr int PW = !C16 ? 4 : PP == 3 ? 6 : 4;
         unsigned part[MA][PW];  // probabilities: hi and lo of four keys, a third part; or 32 bits
+        if (softcap > 0.f) {
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma) {
+                const float by = QP == 3 ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[ma][r] = cap2 * tanh_of(s[ma][r] * by);
+            }
+        } else {
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma) {
+                const float by = QP == 3 ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[ma][r] *= by;
+            }
+        }
+        if (special) {
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[ma][r] = sees(ma * 16 + n16, key0 + 4 * g + r) ? s[ma][r] : -INFINITY;
+        }
 #pragma unroll
         for (int ma = 0; ma < MA; ++ma) {
             float x[4], top = -INFINITY;
-            const float by = QP == 3 ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] = s[ma][r] * by;
-                if (a.softcap > 0.f) x[r] = cap2 * tanh_of(x[r]);
-                x[r] = seen[r] ? x[r] : -INFINITY;
-            }
-            if (special) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = sees(ma, key0 + 4 * g + r) ? x[r] : -INFINITY;
-            }
+            for (int r = 0; r < 4; ++r) x[r] = seen[r] ? s[ma][r] : -INFINITY;
 #pragma unroll
             for (int r = 0; r < 4; ++r) top = fmaxf(top, x[r]);
-            if (__builtin_amdgcn_ballot_w64(top > m[ma])) {  // (most tiles leave all maxima where they are)
+            // (m may lie up to SLACK below the maximum: most tiles after the first leave it where it is.)
+            if (__builtin_amdgcn_ballot_w64(top > m[ma] + Cfg::SLACK)) {
                 const float m_new = fmaxf(m[ma], max_of_head(top));
                 const float alpha = __builtin_amdgcn_exp2f(m[ma] - (m_new == -INFINITY ? 0.f : m_new));
                 m[ma] = m_new;
@@ -542,13 +559,23 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
         load_v(j + 1);
     }
 
+    const int n_rows = args_of(args).rows;
     // Join the waves: lane (n, g) holds values (4g + r + 16c) * VV + i of row n.
 #pragma unroll
     for (int ma = 0; ma < MA; ++ma) {
         float sum = l[ma];
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        __syncthreads();  // the queries, or what the last rows left, have been read
+        if (row_in_unit(seg, 16 * MA, ma * 16) >= n_rows) break;
+        __syncthreads();  // the queries, or what the last rows left, have been read; all odd values are marked
+        if (lds.any_odd) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const unsigned odd = lds.odd[ma * 16 + n16][4 * g + r];
+#pragma unroll
+                for (int i = 0; i < NO; ++i) o[ma][i][r] = (odd >> i) & 1 ? __builtin_nanf("") : o[ma][i][r];
+            }
+        }
         const bool real = lds.bits[ma * 16 + n16] != 0;  // (what is no node has seen keys of the sequence: none counts)
         if (g == 0) {
             lds.j.m[wave][n16] = real ? m[ma] : -INFINITY;
@@ -565,11 +592,12 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
             }
         __syncthreads();
         constexpr int PER = DC / 4;
+        const TreeArgs &t = args_of(args);
         const int row0 = row_in_unit(seg, 16 * MA, ma * 16), rows = min(16, t.rows - row0);
 #pragma unroll 1
         for (int i = threadIdx.x; i < rows * PER; i += 256) {
             const int r = i / PER, d = (i - r * PER) * 4;
-            if (d >= a.dim) continue;
+            if (d >= t.a.dim) continue;
             floatx4 v[4];
             float mw[4], lw[4];
 #pragma unroll
@@ -585,17 +613,20 @@ __device__ __forceinline__ void tree_segment(const TreeArgs &t, const TreeSegmen
                 v[w] *= f;
                 lw[w] *= f;
             }
-            put(row0 + r, ma * 16 + r, d, (v[0] + v[1]) + (v[2] + v[3]), top, (lw[0] + lw[1]) + (lw[2] + lw[3]));
+            put(t, row0 + r, ma * 16 + r, d, (v[0] + v[1]) + (v[2] + v[3]), top, (lw[0] + lw[1]) + (lw[2] + lw[3]));
         }
     }
 }
 
 template <typename TC, bool Q16, int DC, Rows R, int MA>
-__global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void tree_split(TreeArgs t)
+__global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void tree_split(TreeArgs)
 {
     using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
+    const int unit_cost = tree_unit_cost(MA);
     using TQ = std::conditional_t<Q16, TC, float>;
     __shared__ TreeLds<Cfg, MA> lds;
+    const TreeArgsAt args = (TreeArgsAt)__builtin_amdgcn_kernarg_segment_ptr();
+    const TreeArgs &t = args_of(args);
     const AttnArgs &a = t.a;
 
     // (Neighbouring shares stay on one die: see decode_attn.h.)
@@ -603,7 +634,7 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
     const int units = units_of(a), wg = die * dies + min(die, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
     Share share = {0, 0, true};
     Begin begin;
-    if (a.split) share = find_share(a, wg, lds.found, &begin, [&](int n) { return tree_tiles(t, n); });
+    if (a.split) share = find_share(a, wg, lds.found, &begin, [&](int n) { return tree_tiles(t, n); }, unit_cost);
 
     // This workgroup's place: a sequence, its length and its units' tiles, a unit
     // of it, and how far into the unit's length the share has come.
@@ -624,26 +655,27 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
         length = begin.length;
         tiles_all = tree_tiles(t, length);
         const int in = at - begin.before;
-        unit = in / (tiles_all + kUnitCost);
-        x0 = in - unit * (tiles_all + kUnitCost);
+        unit = in / (tiles_all + unit_cost);
+        x0 = in - unit * (tiles_all + unit_cost);
     }
 
+    const bool split = a.split, part_of_unit = a.part_of_unit;
+    const int n_seqs = a.n_seqs, blocks = a.blocks;
     for (;;) {
-        const int x1 = share.whole ? tiles_all + kUnitCost : min(tiles_all + kUnitCost, x0 + (last - at));
-        const int tile0 = max(0, x0 - kUnitCost), seg_tiles = max(0, x1 - kUnitCost) - tile0;
+        const int x1 = share.whole ? tiles_all + unit_cost : min(tiles_all + unit_cost, x0 + (last - at));
+        const int tile0 = max(0, x0 - unit_cost), seg_tiles = max(0, x1 - unit_cost) - tile0;
         if (seg_tiles == 0) return;  // the share ends before the unit's first tile
         TreeSegment seg;
         seg.seq = seq;
-        seg.kvh = unit / a.blocks;
-        seg.block = unit - seg.kvh * a.blocks;
+        seg.kvh = unit / blocks;
+        seg.block = unit - seg.kvh * blocks;
         seg.tile0 = tile0;
         seg.tile1 = tile0 + seg_tiles;
-        seg.range = tree_range(t, length);
+        seg.range = tree_range(args_of(args), length);
         if (seg.range.end == 0) seg.tile1 = tile0;  // (no keys, and perhaps no pool)
         const bool all = seg_tiles == tiles_all;  // of the unit's tiles
-        // The part that begins a unit, or the one that goes on with it.
-        const int64_t part = ((int64_t)wg * 2 + (tile0 == 0 ? 1 : 0)) * a.part_heads;
-        tree_segment<TC, Q16, DC, R, MA>(t, seg, lds, [&](int row, int r, int d, floatx4 v, float top, float sum) {
+        tree_segment<TC, Q16, DC, R, MA>(args, seg, lds, [&](const TreeArgs &t, int row, int r, int d, floatx4 v, float top, float sum) {
+            const AttnArgs &a = t.a;
             auto put = [&](auto *to) {
                 using TO = std::remove_reference_t<decltype(*to)>;
                 Pack<TO, 4> p;
@@ -658,45 +690,46 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
                 if (d + 2 < a.dim) to[d + 2] = p.v[2];
             };
             if (all) {
-                const int node = row / a.group, head = seg.kvh * a.group + (row - node * a.group);
-                const int64_t at_row = (int64_t)seq * t.n_nodes + node;
+                const int node = t.by_group.of(row), head = seg.kvh * a.group + (row - node * a.group);
+                const int64_t at_row = (int64_t)seg.seq * t.n_nodes + node;
                 v *= sum == 0.f ? 0.f : 1.f / (sum * Cfg::UP);
                 put((TQ *)a.out + at_row * a.o_row + (int64_t)head * a.o_head);
                 if (d == 0 && a.lse) a.lse[at_row * a.q_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
             } else {
+                // The part that begins a unit, or the one that goes on with it.
+                const int64_t part = ((int64_t)wg * 2 + (seg.tile0 == 0 ? 1 : 0)) * a.part_heads + r;
                 v *= 1.f / Cfg::UP;
-                put(a.part_o + (part + r) * a.dim);
+                put(a.part_o + part * a.dim);
                 if (d == 0) {
-                    a.part_ml[(part + r) * 2] = top;
-                    a.part_ml[(part + r) * 2 + 1] = sum;
+                    a.part_ml[part * 2] = top;
+                    a.part_ml[part * 2 + 1] = sum;
                 }
             }
         });
+        const AttnArgs &a = args_of(args).a;
         // Who begins a unit says whether others go on with it.
-        if (a.split && threadIdx.x == 0 && tile0 == 0) {
+        if (split && threadIdx.x == 0 && tile0 == 0) {
             const int rest = tiles_all - seg_tiles;
             const int count = all ? 0 : 1 + (int)(((unsigned)rest + share.size - 1) / (unsigned)share.size);
-            if (a.part_of_unit) a.parts[seq * units + unit] = AttnPart{seq, unit, wg, count};
+            if (part_of_unit) a.parts[seq * units + unit] = AttnPart{seq, unit, wg, count};
             else if (!all) a.parts[wg] = AttnPart{seq, unit, wg, count};
         }
         __syncthreads();  // the LDS that the next unit's waves write has been read
         if (share.whole) {
             const int u = seq * units + unit + (int)gridDim.x;
-            if (!a.split || u >= a.n_seqs * units) return;
+            if (!split || u >= n_seqs * units) return;
             seq = u / units;
             unit = u - seq * units;
-            length = uniform(a.lengths[seq]);
-            tiles_all = tree_tiles(t, length);
-            continue;
-        }
-        at += x1 - x0;
-        if (at >= last) return;
-        x0 = 0;
-        if (++unit == units) {
+        } else {
+            at += x1 - x0;
+            if (at >= last) return;
+            x0 = 0;
+            if (++unit < units) continue;
             unit = 0;
-            length = uniform(a.lengths[++seq]);
-            tiles_all = tree_tiles(t, length);
+            ++seq;
         }
+        length = uniform(a.lengths[seq]);
+        tiles_all = tree_tiles(args_of(args), length);
     }
 }
 
@@ -705,18 +738,21 @@ template <typename TC, int DC> constexpr int kMostBlocks = sizeof(TC) == 4 ? (DC
 
 template <typename TC, bool Q16, int DC> hipError_t tree_split_launch(const TreeArgs &t, hipStream_t stream)
 {
+    constexpr int MOST = kMostBlocks<TC, DC>;
     auto launch = [&](auto rows, auto blocks) {
         hipLaunchKernelGGL((tree_split<TC, Q16, DC, decltype(rows)::value, decltype(blocks)::value>), dim3(t.a.grid), dim3(256), 0, stream, t);
         return hipGetLastError();
     };
-    constexpr int MOST = kMostBlocks<TC, DC>;
-    constexpr std::integral_constant<Rows, kPieces> pieces{};
-    if (!t.pieces) return launch(std::integral_constant<Rows, kAny>{}, std::integral_constant<int, 1>{});
-    if constexpr (MOST >= 4)
-        if (t.row_blocks == 4) return launch(pieces, std::integral_constant<int, 4>{});
-    if constexpr (MOST >= 2)
-        if (t.row_blocks == 2) return launch(pieces, std::integral_constant<int, 2>{});
-    return launch(pieces, std::integral_constant<int, 1>{});
+    auto by_blocks = [&](auto rows) {
+        if constexpr (MOST >= 4)
+            if (t.row_blocks == 4) return launch(rows, std::integral_constant<int, 4>{});
+        if constexpr (MOST >= 2)
+            if (t.row_blocks == 2) return launch(rows, std::integral_constant<int, 2>{});
+        return launch(rows, std::integral_constant<int, 1>{});
+    };
+    if (t.a.dim == DC) return by_blocks(std::integral_constant<Rows, kWhole>{});
+    if (t.pieces) return by_blocks(std::integral_constant<Rows, kPieces>{});
+    return launch(std::integral_constant<Rows, kAny>{}, std::integral_constant<int, 1>{});
 }
 
 template <typename TC, bool Q16> hipError_t tree_split_by_dim(const TreeArgs &t, hipStream_t stream)

@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kMaxParts = 4 * kAttnCus;  // of a unit: workgroups of a call
 constexpr float kLn2 = 0.69314718055994530942f;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 __device__ inline void store_f32(void *p, int64_t i, int dtype, float v)
 {
@@ -42,7 +43,7 @@ template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
     if (u.count == 0) return;
     const int kvh = u.unit / a.blocks, row = (u.unit - kvh * a.blocks) * 16 * t.row_blocks + (int)blockIdx.y;
     if (row >= t.rows) return;
-    const int node = row / a.group, head = kvh * a.group + (row - node * a.group), tid = threadIdx.x;
+    const int node = t.by_group.of(row), head = kvh * a.group + (row - node * a.group), tid = threadIdx.x;
     const int64_t out_row = (int64_t)u.seq * t.n_nodes + node;
     auto slot = [&](int i) { return ((((int64_t)u.first + i) * 2 + (i == 0)) * a.part_heads + blockIdx.y); };
     const int group = tid / T, d = (int)blockIdx.z * 64 + tid % T * V;
@@ -101,6 +102,40 @@ template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
     if (e == 0 && a.lse) a.lse[out_row * a.q_heads + head] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
+// The same where there are many: a thread takes four values of a row, over all
+// parts.
+__global__ __launch_bounds__(256) void tree_join_rows(TreeArgs t, int lanes, Divisor by_lanes)
+{
+    const AttnArgs &a = t.a;
+    const AttnPart u = a.parts[blockIdx.x];
+    if (u.count == 0) return;
+    const int r = by_lanes.of((int)threadIdx.x), lane = (int)threadIdx.x - r * lanes, per = by_lanes.of(256);
+    const int in_block = (int)blockIdx.y * per + r, d = lane * 4;
+    const int kvh = u.unit / a.blocks, row = (u.unit - kvh * a.blocks) * 16 * t.row_blocks + in_block;
+    if (r >= per || in_block >= a.part_heads || row >= t.rows) return;
+    const int node = t.by_group.of(row), head = kvh * a.group + (row - node * a.group);
+    const int64_t out_row = (int64_t)u.seq * t.n_nodes + node;
+    auto slot = [&](int i) { return (((int64_t)u.first + i) * 2 + (i == 0)) * a.part_heads + in_block; };
+    float top = -INFINITY, total = 0.f;
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    // (A part at a time with the maximum so far: in their order, two accesses each that do not wait for others.)
+#pragma unroll 4
+    for (int i = 0; i < u.count; ++i) {
+        const int64_t at = slot(i);
+        const float m = a.part_ml[at * 2], l = a.part_ml[at * 2 + 1];
+        const floatx4 p = *reinterpret_cast<const floatx4 *>(a.part_o + at * a.dim + d);
+        const float now = fmaxf(top, m), base = now == -INFINITY ? 0.f : now;
+        const float old = __builtin_amdgcn_exp2f(top - base), own = __builtin_amdgcn_exp2f(m - base);
+        top = now;
+        total = total * old + l * own;
+        v = v * old + p * own;
+    }
+    v *= total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) store_f32(a.out, out_row * a.o_row + (int64_t)head * a.o_head + d + k, a.q_dtype, v[k]);
+    if (d == 0 && a.lse) a.lse[out_row * a.q_heads + head] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
 }  // namespace
 
 // As attn_plan: either a unit (a key head's rows, up to 16 * row_blocks of them) goes
@@ -109,6 +144,7 @@ size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
 {
     AttnArgs *a = &t->a;
     t->rows = t->n_nodes * a->group;
+    t->by_group = Divisor((unsigned)a->group);
 #define ILPM_TREE_OF(f, ...)                                                 \
     (cache_dtype == ILPM_F32   ? f##_f32(__VA_ARGS__)                        \
      : cache_dtype == ILPM_F16 ? (q32 ? f##_f16_q32(__VA_ARGS__) : f##_f16(__VA_ARGS__)) \
@@ -122,7 +158,7 @@ size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
     const int64_t keys = (a->window > 0 ? std::min<int64_t>(max_len, a->window) : max_len) + t->n_nodes;
     const int64_t tiles = std::max<int64_t>(1, (keys + 15) / 16 + (sinks + 15) / 16);
     // (Tiles are counted in 32 bits.  Where a table could name more, there are units enough without a split.)
-    const int64_t span = (((int64_t)a->capacity + 15) / 16 + 2 + kUnitCost) * units;
+    const int64_t span = (((int64_t)a->capacity + 15) / 16 + 2 + tree_unit_cost(t->row_blocks)) * units;
     a->split = tiles > kWholeTiles && units > 0 && (span < INT_MAX || units == 1);
     if (!a->split) {
         a->grid = (int)units;
@@ -130,7 +166,7 @@ size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
     }
     const int card = ILPM_TREE_OF(tree_card, a->dim, t->row_blocks);
 #undef ILPM_TREE_OF
-    a->grid = (int)std::min<int64_t>({card, kMaxParts, units * ((tiles + kUnitCost + kMinShare - 1) / kMinShare)});
+    a->grid = (int)std::min<int64_t>({card, kMaxParts, units * ((tiles + tree_unit_cost(t->row_blocks) + kMinShare - 1) / kMinShare)});
     a->part_heads = std::min(t->rows, 16 * t->row_blocks);
     a->part_of_unit = units <= a->grid;
     return (size_t)a->grid * (sizeof(AttnPart) + 2 * a->part_heads * (size_t)(a->dim + 2) * sizeof(float));
@@ -146,7 +182,13 @@ hipError_t tree_launch(const TreeArgs &t, int cache_dtype, hipStream_t stream)
                          : cache_dtype == ILPM_F16 ? (q32 ? tree_split_f16_q32(t, stream) : tree_split_f16(t, stream))
                                                    : (q32 ? tree_split_bf16_q32(t, stream) : tree_split_bf16(t, stream));
     if (e != hipSuccess || !a.split) return e;
-    const dim3 grid(a.part_of_unit ? a.n_seqs * a.kv_heads * a.blocks : a.grid, a.part_heads, ceil_div(a.dim, 64));
+    const int joins = a.part_of_unit ? a.n_seqs * a.kv_heads * a.blocks : a.grid;
+    if (a.dim % 4 == 0 && (int64_t)joins * a.part_heads * ceil_div(a.dim, 64) > 8 * kAttnCus) {
+        const int lanes = a.dim / 4;
+        hipLaunchKernelGGL(tree_join_rows, dim3(joins, ceil_div(a.part_heads, 256 / lanes)), dim3(256), 0, stream, t, lanes, Divisor((unsigned)lanes));
+        return hipGetLastError();
+    }
+    const dim3 grid(joins, a.part_heads, ceil_div(a.dim, 64));
     if (a.dim % 4) hipLaunchKernelGGL((tree_join<1>), grid, dim3(256), 0, stream, t);
     else hipLaunchKernelGGL((tree_join<4>), grid, dim3(256), 0, stream, t);
     return hipGetLastError();
