@@ -260,21 +260,23 @@ struct Begin {
     int seq, length, before;
 };
 
-__device__ inline Share share_of(const AttnArgs &a, int total, int top)
+__device__ inline Share share_of(int units, int shares, int total, int top)
 {
     Share s;
-    s.total = total * units_of(a);
-    const int even = (int)(((unsigned)s.total + gridDim.x - 1) / gridDim.x);
+    s.total = total * units;
+    const int even = (int)(((unsigned)s.total + shares - 1) / (unsigned)shares);
     s.size = max(kMinShare, even);
     s.whole = s.size == kMinShare && top <= kWholeTiles;
     return s;
 }
 
 // The shares of this call, and where share `wg` begins (if it lies in the row).
-// tiles_in: a unit's tiles in a sequence of a length; unit_cost: what it costs beside them.
-template <typename Tiles> __device__ inline Share find_share(const AttnArgs &a, int wg, FindShare &f, Begin *begin, Tiles tiles_in, int unit_cost)
+// units: of a sequence; tiles_in: a unit's tiles in a sequence of a length; unit_cost:
+// what it costs beside them.
+template <typename Tiles>
+__device__ inline Share find_share(const AttnArgs &a, int wg, int shares, int units, FindShare &f, Begin *begin, Tiles tiles_in, int unit_cost)
 {
-    const int tid = threadIdx.x, units = units_of(a);
+    const int tid = threadIdx.x;
     *begin = Begin{0, 0, 0};
     if (a.n_seqs <= 64) {  // each wave for itself
         const int lane = tid & 63;
@@ -288,7 +290,7 @@ template <typename Tiles> __device__ inline Share find_share(const AttnArgs &a, 
             const int o = __shfl_up(up_to, d);
             up_to += lane >= d ? o : 0;
         }
-        const Share s = share_of(a, __builtin_amdgcn_readlane(up_to, 63), uniform(top));
+        const Share s = share_of(units, shares, __builtin_amdgcn_readlane(up_to, 63), uniform(top));
         const int64_t at = (int64_t)wg * s.size;
         if (s.whole || at >= s.total) return s;
         // The sequence that holds this place, counted in one unit of each.
@@ -309,7 +311,7 @@ template <typename Tiles> __device__ inline Share find_share(const AttnArgs &a, 
     for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
     if ((tid & 63) == 0) f.top[tid >> 6] = top;
     const int total = scan256(mine, &up_to, f);
-    const Share s = share_of(a, total, uniform(max(max(f.top[0], f.top[1]), max(f.top[2], f.top[3]))));
+    const Share s = share_of(units, shares, total, uniform(max(max(f.top[0], f.top[1]), max(f.top[2], f.top[3]))));
     const int64_t at = (int64_t)wg * s.size;
     if (s.whole || at >= s.total) return s;
     const int want = (int)at / units;
@@ -688,7 +690,7 @@ __global__ __launch_bounds__(256, (AttnKernel<TC, Q16, DC, R, SHORT>::PER_CU)) v
     Share share = {0, 0, true};
     Begin begin;
     if constexpr (!SHORT)
-        if (a.split) share = find_share(a, wg, lds.found, &begin, [&](int n) { return tiles_of(a, n); }, kUnitCost);
+        if (a.split) share = find_share(a, wg, (int)gridDim.x, units, lds.found, &begin, [&](int n) { return tiles_of(a, n); }, kUnitCost);
 
     // This workgroup's place: a sequence, its length and its units' tiles, a unit
     // of it, and how far into the unit's length the share has come.

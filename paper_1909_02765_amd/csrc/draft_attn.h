@@ -92,12 +92,16 @@ __device__ inline const TreeArgs &args_of(TreeArgsAt at)
 // A head size's class, and what of AttnKernel's does not hold here.
 template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeKernel : AttnKernel<TC, Q16, DC, R, false> {
     using Base = AttnKernel<TC, Q16, DC, R, false>;
+    // Of the three that a wave gives to at the end, how many at once: what LDS has room for.
+    static constexpr int GIVE = MA == 4 ? 2 : 3;
     // How far, in powers of two, scores may pass the reference of their row before it is
     // moved up to them, and what f16 probabilities are scaled by so that they still fit.
     static constexpr float SLACK = __is_same(TC, _Float16) ? 4.f : 8.f;
     static constexpr float UP = __is_same(TC, _Float16) ? 0x1p11f : 1.f;
     // Workgroups that a compute unit holds at once.
-    static constexpr int PER_CU = DC >= 192 ? 1 : 2;
+    static constexpr int PER_CU = R == kAny ? (DC >= 192 ? 1 : 2)
+                                  : sizeof(TC) == 4 ? (DC >= 192 ? 1 : DC == 64 && MA == 1 ? 3 : 2)
+                                  : MA == 1 ? (DC == 64 ? 4 : DC == 96 ? 3 : 2) : MA == 2 ? (DC == 64 ? 3 : DC <= 128 ? 2 : 1) : 2;
 };
 
 template <typename Cfg, int MA> struct TreeLds {
@@ -111,14 +115,13 @@ template <typename Cfg, int MA> struct TreeLds {
     // Values of rows that are not finite for a key that not all rows see.
     int any_odd;
     unsigned odd[16 * MA][16];
+    // Of each row each wave's maximum and sum.
+    float m[4][16 * MA], l[4][16 * MA];
     union {
         // The queries, as the lanes of the first product take them, in parts those of 32 bits.
         Words16 q[Cfg::QP][Cfg::NK][MA][64];
-        // Of 16 rows each wave's maxima, sums and outputs (the rows 4 banks apart).
-        struct {
-            float o[4][16][Cfg::DO + 4];
-            float m[4][16], l[4][16];
-        } j;
+        // What each wave gives to another of its outputs, as they lie in registers.
+        floatx4 give[Cfg::GIVE][4][MA * Cfg::NO / 4][64];
     };
 };
 
@@ -162,7 +165,7 @@ template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeRows {
     {
         const TreeArgs &t = args_of(args);
         const AttnArgs &a = t.a;
-        const int n16 = lane & 15, g = lane >> 4, ma = wave % MA, c0 = wave / MA;
+        const int ma = wave % MA, c0 = wave / MA;
         for (int i = threadIdx.x; i < 16 * MA * 16; i += 256) lds.odd[i / 16][i % 16] = 0;
         if (threadIdx.x == 0) lds.any_odd = 0;
         if constexpr (QP == 1) {
@@ -370,10 +373,16 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], i & 1 ? upper[0] : lower[0]),
                         __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], i & 1 ? upper[1] : lower[1])};
     };
-    // Whether row r sees key j, which is in the cache.
-    auto sees = [&](int r, int64_t j) {
-        if (j >= range.length) return ((lds.bits[r] >> min(j - range.length, (int64_t)63)) & 1) != 0;
-        return j >= lds.low[r] || j < all_sinks;
+    // Whether row r sees key key0 + 4g + i, i < 4, where it is in the cache.
+    auto sees = [&](int r, int64_t key0, bool *see) {
+        const unsigned long long bits = lds.bits[r];
+        const int64_t low = lds.low[r], node0 = key0 - range.length;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int node = (int)node0 + 4 * g + i;  // (of keys before the nodes the low half does not matter)
+            const int64_t key = key0 + 4 * g + i;
+            see[i] = node0 + 4 * g + i >= 0 ? ((bits >> (node & 63)) & 1) != 0 : key >= low || key < all_sinks;
+        }
     };
     // Takes values that are not finite out of a tile whose rows do not see the same keys, and marks the rows that see
     // them: bit c * VV + i of odd[row][n] stands for value (n + 16c) * VV + i.  (Hardly ever.)
@@ -402,8 +411,11 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
             if (!seen[r] || odd == 0) continue;
             lds.any_odd = 1;
 #pragma unroll 1
-            for (int row = 0; row < 16 * MA; ++row)
-                if (sees(row, key0 + 4 * g + r)) atomicOr(&lds.odd[row][n16], odd);
+            for (int row = 0; row < 16 * MA; ++row) {
+                bool see[4];
+                sees(row, key0, see);
+                if (see[r]) atomicOr(&lds.odd[row][n16], odd);
+            }
         }
     };
 
@@ -470,9 +482,12 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         }
         if (special) {
 #pragma unroll
-            for (int ma = 0; ma < MA; ++ma)
+            for (int ma = 0; ma < MA; ++ma) {
+                bool see[4];
+                sees(ma * 16 + n16, key0, see);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[ma][r] = sees(ma * 16 + n16, key0 + 4 * g + r) ? s[ma][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r) s[ma][r] = see[r] ? s[ma][r] : -INFINITY;
+            }
         }
 #pragma unroll
         for (int ma = 0; ma < MA; ++ma) {
@@ -559,63 +574,105 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         load_v(j + 1);
     }
 
-    const int n_rows = args_of(args).rows;
-    // Join the waves: lane (n, g) holds values (4g + r + 16c) * VV + i of row n.
+    // Join the waves.  Lane (n, g) holds values (4g + r + 16c) * VV + i of row n; what is no
+    // node has seen keys of the sequence, and none counts.
 #pragma unroll
     for (int ma = 0; ma < MA; ++ma) {
-        float sum = l[ma];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (row_in_unit(seg, 16 * MA, ma * 16) >= n_rows) break;
-        __syncthreads();  // the queries, or what the last rows left, have been read; all odd values are marked
-        if (lds.any_odd) {
+        l[ma] += __shfl_xor(l[ma], 16);
+        l[ma] += __shfl_xor(l[ma], 32);
+        if (g == 0) {
+            const bool real = lds.bits[ma * 16 + n16] != 0;
+            lds.m[wave][ma * 16 + n16] = real ? m[ma] : -INFINITY;
+            lds.l[wave][ma * 16 + n16] = real ? l[ma] : 0.f;
+        }
+    }
+    __syncthreads();  // the queries have been read; all odd values are marked
+    // A quarter of the values of all rows to each wave, of one block of rows: the others give it theirs.
+    constexpr int QUARTER = MA * NO / 4;
+    const int my_block = wave * MA / 4;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int ma = 0; ma < MA; ++ma) {
+        float mw[4], most = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            mw[w] = lds.m[w][ma * 16 + n16];
+            most = fmaxf(most, mw[w]);
+        }
+        const float base = most == -INFINITY ? 0.f : most;
+        const bool real = lds.bits[ma * 16 + n16] != 0;
+        const float f = real ? __builtin_amdgcn_exp2f(m[ma] - base) : 0.f;
+        if (ma == my_block) {
+            top = most;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sum += lds.l[w][ma * 16 + n16] * __builtin_amdgcn_exp2f(mw[w] - base);
+        }
+#pragma unroll
+        for (int i = 0; i < NO; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[ma][i][r] = real ? o[ma][i][r] * f : 0.f;
+    }
+    if (lds.any_odd) {
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const unsigned odd = lds.odd[ma * 16 + n16][4 * g + r];
 #pragma unroll
                 for (int i = 0; i < NO; ++i) o[ma][i][r] = (odd >> i) & 1 ? __builtin_nanf("") : o[ma][i][r];
             }
-        }
-        const bool real = lds.bits[ma * 16 + n16] != 0;  // (what is no node has seen keys of the sequence: none counts)
-        if (g == 0) {
-            lds.j.m[wave][n16] = real ? m[ma] : -INFINITY;
-            lds.j.l[wave][n16] = real ? sum : 0.f;
-        }
+    }
+    floatx4 mine[QUARTER];
+    // Each wave's quarter by numbers known at compile time.  (The barriers differ so that the four stay four: made one,
+    // with a number found at run time, it would put all outputs into memory, from the loop over the tiles on.)
+    auto quarter = [&](int w, auto f) {
+        auto one = [&](auto number) {
+            constexpr int k = decltype(number)::value;
+            if (w != k) return;
 #pragma unroll
-        for (int c = 0; c < NV; ++c)
+            for (int i = 0; i < QUARTER; ++i) f(i, o[(k * QUARTER + i) / NO][(k * QUARTER + i) % NO]);
+            __builtin_amdgcn_sched_barrier(k);
+        };
+        one(std::integral_constant<int, 0>{});
+        one(std::integral_constant<int, 1>{});
+        one(std::integral_constant<int, 2>{});
+        one(std::integral_constant<int, 3>{});
+    };
+    quarter(wave, [&](int i, const floatx4 &v) { mine[i] = v; });
+    if constexpr (Cfg::GIVE == 3) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                Pack<float, VV> p;
-#pragma unroll
-                for (int i = 0; i < VV; ++i) p.v[i] = real ? o[ma][c * VV + i][r] : 0.f;
-                *reinterpret_cast<Pack<float, VV> *>(&lds.j.o[wave][n16][(4 * g + r + 16 * c) * VV]) = p;
-            }
+        for (int step = 1; step < 4; ++step)
+            quarter((wave + step) & 3, [&](int i, const floatx4 &v) { lds.give[step - 1][wave][i][lane] = v; });
         __syncthreads();
-        constexpr int PER = DC / 4;
-        const TreeArgs &t = args_of(args);
-        const int row0 = row_in_unit(seg, 16 * MA, ma * 16), rows = min(16, t.rows - row0);
+#pragma unroll
+        for (int step = 1; step < 4; ++step)
+#pragma unroll
+            for (int i = 0; i < QUARTER; ++i) mine[i] += lds.give[step - 1][(wave - step) & 3][i][lane];
+    } else {
+        // (What a step reads the one after the next writes, behind the next one's barrier.)
 #pragma unroll 1
-        for (int i = threadIdx.x; i < rows * PER; i += 256) {
-            const int r = i / PER, d = (i - r * PER) * 4;
-            if (d >= t.a.dim) continue;
-            floatx4 v[4];
-            float mw[4], lw[4];
+        for (int step = 1; step < 4; ++step) {
+            quarter((wave + step) & 3, [&](int i, const floatx4 &v) { lds.give[step & 1][wave][i][lane] = v; });
+            __syncthreads();
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                v[w] = *reinterpret_cast<const floatx4 *>(&lds.j.o[w][r][d]);
-                mw[w] = lds.j.m[w][r];
-                lw[w] = lds.j.l[w][r];
-            }
-            const float top = fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3])), base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float f = __builtin_amdgcn_exp2f(mw[w] - base);
-                v[w] *= f;
-                lw[w] *= f;
-            }
-            put(t, row0 + r, ma * 16 + r, d, (v[0] + v[1]) + (v[2] + v[3]), top, (lw[0] + lw[1]) + (lw[2] + lw[3]));
+            for (int i = 0; i < QUARTER; ++i) mine[i] += lds.give[step & 1][(wave - step) & 3][i][lane];
         }
     }
+    const int r_block = my_block * 16 + n16, first = wave * QUARTER % NO;
+    if (row_in_unit(seg, 16 * MA, r_block) >= args_of(args).rows) return;
+    constexpr int POW = QUARTER & -QUARTER, RUN = POW < VV ? POW : VV;  // values that lie together
+    put(args_of(args), row_in_unit(seg, 16 * MA, r_block), r_block, top, sum, first == 0 && g == 0, [&](auto &&give) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int k = 0; k < QUARTER; k += RUN) {
+                Pack<float, RUN> p;
+#pragma unroll
+                for (int i = 0; i < RUN; ++i) p.v[i] = mine[k + i][r];
+                const int c = (first + k) / VV, i = (first + k) % VV;
+                give((4 * g + r + 16 * c) * VV + i, p);
+            }
+    });
 }
 
 template <typename TC, bool Q16, int DC, Rows R, int MA>
@@ -629,27 +686,30 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
     const TreeArgs &t = args_of(args);
     const AttnArgs &a = t.a;
 
-    // (Neighbouring shares stay on one die: see decode_attn.h.)
+    // (Neighbours stay on one die: see decode_attn.h.)  The blocks of a share's rows are
+    // neighbours and take its keys at the same time, so that their die's cache has them
+    // for all but the first.
     const int die = blockIdx.x & 7, dies = gridDim.x >> 3;
-    const int units = units_of(a), wg = die * dies + min(die, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
+    const int units = a.kv_heads, wg = die * dies + min(die, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
+    const int share_at = wg / a.blocks, block = wg - share_at * a.blocks, shares = (int)gridDim.x / a.blocks;
     Share share = {0, 0, true};
     Begin begin;
-    if (a.split) share = find_share(a, wg, lds.found, &begin, [&](int n) { return tree_tiles(t, n); }, unit_cost);
+    if (a.split) share = find_share(a, share_at, shares, units, lds.found, &begin, [&](int n) { return tree_tiles(t, n); }, unit_cost);
 
     // This workgroup's place: a sequence, its length and its units' tiles, a unit
     // of it, and how far into the unit's length the share has come.
     int seq, length, unit, tiles_all, x0 = 0;
     int at = 0, last = 0;
-    if (a.split && !a.part_of_unit && threadIdx.x == 0) a.parts[wg] = AttnPart{0, 0, 0, 0};  // (whatever follows, the join reads it)
+    if (a.split && !a.part_of_unit && block == 0 && threadIdx.x == 0) a.parts[share_at] = AttnPart{0, 0, 0, 0};  // (whatever follows, the join reads it)
     if (share.whole) {
-        if (wg >= a.n_seqs * units) return;
-        seq = wg / units;
-        unit = wg - seq * units;
+        if (share_at >= a.n_seqs * units) return;
+        seq = share_at / units;
+        unit = share_at - seq * units;
         length = uniform(a.lengths[seq]);
         tiles_all = tree_tiles(t, length);
     } else {
-        if ((int64_t)wg * share.size >= share.total) return;
-        at = wg * share.size;
+        if ((int64_t)share_at * share.size >= share.total) return;
+        at = share_at * share.size;
         last = (int)min((int64_t)at + share.size, (int64_t)share.total);
         seq = begin.seq;
         length = begin.length;
@@ -660,47 +720,49 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
     }
 
     const bool split = a.split, part_of_unit = a.part_of_unit;
-    const int n_seqs = a.n_seqs, blocks = a.blocks;
+    const int n_seqs = a.n_seqs;
     for (;;) {
         const int x1 = share.whole ? tiles_all + unit_cost : min(tiles_all + unit_cost, x0 + (last - at));
         const int tile0 = max(0, x0 - unit_cost), seg_tiles = max(0, x1 - unit_cost) - tile0;
         if (seg_tiles == 0) return;  // the share ends before the unit's first tile
         TreeSegment seg;
         seg.seq = seq;
-        seg.kvh = unit / blocks;
-        seg.block = unit - seg.kvh * blocks;
+        seg.kvh = unit;
+        seg.block = block;
         seg.tile0 = tile0;
         seg.tile1 = tile0 + seg_tiles;
         seg.range = tree_range(args_of(args), length);
         if (seg.range.end == 0) seg.tile1 = tile0;  // (no keys, and perhaps no pool)
         const bool all = seg_tiles == tiles_all;  // of the unit's tiles
-        tree_segment<TC, Q16, DC, R, MA>(args, seg, lds, [&](const TreeArgs &t, int row, int r, int d, floatx4 v, float top, float sum) {
+        // Row `row` of the unit, r of its block: its maximum and sum, and its values, in packs, from `each`.
+        tree_segment<TC, Q16, DC, R, MA>(args, seg, lds, [&](const TreeArgs &t, int row, int r, float top, float sum, bool lead, auto each) {
             const AttnArgs &a = t.a;
-            auto put = [&](auto *to) {
-                using TO = std::remove_reference_t<decltype(*to)>;
-                Pack<TO, 4> p;
+            auto put = [&](auto *to, float by) {
+                each([&](int d, auto p) {
+                    constexpr int N = sizeof(p.v) / sizeof(float);
+                    using TO = std::remove_reference_t<decltype(*to)>;
+                    Pack<TO, N> q;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) p.v[k] = (TO)v[k];
-                if (d + 4 <= a.dim) {
-                    store_loose<TO, 4>(to + d, p);
-                    return;
-                }
-                to[d] = p.v[0];
-                if (d + 1 < a.dim) to[d + 1] = p.v[1];
-                if (d + 2 < a.dim) to[d + 2] = p.v[2];
+                    for (int k = 0; k < N; ++k) q.v[k] = (TO)(p.v[k] * by);
+                    if (d + N <= a.dim) {
+                        store_loose<TO, N>(to + d, q);
+                        return;
+                    }
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if (d + k < a.dim) to[d + k] = q.v[k];
+                });
             };
             if (all) {
                 const int node = t.by_group.of(row), head = seg.kvh * a.group + (row - node * a.group);
                 const int64_t at_row = (int64_t)seg.seq * t.n_nodes + node;
-                v *= sum == 0.f ? 0.f : 1.f / (sum * Cfg::UP);
-                put((TQ *)a.out + at_row * a.o_row + (int64_t)head * a.o_head);
-                if (d == 0 && a.lse) a.lse[at_row * a.q_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+                put((TQ *)a.out + at_row * a.o_row + (int64_t)head * a.o_head, sum == 0.f ? 0.f : 1.f / (sum * Cfg::UP));
+                if (lead && a.lse) a.lse[at_row * a.q_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
             } else {
                 // The part that begins a unit, or the one that goes on with it.
                 const int64_t part = ((int64_t)wg * 2 + (seg.tile0 == 0 ? 1 : 0)) * a.part_heads + r;
-                v *= 1.f / Cfg::UP;
-                put(a.part_o + part * a.dim);
-                if (d == 0) {
+                put(a.part_o + part * a.dim, 1.f / Cfg::UP);
+                if (lead) {
                     a.part_ml[part * 2] = top;
                     a.part_ml[part * 2 + 1] = sum;
                 }
@@ -708,15 +770,15 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
         });
         const AttnArgs &a = args_of(args).a;
         // Who begins a unit says whether others go on with it.
-        if (split && threadIdx.x == 0 && tile0 == 0) {
+        if (split && block == 0 && threadIdx.x == 0 && tile0 == 0) {
             const int rest = tiles_all - seg_tiles;
             const int count = all ? 0 : 1 + (int)(((unsigned)rest + share.size - 1) / (unsigned)share.size);
-            if (part_of_unit) a.parts[seq * units + unit] = AttnPart{seq, unit, wg, count};
-            else if (!all) a.parts[wg] = AttnPart{seq, unit, wg, count};
+            if (part_of_unit) a.parts[seq * units + unit] = AttnPart{seq, unit, share_at, count};
+            else if (!all) a.parts[share_at] = AttnPart{seq, unit, share_at, count};
         }
         __syncthreads();  // the LDS that the next unit's waves write has been read
         if (share.whole) {
-            const int u = seq * units + unit + (int)gridDim.x;
+            const int u = seq * units + unit + shares;
             if (!split || u >= n_seqs * units) return;
             seq = u / units;
             unit = u - seq * units;
@@ -755,25 +817,32 @@ template <typename TC, bool Q16, int DC> hipError_t tree_split_launch(const Tree
     return launch(std::integral_constant<Rows, kAny>{}, std::integral_constant<int, 1>{});
 }
 
-template <typename TC, bool Q16> hipError_t tree_split_by_dim(const TreeArgs &t, hipStream_t stream)
-{
-    if (t.a.dim <= 64) return tree_split_launch<TC, Q16, 64>(t, stream);
-    if (t.a.dim <= 96) return tree_split_launch<TC, Q16, 96>(t, stream);
-    if (t.a.dim <= 128) return tree_split_launch<TC, Q16, 128>(t, stream);
-    if (t.a.dim <= 192) return tree_split_launch<TC, Q16, 192>(t, stream);
-    return tree_split_launch<TC, Q16, 256>(t, stream);
-}
-
 // Of a head size's class: the most row blocks of a workgroup, and the
 // workgroups that the card holds at once.
+template <typename TC, bool Q16, typename F> auto tree_by_class(int dim, F f)
+{
+    if (dim <= 64) return f(std::integral_constant<int, 64>{});
+    if (dim <= 96) return f(std::integral_constant<int, 96>{});
+    if (dim <= 128) return f(std::integral_constant<int, 128>{});
+    if (dim <= 192) return f(std::integral_constant<int, 192>{});
+    return f(std::integral_constant<int, 256>{});
+}
+template <typename TC, bool Q16> hipError_t tree_split_by_dim(const TreeArgs &t, hipStream_t stream)
+{
+    return tree_by_class<TC, Q16>(t.a.dim, [&](auto dc) { return tree_split_launch<TC, Q16, decltype(dc)::value>(t, stream); });
+}
 template <typename TC, bool Q16> int tree_most_by_dim(int dim)
 {
-    return dim <= 64 ? kMostBlocks<TC, 64> : dim <= 96 ? kMostBlocks<TC, 96> : dim <= 128 ? kMostBlocks<TC, 128> : dim <= 192 ? kMostBlocks<TC, 192> : kMostBlocks<TC, 256>;
+    return tree_by_class<TC, Q16>(dim, [](auto dc) { return kMostBlocks<TC, decltype(dc)::value>; });
 }
-template <typename TC, bool Q16> int tree_card_by_dim(int dim, int blocks)
+template <typename TC, bool Q16> int tree_card_by_dim(int dim, bool pieces, int blocks)
 {
-    (void)blocks;
-    return kAttnCus * (dim <= 128 ? 2 : 1);
+    return kAttnCus * tree_by_class<TC, Q16>(dim, [&](auto dc) {
+        constexpr int DC = decltype(dc)::value;
+        if (!pieces) return TreeKernel<TC, Q16, DC, kAny, 1>::PER_CU;
+        return blocks == 4 ? TreeKernel<TC, Q16, DC, kPieces, 4>::PER_CU
+               : blocks == 2 ? TreeKernel<TC, Q16, DC, kPieces, 2>::PER_CU : TreeKernel<TC, Q16, DC, kPieces, 1>::PER_CU;
+    });
 }
 
 }  // namespace

@@ -10,7 +10,7 @@ namespace ilpm {
 #define ILPM_TREE_KERNELS(name)                                          \
     hipError_t tree_split_##name(const TreeArgs &t, hipStream_t stream); \
     int tree_most_##name(int dim);                                       \
-    int tree_card_##name(int dim, int blocks);
+    int tree_card_##name(int dim, bool pieces, int blocks);
 ILPM_TREE_KERNELS(f32)
 ILPM_TREE_KERNELS(f16)
 ILPM_TREE_KERNELS(f16_q32)
@@ -31,6 +31,14 @@ __device__ inline void store_f32(void *p, int64_t i, int dtype, float v)
     else ((__bf16 *)p)[i] = (__bf16)v;
 }
 
+// Part i of a unit, for a row of it: of the workgroup of the row's block that holds the
+// unit's i-th share, its part that begins a unit or the one that goes on with it.
+__device__ inline int64_t part_at(const TreeArgs &t, const AttnPart &u, int row, int i)
+{
+    const int block = row / (16 * t.row_blocks), in_block = row - block * 16 * t.row_blocks;
+    return ((((int64_t)u.first + i) * t.a.blocks + block) * 2 + (i == 0)) * t.a.part_heads + in_block;
+}
+
 // Joins the parts of the unit at place blockIdx.x, for its row blockIdx.y and 64
 // values of it, blockIdx.z, as attn_decode's parts are (attn_join).
 template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
@@ -41,11 +49,9 @@ template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
     const AttnArgs &a = t.a;
     const AttnPart u = a.parts[blockIdx.x];
     if (u.count == 0) return;
-    const int kvh = u.unit / a.blocks, row = (u.unit - kvh * a.blocks) * 16 * t.row_blocks + (int)blockIdx.y;
-    if (row >= t.rows) return;
-    const int node = t.by_group.of(row), head = kvh * a.group + (row - node * a.group), tid = threadIdx.x;
+    const int row = blockIdx.y, node = t.by_group.of(row), head = u.unit * a.group + (row - node * a.group), tid = threadIdx.x;
     const int64_t out_row = (int64_t)u.seq * t.n_nodes + node;
-    auto slot = [&](int i) { return ((((int64_t)u.first + i) * 2 + (i == 0)) * a.part_heads + blockIdx.y); };
+    auto slot = [&](int i) { return part_at(t, u, row, i); };
     const int group = tid / T, d = (int)blockIdx.z * 64 + tid % T * V;
     auto part = [&](int i) {
         Pack<float, V> p = {};
@@ -110,12 +116,11 @@ __global__ __launch_bounds__(256) void tree_join_rows(TreeArgs t, int lanes, Div
     const AttnPart u = a.parts[blockIdx.x];
     if (u.count == 0) return;
     const int r = by_lanes.of((int)threadIdx.x), lane = (int)threadIdx.x - r * lanes, per = by_lanes.of(256);
-    const int in_block = (int)blockIdx.y * per + r, d = lane * 4;
-    const int kvh = u.unit / a.blocks, row = (u.unit - kvh * a.blocks) * 16 * t.row_blocks + in_block;
-    if (r >= per || in_block >= a.part_heads || row >= t.rows) return;
-    const int node = t.by_group.of(row), head = kvh * a.group + (row - node * a.group);
+    const int row = (int)blockIdx.y * per + r, d = lane * 4;
+    if (r >= per || row >= t.rows) return;
+    const int node = t.by_group.of(row), head = u.unit * a.group + (row - node * a.group);
     const int64_t out_row = (int64_t)u.seq * t.n_nodes + node;
-    auto slot = [&](int i) { return (((int64_t)u.first + i) * 2 + (i == 0)) * a.part_heads + in_block; };
+    auto slot = [&](int i) { return part_at(t, u, row, i); };
     float top = -INFINITY, total = 0.f;
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
     // (A part at a time with the maximum so far: in their order, two accesses each that do not wait for others.)
@@ -138,8 +143,9 @@ __global__ __launch_bounds__(256) void tree_join_rows(TreeArgs t, int lanes, Div
 
 }  // namespace
 
-// As attn_plan: either a unit (a key head's rows, up to 16 * row_blocks of them) goes
-// to a workgroup, or as many workgroups as the card holds share all tiles.
+// As attn_plan: either a unit (a key head of a sequence) goes to a workgroup for each
+// of its blocks of rows, or as many workgroups as the card holds share all tiles,
+// each share a workgroup for each block.
 size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
 {
     AttnArgs *a = &t->a;
@@ -153,7 +159,7 @@ size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
     const int most = t->pieces ? ILPM_TREE_OF(tree_most, a->dim) : 1;
     t->row_blocks = std::min(most, t->rows > 32 ? 4 : t->rows > 16 ? 2 : 1);
     a->blocks = std::max(1, ceil_div(t->rows, 16 * t->row_blocks));
-    const int64_t units = (int64_t)a->n_seqs * a->kv_heads * a->blocks;
+    const int64_t units = (int64_t)a->n_seqs * a->kv_heads;
     const int64_t sinks = a->window > 0 ? std::min<int64_t>(t->sinks, max_len) : 0;
     const int64_t keys = (a->window > 0 ? std::min<int64_t>(max_len, a->window) : max_len) + t->n_nodes;
     const int64_t tiles = std::max<int64_t>(1, (keys + 15) / 16 + (sinks + 15) / 16);
@@ -161,14 +167,15 @@ size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
     const int64_t span = (((int64_t)a->capacity + 15) / 16 + 2 + tree_unit_cost(t->row_blocks)) * units;
     a->split = tiles > kWholeTiles && units > 0 && (span < INT_MAX || units == 1);
     if (!a->split) {
-        a->grid = (int)units;
+        a->grid = (int)units * a->blocks;
         return 0;
     }
-    const int card = ILPM_TREE_OF(tree_card, a->dim, t->row_blocks);
+    const int card = ILPM_TREE_OF(tree_card, a->dim, t->pieces, t->row_blocks);
 #undef ILPM_TREE_OF
-    a->grid = (int)std::min<int64_t>({card, kMaxParts, units * ((tiles + tree_unit_cost(t->row_blocks) + kMinShare - 1) / kMinShare)});
+    const int shares = (int)std::min<int64_t>({std::max(1, std::min(card, kMaxParts) / a->blocks), units * ((tiles + tree_unit_cost(t->row_blocks) + kMinShare - 1) / kMinShare)});
+    a->grid = shares * a->blocks;
     a->part_heads = std::min(t->rows, 16 * t->row_blocks);
-    a->part_of_unit = units <= a->grid;
+    a->part_of_unit = units <= shares;
     return (size_t)a->grid * (sizeof(AttnPart) + 2 * a->part_heads * (size_t)(a->dim + 2) * sizeof(float));
 }
 
@@ -182,13 +189,13 @@ hipError_t tree_launch(const TreeArgs &t, int cache_dtype, hipStream_t stream)
                          : cache_dtype == ILPM_F16 ? (q32 ? tree_split_f16_q32(t, stream) : tree_split_f16(t, stream))
                                                    : (q32 ? tree_split_bf16_q32(t, stream) : tree_split_bf16(t, stream));
     if (e != hipSuccess || !a.split) return e;
-    const int joins = a.part_of_unit ? a.n_seqs * a.kv_heads * a.blocks : a.grid;
-    if (a.dim % 4 == 0 && (int64_t)joins * a.part_heads * ceil_div(a.dim, 64) > 8 * kAttnCus) {
+    const int joins = a.part_of_unit ? a.n_seqs * a.kv_heads : a.grid / a.blocks;
+    if (a.dim % 4 == 0 && (int64_t)joins * t.rows * ceil_div(a.dim, 64) > 8 * kAttnCus) {
         const int lanes = a.dim / 4;
-        hipLaunchKernelGGL(tree_join_rows, dim3(joins, ceil_div(a.part_heads, 256 / lanes)), dim3(256), 0, stream, t, lanes, Divisor((unsigned)lanes));
+        hipLaunchKernelGGL(tree_join_rows, dim3(joins, ceil_div(t.rows, 256 / lanes)), dim3(256), 0, stream, t, lanes, Divisor((unsigned)lanes));
         return hipGetLastError();
     }
-    const dim3 grid(joins, a.part_heads, ceil_div(a.dim, 64));
+    const dim3 grid(joins, t.rows, ceil_div(a.dim, 64));
     if (a.dim % 4) hipLaunchKernelGGL((tree_join<1>), grid, dim3(256), 0, stream, t);
     else hipLaunchKernelGGL((tree_join<4>), grid, dim3(256), 0, stream, t);
     return hipGetLastError();

@@ -5,6 +5,6 @@ namespace ilpm {
 
 hipError_t tree_split_bf16_q32(const TreeArgs &t, hipStream_t stream) { return tree_split_by_dim<__bf16, false>(t, stream); }
 int tree_most_bf16_q32(int dim) { return tree_most_by_dim<__bf16, false>(dim); }
-int tree_card_bf16_q32(int dim, int blocks) { return tree_card_by_dim<__bf16, false>(dim, blocks); }
+int tree_card_bf16_q32(int dim, bool pieces, int blocks) { return tree_card_by_dim<__bf16, false>(dim, pieces, blocks); }
 
 }  // namespace ilpm
