@@ -713,6 +713,8 @@ typedef struct ilpm_verify_args {
     int dtype; /* of target and draft */
 } ilpm_verify_args;
 int ilpm_verify_drafts(const ilpm_verify_args *args, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ilpm_verify_drafts (0 where it needs none).  Pure host. */
 int ilpm_verify_drafts_workspace_size(int n_seqs, int n_nodes, int vocab, size_t *bytes);
 
 /*

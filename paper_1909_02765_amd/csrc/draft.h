@@ -21,20 +21,18 @@ hipError_t append_norm_launch(const AppendNormArgs &n, int x_dtype, int cache_dt
 constexpr int kVerifyChunk = 4096;  // probabilities that a workgroup sums
 
 // Where a sequence's walk ended, and what is left of that node's row: a p - b q, or p
-// without the tokens gone[0..n_gone).
+// without the tokens of the children that are bits of `gone`.
 struct VerifyEnd {
-    int node, n_gone;  // node -1: no tree
+    int node;  // -1: no tree
     double a, b;
-    int gone[ILPM_MAX_NODES];
-};
-struct VerifySum {
-    double left, all;  // of a chunk: of what is left of the row, of the row
+    unsigned long long gone;
+    int token[ILPM_MAX_NODES];
 };
 struct VerifyArgs {
     ilpm_verify_args v;
-    int chunks;  // of a row
+    int chunks;  // of a row; 0: short rows, without a workspace
     VerifyEnd *ends;
-    VerifySum *sums;  // [n_seqs][chunks]
+    double *sums;  // [n_seqs][chunks]: of what is left of the row
 };
 size_t verify_plan(VerifyArgs *a);
 void verify_workspace(VerifyArgs *a, void *ws);

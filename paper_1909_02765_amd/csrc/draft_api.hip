@@ -260,7 +260,7 @@ int verify_drafts(const ilpm_verify_args *args, void *workspace, size_t workspac
         if ((uintptr_t)p % 4) return ILPM_ERR_INVALID_ARG;
 
     const int64_t e = element_bytes(v.dtype), nodes = (int64_t)v.n_seqs * v.n_nodes * 4, seqs = (int64_t)v.n_seqs * 4;
-    const bool has_ws = workspace != nullptr;
+    const bool has_ws = workspace && need > 0;
     const Span write[] = {flat_span(v.path, nodes), flat_span(v.counts, seqs), flat_span(v.next_tokens, seqs),
                           flat_span(workspace, (int64_t)need)};
     const int writes = has_ws ? 4 : 3;
@@ -277,10 +277,12 @@ int verify_drafts(const ilpm_verify_args *args, void *workspace, size_t workspac
     int dev = 0;
     if ((rc = api_device_check(&dev)) != ILPM_OK) return rc;
     void *ws = workspace;
-    if (!ws) rc = api_workspace(dev, need, stream, &ws);
-    else if (workspace_bytes < need) rc = ILPM_ERR_WORKSPACE;
-    if (rc != ILPM_OK) return rc;
-    verify_workspace(&a, ws);
+    if (need > 0) {
+        if (!ws) rc = api_workspace(dev, need, stream, &ws);
+        else if (workspace_bytes < need) rc = ILPM_ERR_WORKSPACE;
+        if (rc != ILPM_OK) return rc;
+        verify_workspace(&a, ws);
+    }
     (void)hipGetLastError();
     const hipError_t err = verify_launch(a, stream);
     return err == hipSuccess ? ILPM_OK : api_hip_fail(err);

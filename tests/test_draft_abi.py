@@ -147,7 +147,7 @@ def verify(tokens=GB, parents=2 * GB, target=10 * GB, draft=20 * GB, strides=(7 
     dict(vocab=0), dict(vocab=-5), dict(strides=(-1, 1000, 7000, 1000)), dict(strides=(7000, -1, 7000, 1000)),
     dict(strides=(7000, 1000, -1, 1000)), dict(strides=(7000, 1000, 7000, 1 << 41)),
     dict(path=GB), dict(path=2 * GB), dict(path=10 * GB + 4000), dict(counts=3 * GB), dict(counts=4 * GB), dict(last=5 * GB),
-    dict(last=20 * GB), dict(ws=10 * GB), dict(ws=4 * GB), dict(ws=GB), dict(ws=6 * GB)])
+    dict(last=20 * GB)] + [dict(ws=n * GB, target=30 * GB, draft=40 * GB, vocab=1000000, strides=(7000000, 1000000) * 2) for n in (30, 40, 1, 2, 3, 4, 5, 6)])
 def test_verification_refuses(kw):
     assert verify(**kw) == ilpm.ERR_INVALID_ARG
 
@@ -162,7 +162,8 @@ def test_verification_of_nothing_and_its_workspace():
     assert ilpm.lib.ilpm_verify_drafts(None, None, 0, None) == ilpm.ERR_INVALID_ARG
     need = ctypes.c_size_t(0)
     size = ilpm.lib.ilpm_verify_drafts_workspace_size
-    assert size(4, 7, 1000, ctypes.byref(need)) == ilpm.OK and need.value > 0
+    assert size(4, 7, 1000000, ctypes.byref(need)) == ilpm.OK and need.value > 0
+    assert size(4, 7, 1000, ctypes.byref(need)) == ilpm.OK
     assert size(0, 7, 1000, ctypes.byref(need)) == ilpm.OK and need.value == 0
     assert size(4, 7, 1000, None) == ilpm.ERR_INVALID_ARG
     assert size(4, 0, 1000, ctypes.byref(need)) == ilpm.ERR_INVALID_ARG
