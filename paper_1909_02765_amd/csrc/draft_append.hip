@@ -7,6 +7,8 @@
 // neighbouring lanes of one wave, in the packs that the rotation takes.  All of a
 // head is read before any of it is written, by one wave, which lets queries be
 // normed in place.
+#include <algorithm>
+
 #include "draft.h"
 
 namespace ilpm {
@@ -17,11 +19,9 @@ struct Place {
     int page, slot;
 };
 
-__device__ inline Place place_of(const AppendNormArgs &n, int t, const Divisor &by_page)
+__device__ inline Place place_of(const AppendArgs &a, int seq, int slot, const Divisor &by_page)
 {
-    const AppendArgs &a = n.a;
     Place p = {-1, 0};
-    const int seq = a.seq_ids[t], slot = n.slots[t];
     if (seq < 0 || seq >= a.n_seqs || slot < 0) return p;
     const int at = by_page.of(slot);
     if (at >= a.max_pages) return p;
@@ -34,9 +34,30 @@ __device__ inline Place place_of(const AppendNormArgs &n, int t, const Divisor &
 
 template <typename TP> __device__ inline float weight(const void *w, int i) { return w ? (float)((const TP *)w)[i] : 1.f; }
 
-__device__ inline float sum_lanes(float v, int lanes)
+// Sums over 2^log neighbouring lanes, in the vector unit.  (Once the lanes of a
+// four or eight hold the same, a mirror is as good a partner as any.)
+template <int CTRL> __device__ inline float dpp(float v)
 {
-    for (int d = 1; d < lanes; d <<= 1) v += __shfl_xor(v, d);
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ inline float sum_lanes(float v, int log)
+{
+    if (log > 0) v += dpp<0xb1>(v);   // of pairs
+    if (log > 1) v += dpp<0x4e>(v);   // of fours
+    if (log > 2) v += dpp<0x141>(v);  // eight mirrored
+    if (log > 3) v += dpp<0x140>(v);  // sixteen mirrored
+    if (log > 4) {
+        const unsigned x = __builtin_bit_cast(unsigned, v);
+        const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        const unsigned a0 = a[0], a1 = a[1];
+        v = __builtin_bit_cast(float, a0) + __builtin_bit_cast(float, a1);
+    }
+    if (log > 5) {
+        const unsigned x = __builtin_bit_cast(unsigned, v);
+        const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        const unsigned b0 = b[0], b1 = b[1];
+        v = __builtin_bit_cast(float, b0) + __builtin_bit_cast(float, b1);
+    }
     return v;
 }
 
@@ -59,7 +80,7 @@ template <typename TX, typename TC, typename TP> __global__ __launch_bounds__(25
     const bool turn = !value && a.rot_dim > 0 && pos >= 0 && pos < a.n_positions;
     Place at = {-1, 0};
     if (!query) {
-        at = place_of(n, t, by_page);
+        at = place_of(a, a.seq_ids[t], n.slots[t], by_page);
         if (at.page < 0 || (a.rot_dim > 0 && !(pos >= 0 && pos < a.n_positions))) return;
     }
     const TX *src = query ? (const TX *)a.q + (int64_t)t * a.q_row + h * a.q_head
@@ -70,10 +91,10 @@ template <typename TX, typename TC, typename TP> __global__ __launch_bounds__(25
         sum += row[e];
     }
     if (!value && n.norm != ILPM_NORM_NONE) {
-        const float inv = 1.f / (float)a.dim, mean = n.norm == ILPM_NORM_LAYER ? sum_lanes(sum, 64) * inv : 0.f;
+        const float inv = 1.f / (float)a.dim, mean = n.norm == ILPM_NORM_LAYER ? sum_lanes(sum, 6) * inv : 0.f;
         float var = 0.f;
         for (int e = lane; e < a.dim; e += 64) var += (row[e] - mean) * (row[e] - mean);
-        const float rstd = 1.f / sqrtf(sum_lanes(var, 64) * inv + n.eps);
+        const float rstd = 1.f / sqrtf(sum_lanes(var, 6) * inv + n.eps);
         const void *w = query ? n.q_w : n.k_w;
         for (int e = lane; e < a.dim; e += 64) row[e] = (row[e] - mean) * rstd * weight<TP>(w, e);
     }
@@ -100,12 +121,200 @@ template <typename TX, typename TC, typename TP> __global__ __launch_bounds__(25
     else put((TC *)a.kc + (int64_t)at.page * a.kc_page + (int64_t)at.slot * a.kc_slot + h * a.kc_head);
 }
 
+constexpr int kCardGroups = 256 * 8;  // workgroups of 256 threads that the card holds at once
+
+// N weights from i on.
+template <typename TP, int N> __device__ inline void load_weights(const void *w, int i, float *to)
+{
+    Pack<TP, N> p;
+    if (w) p = load_loose<TP, N>((const TP *)w + i);
+#pragma unroll
+    for (int k = 0; k < N; ++k) to[k] = w ? (float)p.v[k] : 1.f;
+}
+
+// The packs of VEC that cover n elements: where they do not divide, the last one
+// ends with them, over some of the one before it.
+template <int VEC> __host__ __device__ inline int packs(int n) { return (n + VEC - 1) / VEC; }
+template <int VEC> __device__ inline int pack_at(int u, int n) { return min(u * VEC, n - VEC); }
+
+// 1 / sqrt(x) to a unit or two of the last place, of numbers below the normal ones too.
+__device__ inline float rsqrt_of(float x)
+{
+    const bool small = x < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(small ? x * 0x1p100f : x) * (small ? 0x1p50f : 1.f);
+}
+
+// How a head lies over lanes: the turned part and the rest in lanes of two packs of
+// VEC elements where they divide (halves always: a pack and its partners), else
+// of one.
+template <int VEC> struct Lanes {
+    int turns, rest;            // elements that packs begin in: of halves the first half
+    bool two_turned, two_rest;
+    int turned, all;            // lanes
+    __host__ __device__ Lanes(int dim, int rot, bool pairs)
+    {
+        rest = dim - rot;
+        two_rest = rest % (2 * VEC) == 0;
+        two_turned = !pairs || rot % (2 * VEC) == 0;
+        turns = two_turned ? rot / 2 : rot;
+        turned = packs<VEC>(turns);
+        all = turned + packs<VEC>(two_rest ? rest / 2 : rest);
+    }
+};
+
+// 2^log lanes a head, one or two packs of VEC elements each; what a pack shares with
+// the one before it counts in the sums once, and both write the same.  A lane keeps
+// its place in a head and its weights over the tokens blockIdx.y, blockIdx.y +
+// gridDim.y, ...  What bounds it: the bytes of queries, keys and values, read and
+// written once.
+template <typename TX, typename TC, typename TP, int VEC>
+__global__ __launch_bounds__(256) void append_norm_packs(AppendNormArgs n, Divisor by_page, int log)
+{
+    const AppendArgs &a = n.a;
+    const Lanes<VEC> as(a.dim, a.rot_dim, a.pairs != 0);
+    const int lanes = 1 << log, heads = a.q_heads + 2 * a.kv_heads, half = a.rot_dim / 2;
+    const int id = (int)(blockIdx.x * 256 + threadIdx.x), i = id >> log, u = id & (lanes - 1);
+    if (i >= heads) return;  // (whole heads: a wave's lanes of a head stay together)
+    const bool query = i < a.q_heads, value = i >= a.q_heads + a.kv_heads, on = u < as.all;
+    const int h = query ? i : value ? i - a.q_heads - a.kv_heads : i - a.q_heads;
+    const bool rotated = u < as.turned, two = rotated ? as.two_turned : as.two_rest;
+    // Elements e.. and, of two packs, others from e2; the first `over` of them belong to the pack before.
+    const int in = rotated ? u : u - as.turned, width = rotated ? as.turns : as.two_rest ? as.rest / 2 : as.rest;
+    const int from = !on ? 0 : pack_at<VEC>(in, width), over = !on ? VEC : in * VEC - from;
+    const int e = on && !rotated ? a.rot_dim + from : from, e2 = on && two ? e + width : e;
+    const TX *src = query ? (const TX *)a.q + h * a.q_head : value ? (const TX *)a.v + h * a.v_head : (const TX *)a.k + h * a.k_head;
+    const int64_t row = query ? a.q_row : value ? a.v_row : a.k_row;
+    TC *cache = value ? (TC *)a.vc + h * a.vc_head : (TC *)a.kc + h * a.kc_head;
+    const int64_t page_row = value ? a.vc_page : a.kc_page, slot_row = value ? a.vc_slot : a.kc_slot;
+    const bool norms = n.norm != ILPM_NORM_NONE, turns = rotated && !value && on, layer = n.norm == ILPM_NORM_LAYER;
+    float w[VEC], w2[VEC];
+    load_weights<TP, VEC>(norms && !value ? (query ? n.q_w : n.k_w) : nullptr, e, w);
+    load_weights<TP, VEC>(norms && !value ? (query ? n.q_w : n.k_w) : nullptr, e2, w2);
+    const float inv = 1.f / (float)a.dim;
+
+    // A token's values and where it is, read while the one before it is written.
+    struct Token {
+        Pack<TX, VEC> p, p2;
+        int pos, seq, slot;
+    };
+    auto read = [&](int t) {
+        Token k;
+        t = min(t, a.n_tokens - 1);
+        k.p = load_loose<TX, VEC>(src + t * row + e);
+        k.p2 = load_loose<TX, VEC>(src + t * row + e2);
+        k.pos = a.positions[t];
+        k.seq = a.seq_ids[t];
+        k.slot = n.slots[t];
+        return k;
+    };
+    Token next = read((int)blockIdx.y);
+#pragma unroll 1
+    for (int t = (int)blockIdx.y; t < a.n_tokens; t += (int)gridDim.y) {
+        const Token k = next;
+        const bool known = a.rot_dim > 0 && k.pos >= 0 && k.pos < a.n_positions, turn = turns && known;
+        Place at = {-1, 0};
+        if (!query) {
+            at = place_of(a, k.seq, k.slot, by_page);
+            if (a.rot_dim > 0 && !known) at.page = -1;
+        }
+        // VEC angles for halves, VEC / 2 for a pack of pairs.
+        constexpr int HV = VEC / 2;
+        Pack<float, HV> c[2], s[2];
+        if (turn) {
+            const float *cs = a.cos + (int64_t)k.pos * half, *sn = a.sin + (int64_t)k.pos * half;
+            const int first = a.pairs ? e / 2 : e, second = a.pairs ? e2 / 2 : e + HV;
+            c[0] = load_loose<float, HV>(cs + first), s[0] = load_loose<float, HV>(sn + first);
+            c[1] = load_loose<float, HV>(cs + second), s[1] = load_loose<float, HV>(sn + second);
+        }
+        next = read((int)min((int64_t)t + gridDim.y, (int64_t)a.n_tokens));  // (behind what this token waits for)
+        float x[VEC], y[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = (float)k.p.v[j], y[j] = (float)k.p2.v[j];
+        if (norms) {
+            float mean = 0.f;
+            auto sum = [&](auto f) {
+                float v = 0.f, v2 = 0.f;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    v += j >= over ? f(x[j]) : 0.f;
+                    v2 += j >= over ? f(y[j]) : 0.f;
+                }
+                return sum_lanes(two ? v + v2 : v, log);
+            };
+            if (layer) mean = sum([](float v) { return v; }) * inv;
+            const float rstd = rsqrt_of(sum([&](float v) { return (v - mean) * (v - mean); }) * inv + n.eps);
+            if (!value) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    x[j] = (layer ? (x[j] - mean) * rstd : x[j] * rstd) * w[j];
+                    y[j] = (layer ? (y[j] - mean) * rstd : y[j] * rstd) * w2[j];
+                }
+            }
+        }
+        if (!on || (!query && at.page < 0)) continue;
+        if (turn && !a.pairs) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float v = x[j], cj = c[j / HV].v[j % HV], sj = s[j / HV].v[j % HV];
+                x[j] = v * cj - y[j] * sj;
+                y[j] = y[j] * cj + v * sj;
+            }
+        } else if (turn) {
+#pragma unroll
+            for (int j = 0; j < VEC; j += 2) {
+                const float v = x[j], w = y[j];
+                x[j] = v * c[0].v[j / 2] - x[j + 1] * s[0].v[j / 2];
+                x[j + 1] = x[j + 1] * c[0].v[j / 2] + v * s[0].v[j / 2];
+                y[j] = w * c[1].v[j / 2] - y[j + 1] * s[1].v[j / 2];
+                y[j + 1] = y[j + 1] * c[1].v[j / 2] + w * s[1].v[j / 2];
+            }
+        }
+        auto put = [&](auto *dst) {
+            using TD = std::remove_reference_t<decltype(*dst)>;
+            Pack<TD, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o.v[j] = (TD)x[j];
+            store_loose<TD, VEC>(dst + e, o);
+            if (!two) return;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o.v[j] = (TD)y[j];
+            store_loose<TD, VEC>(dst + e2, o);
+        };
+        if (query) put((TX *)a.q_out + (int64_t)t * a.qo_row + h * a.qo_head);
+        else put(cache + (int64_t)at.page * page_row + (int64_t)at.slot * slot_row);
+    }
+}
+
+// Whether heads fall into packs of VEC: what turns and what does not have one pack
+// at least, and together not more than a wave has lanes.
+template <int VEC> bool packs_fit(const AppendArgs &a, int *log)
+{
+    const Lanes<VEC> as(a.dim, a.rot_dim, a.pairs != 0);
+    if ((as.turns > 0 && as.turns < VEC) || (as.rest > 0 && as.rest < VEC)) return false;
+    for (*log = 0; 1 << *log < as.all;) ++*log;
+    return *log <= 6;
+}
+
+template <typename TX, typename TC, typename TP, int VEC>
+bool launch_packs(const AppendNormArgs &n, const Divisor &by_page, int heads, hipStream_t stream)
+{
+    int log;
+    if (!packs_fit<VEC>(n.a, &log)) return false;
+    const int groups = (int)((((int64_t)heads << log) + 255) / 256);
+    // As many workgroups as the card holds at once.
+    const int slices = std::min(n.a.n_tokens, std::max(1, kCardGroups / groups));
+    hipLaunchKernelGGL((append_norm_packs<TX, TC, TP, VEC>), dim3(groups, slices), dim3(256), 0, stream, n, by_page, log);
+    return true;
+}
+
 template <typename TX, typename TC, typename TP> hipError_t launch(const AppendNormArgs &n, hipStream_t stream)
 {
     const AppendArgs &a = n.a;
     const int heads = a.q_heads + 2 * a.kv_heads, total = heads * a.n_tokens;
-    hipLaunchKernelGGL((append_norm_any<TX, TC, TP>), dim3(ceil_div(total, 4)), dim3(256), 0, stream, n, Divisor((unsigned)heads),
-                       Divisor((unsigned)a.page_size), total);
+    const Divisor by_page((unsigned)a.page_size);
+    if (!launch_packs<TX, TC, TP, 8>(n, by_page, heads, stream) && !launch_packs<TX, TC, TP, 4>(n, by_page, heads, stream) &&
+        !launch_packs<TX, TC, TP, 2>(n, by_page, heads, stream))
+        hipLaunchKernelGGL((append_norm_any<TX, TC, TP>), dim3(ceil_div(total, 4)), dim3(256), 0, stream, n, Divisor((unsigned)heads), by_page, total);
     return hipGetLastError();
 }
 
