@@ -651,3 +651,182 @@ def test_copy_nothing():
     ilpm.kv_copy(t["kp"], t["vp"], t["src"][:0], t["dst"][:0], z[:0], z[:0], z[:0])
     ilpm.kv_copy(t["kp"][:0], t["vp"][:0], t["src"], t["dst"], z, z, z + 1)
     assert torch.equal(t["kp"], before)
+
+
+# ---- streams, graphs and workspaces ----
+
+def step_case(seed):
+    """A batch's cache and one drafted step's inputs, and the calls of the step on them."""
+    g = gen(seed)
+    n, t, hq, hk, d, vocab = 4, 9, 8, 2, 64, 6000
+    c = attn_case(g, [700, 20, 0, 333], [[-1] + [int(torch.randint(0, i, (), generator=g)) for i in range(1, t)] for _ in range(n)], hq, hk, d, BF16, BF16, 16)
+    v = verify_case(g, n, t, vocab, F32, False, std=4.0)
+    v["parents"] = c["parents"]
+    angle = torch.rand((800, d // 2), generator=g) * 6.3
+    depth = ints([[len(a) - 1 for a in ref.above(row)] for row in c["parents"].tolist()])
+    s = {k: x.cuda() for k, x in dict(c, k=randn(g, (n * t, hk, d), BF16), v=randn(g, (n * t, hk, d), BF16), cos=angle.cos(), sin=angle.sin(),
+                                      seq=ints([[i] * t for i in range(n)]).view(-1), pos=(c["lengths"][:, None] + depth).view(-1),
+                                      slots=(c["lengths"][:, None] + torch.arange(t)).view(-1).to(torch.int32), tokens=v["tokens"],
+                                      target=v["target"], uniforms=v["uniforms"]).items()}
+    return s
+
+
+def step(s, stream=None):
+    ilpm = lib()
+    q = ilpm.kv_append_norm(s["k"], s["v"], s["kp"], s["vp"], s["table"], s["seq"], s["pos"], slots=s["slots"], q=s["q"], cos=s["cos"],
+                            sin=s["sin"], stream=stream)
+    a, lse = ilpm.attn_tree(q, s["kp"], s["vp"], s["table"], s["lengths"], s["parents"], return_lse=True, stream=stream)
+    path, counts, last = ilpm.verify_drafts(s["tokens"], s["parents"], s["target"], s["uniforms"], stream=stream)
+    ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], s["lengths"], s["lengths"], counts, path=path, stream=stream)
+    return [q, a, lse, path, counts, last, s["kp"], s["vp"]]
+
+
+def same(a, b):
+    return all(torch.equal(torch.nan_to_num(x.float(), 7.0), torch.nan_to_num(y.float(), 7.0)) for x, y in zip(a, b))
+
+
+def fresh(s):
+    return {k: v.clone() for k, v in s.items()}
+
+
+def test_a_step_is_the_same_every_time_and_on_other_streams():
+    s = step_case(31)
+    note("[step] twice")
+    want = step(fresh(s))
+    again = step(fresh(s))
+    torch.cuda.synchronize()
+    assert same(want, again)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    cases = [fresh(s) for _ in streams]
+    torch.cuda.synchronize()
+    note("[step] three streams at once")
+    got = [step(c, stream=st) for c, st in zip(cases, streams)]
+    torch.cuda.synchronize()
+    for x in got:
+        assert same(want, x)
+    note("[step] current stream")
+    c = fresh(s)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[0]):
+        x = step(c)
+    torch.cuda.synchronize()
+    assert same(want, x)
+
+
+def test_two_steps_captured_and_replayed():
+    """Two graphs of different inputs, each with its own memory, replayed in turn with eager work between."""
+    a, b = step_case(32), step_case(33)
+    wants = [step(fresh(a)), step(fresh(b))]
+    torch.cuda.synchronize()
+    graphs, outs, cases = [], [], []
+    for s in (a, b):
+        c = fresh(s)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(c))
+        graphs.append(g)
+        cases.append(c)
+    for turn in range(4):
+        note(f"[step] replay {turn}")
+        for g, s, c, out, want in zip(graphs, (a, b), cases, outs, wants):
+            for k in ("kp", "vp"):
+                c[k].copy_(s[k])
+            g.replay()
+            torch.cuda.synchronize()
+            assert same(want, out), turn
+        assert same(wants[0], step(fresh(a)))   # eager work between
+        torch.cuda.synchronize()
+    # Other inputs in the same memory: what was found in the replays before must not matter.
+    c, out = cases[0], outs[0]
+    for k in c:
+        c[k].copy_(b[k])
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    assert same(wants[1], out)
+
+
+def test_workspaces_of_the_caller():
+    ilpm = lib()
+    s = step_case(34)
+    need = ilpm.attn_tree_workspace_size(s["kp"], s["vp"], s["table"], 8, 9)
+    assert need > 0
+    out = lambda **kw: ilpm.attn_tree(s["q"], s["kp"], s["vp"], s["table"], s["lengths"], s["parents"], **kw)  # noqa: E731
+    want = out()
+    ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
+    assert torch.equal(want, out(workspace=ws)) and torch.equal(want, out(workspace=ws))
+    with pytest.raises(ilpm.IlpmError, match="workspace too small"):
+        out(workspace=ws[:need - 1])
+    with pytest.raises(ValueError, match="contiguous"):
+        out(workspace=torch.empty((2, need), dtype=torch.uint8, device="cuda")[:, ::2])
+    v = verify_case(gen(35), 2, 4, 100000, F32, False)
+    need = ilpm.verify_drafts_workspace_size(2, 4, 100000)
+    with pytest.raises(ilpm.IlpmError, match="workspace too small"):
+        ilpm.verify_drafts(*(v[k].cuda() for k in ("tokens", "parents", "target", "uniforms")), workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+
+
+def test_refusals_of_the_binding():
+    ilpm = lib()
+    s = step_case(36)
+
+    def caller(f, names):
+        return lambda **kw: f(*[kw.get(k, s[k]) for k in names], **{k: v for k, v in kw.items() if k not in names})
+
+    append = caller(ilpm.kv_append_norm, ("k", "v", "kp", "vp", "table", "seq", "pos"))
+    attn = caller(ilpm.attn_tree, ("q", "kp", "vp", "table", "lengths", "parents"))
+    check = caller(ilpm.verify_drafts, ("tokens", "parents", "target", "uniforms"))
+    with pytest.raises(ValueError, match="norm must be"):
+        append(norm="l2")
+    with pytest.raises(ValueError, match="slots"):
+        append(slots=s["slots"][:3])
+    with pytest.raises(ValueError, match="without q"):
+        append(q_w=torch.ones(64, device="cuda"))
+    with pytest.raises(ValueError, match="k_w must be"):
+        append(k_w=torch.ones(65, device="cuda"))
+    with pytest.raises(TypeError, match="of one type"):
+        append(q=s["q"], q_w=torch.ones(64, device="cuda"), k_w=torch.ones(64, device="cuda", dtype=BF16))
+    with pytest.raises(ilpm.IlpmError):
+        append(norm=None, k_w=torch.ones(64, device="cuda"))
+    with pytest.raises(TypeError, match="int32"):
+        append(slots=s["slots"].long())
+    with pytest.raises(ValueError, match="parents must be"):
+        attn(parents=s["parents"][:2])
+    with pytest.raises(ValueError, match="parents must be"):
+        attn(parents=torch.zeros((4, 12), dtype=torch.int32, device="cuda")[:, :9])   # rows that are not together
+    with pytest.raises(ValueError, match="q must be"):
+        attn(q=s["q"][:-1])
+    with pytest.raises(ilpm.IlpmError, match="unsupported"):
+        attn(q=torch.zeros((4 * 65, 8, 64), dtype=BF16, device="cuda"), parents=torch.zeros((4, 65), dtype=torch.int32, device="cuda"))
+    with pytest.raises(ilpm.IlpmError):
+        attn(window=-1)
+    with pytest.raises(ilpm.IlpmError):
+        attn(sinks=-1)
+    with pytest.raises(TypeError, match="mask"):
+        attn(mask=torch.zeros((4, 9), device="cuda"))
+    with pytest.raises(TypeError, match="CUDA"):
+        attn(lengths=s["lengths"].cpu())
+    with pytest.raises(ValueError, match="target must be"):
+        check(target=s["target"][:, :5])
+    with pytest.raises(ValueError, match="draft must be"):
+        check(draft=s["target"].to(BF16))
+    with pytest.raises(ValueError, match="uniforms"):
+        check(uniforms=s["uniforms"][:, :3].contiguous())
+    with pytest.raises(TypeError, match="float32"):
+        check(uniforms=s["uniforms"].double())
+    with pytest.raises(TypeError, match="path must be"):
+        check(path=torch.zeros((4, 9), dtype=torch.int64, device="cuda"))
+    with pytest.raises(ilpm.IlpmError):
+        check(target=torch.zeros((4, 9, 0), device="cuda"))
+    z = torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="dst_table"):
+        ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"][:2], z, z, z)
+    with pytest.raises(ValueError, match="counts"):
+        ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], z, z, z[:2])
+    with pytest.raises(ValueError, match="path"):
+        ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], z, z, z, path=torch.zeros((3, 4), dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError, match="more than the path"):
+        ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], z, z, z, path=torch.zeros((4, 4), dtype=torch.int32, device="cuda"), max_count=5)
+    with pytest.raises(ilpm.IlpmError, match="unsupported"):
+        ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], z, z, z, path=torch.zeros((4, 65), dtype=torch.int32, device="cuda"))
+    with pytest.raises(ilpm.IlpmError):
+        ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], z, z, z, max_count=-1)
