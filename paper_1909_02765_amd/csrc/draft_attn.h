@@ -302,12 +302,18 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         }
         return e;
     };
+    // Where a group's keys lie, in LDS (those that are not seen at the pool's first row: it is read, and none of it
+    // used), and which are seen: bit 16t + n is key n of its tile t.
+    unsigned long long seen_of[2] = {0, 0};
     auto place = [&](int group, Entry e) {
         const AttnArgs &a = args_of(args).a;
         const bool ok = e.page >= 0 && e.page < a.n_pages;
         Places &p = lds.places[wave][group & 1];
-        p.k[lane] = ok ? (int64_t)e.page * a.k_page + (int64_t)e.slot * a.k_slot : -1;
-        p.v[lane] = ok ? (int64_t)e.page * a.v_page + (int64_t)e.slot * a.v_slot : -1;
+        p.k[lane] = ok ? (int64_t)e.page * a.k_page + (int64_t)e.slot * a.k_slot : 0;
+        p.v[lane] = ok ? (int64_t)e.page * a.v_page + (int64_t)e.slot * a.v_slot : 0;
+        const unsigned long long seen = __builtin_amdgcn_ballot_w64(ok);
+        if (group & 1) seen_of[1] = seen;
+        else seen_of[0] = seen;
         // (Only this wave reads them, and a wave's LDS accesses keep their order.)
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -321,20 +327,18 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     const float softcap = a.softcap;
     Words16 kt[NK];
     Words<sizeof(TC) * VV> vt[4][NV];
-    bool seen[4];
-    // A key that is not seen reads the pool's first row, and none of it is used.
+    // (Behind the last tile that one again.)
     auto load_k = [&](int j) {
-        const int64_t at = lds.places[wave][(j >> 2) & 1].k[(j & 3) * 16 + n16];
-        const TC *row = kh + (j < tiles ? max(at, (int64_t)0) : 0);
+        j = min(j, tiles - 1);
+        const TC *row = kh + lds.places[wave][(j >> 2) & 1].k[(j & 3) * 16 + n16];
 #pragma unroll
         for (int c = 0; c < NK; ++c) kt[c] = load_piece<TC, KV, R, true>(row, (g + 4 * c) * KV, dim);
     };
     auto load_v = [&](int j) {
+        j = min(j, tiles - 1);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int64_t at = lds.places[wave][(j >> 2) & 1].v[(j & 3) * 16 + 4 * g + r];
-            seen[r] = at >= 0;
-            const TC *row = vh + (j < tiles ? max(at, (int64_t)0) : 0);
+            const TC *row = vh + lds.places[wave][(j >> 2) & 1].v[(j & 3) * 16 + 4 * g + r];
 #pragma unroll
             for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
                 vt[r][c] = load_piece<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R, false>(row, (n16 + 16 * c) * VV, dim);
@@ -367,11 +371,12 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     const float scale2 = softcap > 0.f ? a.scale / softcap : a.scale * kLog2e;
     const float cap2 = softcap * kLog2e;
     const int top_low = uniform(lds.top_low);
+    constexpr bool UNSCALE = QP == 3 && __is_same(TC, _Float16);  // (parts of bf16 need none)
 
-    // Selectors that put rows' 16-bit values together; 0 for those of keys that are not seen.
-    auto values = [&](int c, int i, const unsigned *lower, const unsigned *upper) {
-        return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], i & 1 ? upper[0] : lower[0]),
-                        __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], i & 1 ? upper[1] : lower[1])};
+    // Value i of piece c of a lane's four rows, put together from their 16-bit halves.
+    auto values = [&](int c, int i) {
+        const unsigned halves = i & 1 ? 0x07060302u : 0x05040100u;
+        return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], halves), __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], halves)};
     };
     // Whether row r sees key key0 + 4g + i, i < 4, where it is in the cache.
     auto sees = [&](int r, int64_t key0, bool *see) {
@@ -408,7 +413,7 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
                     }
                 }
             }
-            if (!seen[r] || odd == 0) continue;
+            if (odd == 0) continue;
             lds.any_odd = 1;
 #pragma unroll 1
             for (int row = 0; row < 16 * MA; ++row) {
@@ -429,7 +434,7 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         const int64_t key0 = start_of(tile);
         const bool special = key0 + 15 >= range.length || (tile >= sink_tiles && key0 < top_low);
 
-        // The scores of all rows, then the next tile's keys are on their way.
+        // The scores of the blocks of rows, then the next tile's keys are on their way.
         floatx4 s[MA];
         int ql = lane;
         asm volatile("" : "+v"(ql));  // (read for each tile, not kept)
@@ -462,40 +467,52 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         }
         load_k(j + 1);
 
-        if (special) take_out(key0);
+        // Scores times `by` are logarithms to the base 2; with a cap, or a scale that is not above 0, they are first made so.
+        float by[MA];
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) by[ma] = UNSCALE ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
+        if (softcap > 0.f || !(scale2 > 0.f)) {
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[ma][r] *= by[ma];
+                    if (softcap > 0.f) s[ma][r] = cap2 * tanh_of(s[ma][r]);
+                }
+                by[ma] = 1.f;
+            }
+        }
+        // Most tiles are seen whole by all rows.
+        const unsigned tile_seen = (unsigned)((j & 4 ? seen_of[1] : seen_of[0]) >> ((j & 3) * 16)) & 0xffffu;
+        if (special || tile_seen != 0xffffu) {
+            bool seen[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) seen[r] = ((tile_seen >> (4 * g + r)) & 1) != 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < NV; ++c) {
+                    using V = std::remove_reference_t<decltype(vt[r][c])>;
+                    vt[r][c] = seen[r] ? vt[r][c] : V{};
+                }
+            if (special) take_out(key0);
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma) {
+                if (special) {
+                    bool see[4];
+                    sees(ma * 16 + n16, key0, see);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[ma][r] = see[r] ? s[ma][r] : -INFINITY;
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[ma][r] = seen[r] ? s[ma][r] : -INFINITY;
+            }
+        }
         constexpr int PW = !C16 ? 4 : PP == 3 ? 6 : 4;
         unsigned part[MA][PW];  // probabilities: hi and lo of four keys, a third part; or 32 bits
-        if (softcap > 0.f) {
-#pragma unroll
-            for (int ma = 0; ma < MA; ++ma) {
-                const float by = QP == 3 ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[ma][r] = cap2 * tanh_of(s[ma][r] * by);
-            }
-        } else {
-#pragma unroll
-            for (int ma = 0; ma < MA; ++ma) {
-                const float by = QP == 3 ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[ma][r] *= by;
-            }
-        }
-        if (special) {
-#pragma unroll
-            for (int ma = 0; ma < MA; ++ma) {
-                bool see[4];
-                sees(ma * 16 + n16, key0, see);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[ma][r] = see[r] ? s[ma][r] : -INFINITY;
-            }
-        }
 #pragma unroll
         for (int ma = 0; ma < MA; ++ma) {
-            float x[4], top = -INFINITY;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = seen[r] ? s[ma][r] : -INFINITY;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, x[r]);
+            const float top = fmaxf(fmaxf(s[ma][0], s[ma][1]), fmaxf(s[ma][2], s[ma][3])) * by[ma];
             // (m may lie up to SLACK below the maximum: most tiles after the first leave it where it is.)
             if (__builtin_amdgcn_ballot_w64(top > m[ma] + Cfg::SLACK)) {
                 const float m_new = fmaxf(m[ma], max_of_head(top));
@@ -506,8 +523,9 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
                 for (int i = 0; i < NO; ++i) o[ma][i] *= alpha;
             }
             const float base = m[ma] == -INFINITY ? 0.f : m[ma];
+            float x[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(x[r] - base);
+            for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ma][r], by[ma], -base));
             l[ma] += (x[0] + x[1]) + (x[2] + x[3]);
             if constexpr (!C16) {
 #pragma unroll
@@ -533,6 +551,14 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
             }
         }
 
+        // The same four keys twice, against the first and second parts of their probabilities.
+        auto weigh = [&](int ma, int i, Words16 vv) {
+            floatx4 &sum = o[ma][i];
+            sum = mfma_values32<TC>(vv, Words16{part[ma][0], part[ma][1], part[ma][2], part[ma][3]}, sum);
+            // (By the same instruction: one of 16x16x16 right after it, on the same registers, found them as they were
+            // before it.)
+            if constexpr (PP == 3) sum = mfma_values32<TC>(vv, Words16{part[ma][4], part[ma][5], 0u, 0u}, sum);
+        };
         if constexpr (!C16) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
@@ -540,35 +566,20 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
                 for (int c = 0; c < NV; ++c)
 #pragma unroll
                     for (int i = 0; i < VV; ++i) {
-                        const float v = seen[r] ? __builtin_bit_cast(floatx4, vt[r][c])[i] : 0.f;
+                        const float v = __builtin_bit_cast(floatx4, vt[r][c])[i];
 #pragma unroll
-                        for (int ma = 0; ma < MA; ++ma)
-                            o[ma][c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __builtin_bit_cast(float, part[ma][r]), o[ma][c * VV + i], 0, 0, 0);
+                        for (int ma = 0; ma < MA; ++ma) {
+                                            o[ma][c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __builtin_bit_cast(float, part[ma][r]), o[ma][c * VV + i], 0, 0, 0);
+                        }
                     }
         } else {
-            // Selectors of the lower and the upper halves of two rows' registers: a byte 0x0c gives 0.
-            unsigned lower[2], upper[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const unsigned keep = (seen[2 * h] ? 0xffffu : 0u) | (seen[2 * h + 1] ? 0xffff0000u : 0u);
-                lower[h] = (0x05040100u & keep) | (0x0c0c0c0cu & ~keep);
-                upper[h] = (0x07060302u & keep) | (0x0c0c0c0cu & ~keep);
-            }
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
                 for (int i = 0; i < VV; ++i) {
-                    const Words<8> v = values(c, i, lower, upper);
-                    // The same four keys twice, against the first and second parts of their probabilities.
-                    const Words16 vv = {v[0], v[1], v[0], v[1]};
+                    const Words<8> v = values(c, i);
 #pragma unroll
-                    for (int ma = 0; ma < MA; ++ma) {
-                        floatx4 &sum = o[ma][c * VV + i];
-                        sum = mfma_values32<TC>(vv, Words16{part[ma][0], part[ma][1], part[ma][2], part[ma][3]}, sum);
-                        // (By the same instruction: one of 16x16x16 right after it, on the same registers, found them as
-                        // they were before it.)
-                        if constexpr (PP == 3) sum = mfma_values32<TC>(vv, Words16{part[ma][4], part[ma][5], 0u, 0u}, sum);
-                    }
+                    for (int ma = 0; ma < MA; ++ma) weigh(ma, c * VV + i, Words16{v[0], v[1], v[0], v[1]});
                 }
         }
         load_v(j + 1);
