@@ -65,7 +65,7 @@ struct TreeArgs {
     bool pieces;     // heads are whole pieces of 16 bytes
 };
 // What a unit costs beside its tiles, in tiles, by its row blocks.
-__host__ __device__ inline int tree_unit_cost(int row_blocks) { return 4 + 5 * row_blocks; }
+__host__ __device__ inline int tree_unit_cost(int row_blocks) { return 12 + 4 * row_blocks; }
 size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len);
 void tree_workspace(TreeArgs *t, void *ws);
 hipError_t tree_launch(const TreeArgs &t, int cache_dtype, hipStream_t stream);

@@ -150,7 +150,7 @@ template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeRows {
         const TreeArgs &t = args_of(args);
         const AttnArgs &a = t.a;
         const int n16 = lane & 15, g = lane >> 4, ma = wave % MA, c0 = wave / MA;
-        parent = wave == 0 && lane < t.n_nodes ? t.parents[(int64_t)seg.seq * t.n_nodes + lane] : -2;
+        parent = lane < t.n_nodes ? t.parents[(int64_t)seg.seq * t.n_nodes + lane] : -2;
         const int in_unit = min(row_in_unit(seg, 16 * MA, ma * 16 + n16), t.rows - 1), node = t.by_group.of(in_unit);
         row = (const TQ *)a.q + ((int64_t)seg.seq * t.n_nodes + node) * a.q_row +
               ((int64_t)seg.kvh * a.group + (in_unit - node * a.group)) * a.q_head;
@@ -282,7 +282,7 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     const TreeRange range = seg.range;
     const int sink_tiles = (range.sinks + 15) / 16;
     // Tile j of this wave is tile 4j + wave of the segment.
-    const int tiles = max(0, (seg.tile1 - seg.tile0 - wave + 3) / 4);
+    int tiles = max(0, (seg.tile1 - seg.tile0 - wave + 3) / 4);
     auto start_of = [&](int tile) { return tile < sink_tiles ? tile * 16 : range.first + (tile - sink_tiles) * 16; };
 
     // Lane (n, g) looks up key n of tile 4*group + g.
@@ -351,6 +351,9 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     // The first tile, the rows' nodes and queries: none waits for another.
     TreeRows<TC, Q16, DC, R, MA> rows;
     rows.load(args, seg, lane, wave);
+    // (Behind the last node of a smaller tree there is nothing to do.)
+    const unsigned long long nodes = __builtin_amdgcn_ballot_w64(rows.parent >= -1 && rows.parent < lane);
+    if (row_in_unit(seg, 16 * MA, 0) >= (64 - (nodes ? __builtin_clzll(nodes) : 64)) * a.group) tiles = 0;
     if (tiles > 0) {
         place(0, e0);
         load_k(0);
