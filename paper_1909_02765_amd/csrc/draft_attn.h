@@ -381,16 +381,14 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         const unsigned halves = i & 1 ? 0x07060302u : 0x05040100u;
         return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], halves), __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], halves)};
     };
-    // Whether row r sees key key0 + 4g + i, i < 4, where it is in the cache.
-    auto sees = [&](int r, int64_t key0, bool *see) {
+    // Which of the keys key0..key0 + 15 row r sees, where they are in the cache.
+    auto sees = [&](int r, int64_t key0) {
+        auto upto = [](int64_t n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << (int)n) - 1u; };  // the first n keys
         const unsigned long long bits = lds.bits[r];
-        const int64_t low = lds.low[r], node0 = key0 - range.length;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int node = (int)node0 + 4 * g + i;  // (of keys before the nodes the low half does not matter)
-            const int64_t key = key0 + 4 * g + i;
-            see[i] = node0 + 4 * g + i >= 0 ? ((bits >> (node & 63)) & 1) != 0 : key >= low || key < all_sinks;
-        }
+        const int64_t node0 = key0 - range.length;
+        const unsigned nodes = (unsigned)(node0 >= 0 ? node0 < 64 ? bits >> (int)node0 : 0 : node0 > -16 ? bits << (int)-node0 : 0);
+        const unsigned before = upto(-node0);  // the sequence's own
+        return (nodes & ~before & 0xffffu) | (before & (~upto(lds.low[r] - key0) | upto(all_sinks - key0)));
     };
     // Takes values that are not finite out of a tile whose rows do not see the same keys, and marks the rows that see
     // them: bit c * VV + i of odd[row][n] stands for value (n + 16c) * VV + i.  (Hardly ever.)
@@ -419,11 +417,8 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
             if (odd == 0) continue;
             lds.any_odd = 1;
 #pragma unroll 1
-            for (int row = 0; row < 16 * MA; ++row) {
-                bool see[4];
-                sees(row, key0, see);
-                if (see[r]) atomicOr(&lds.odd[row][n16], odd);
-            }
+            for (int row = 0; row < 16 * MA; ++row)
+                if ((sees(row, key0) >> (4 * g + r)) & 1) atomicOr(&lds.odd[row][n16], odd);
         }
     };
 
@@ -501,14 +496,9 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
             if (special) take_out(key0);
 #pragma unroll
             for (int ma = 0; ma < MA; ++ma) {
-                if (special) {
-                    bool see[4];
-                    sees(ma * 16 + n16, key0, see);
+                const unsigned see = (special ? sees(ma * 16 + n16, key0) & tile_seen : tile_seen) >> (4 * g);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[ma][r] = see[r] ? s[ma][r] : -INFINITY;
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[ma][r] = seen[r] ? s[ma][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r) s[ma][r] = (see >> r) & 1 ? s[ma][r] : -INFINITY;
             }
         }
         constexpr int PW = !C16 ? 4 : PP == 3 ? 6 : 4;
