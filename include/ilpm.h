@@ -658,10 +658,10 @@ typedef struct ilpm_tree_options {
  * lse = -infinity.  A chain of n tokens (parents -1, 0, 1, ...) is a prompt's
  * next part; a single node is ilpm_attn_decode's new token.
  * Over 16-bit caches the exponentials that weigh the values are rounded (those in
- * lse are not): under 16-bit queries to 2^-17 of themselves over bf16 and 2^-23 over
- * f16, or there by up to 2^-40 where that is more; under fp32 queries over bf16 to 2^-24, over f16 as
- * under 16-bit ones.  An infinite v_j that is seen gives infinity or NaN.  Of fp32
- * queries over f16 what is below 2^-39 of a row's largest value is lost.
+ * lse are not): over bf16 to 2^-17 of themselves under bf16 queries and to 2^-24 under
+ * fp32 ones, over f16 to 2^-23, or by up to 2^-35 of the largest where that is more.
+ * An infinite v_j that is seen gives infinity or NaN.  Of fp32 queries over f16 what
+ * is below 2^-39 of a row's largest value is lost.
  * head_dim is at most 256 (ILPM_ERR_UNSUPPORTED above).
  * The workspace is as ilpm_attn_decode's, of ilpm_attn_tree_workspace_size bytes.
  */

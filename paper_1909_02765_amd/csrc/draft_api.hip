@@ -46,7 +46,7 @@ int kv_append_norm(const ilpm_kv_cache *cache, const ilpm_heads *k, const ilpm_h
     if (!o.seq_ids || !o.positions || ((uintptr_t)o.seq_ids | (uintptr_t)o.positions | (uintptr_t)slots) % 4) return ILPM_ERR_INVALID_ARG;
     if (o.rot_dim > 0 && o.n_positions > 0 && (!o.cos || !o.sin || ((uintptr_t)o.cos | (uintptr_t)o.sin) % 4)) return ILPM_ERR_INVALID_ARG;
     const int64_t heads = (int64_t)(q ? q->heads : 0) + 2 * (int64_t)c.kv_heads;
-    if (n_tokens > kMaxGroups || heads * n_tokens > kMaxGroups * 4) return ILPM_ERR_UNSUPPORTED;
+    if (n_tokens > kMaxGroups || heads > kMaxGroups || heads * n_tokens > kMaxGroups * 4) return ILPM_ERR_UNSUPPORTED;
 
     // What is written: the pools and q_out.
     const int64_t angles = o.rot_dim > 0 ? (int64_t)o.n_positions * (o.rot_dim / 2) * 4 : 0;

@@ -39,7 +39,7 @@ __device__ inline int64_t part_at(const TreeArgs &t, const AttnPart &u, int row,
     return ((((int64_t)u.first + i) * t.a.blocks + block) * 2 + (i == 0)) * t.a.part_heads + in_block;
 }
 
-// Joins the parts of the unit at place blockIdx.x, for its row blockIdx.y and 64
+// Joins the parts of the unit at place blockIdx.y, for its row blockIdx.x and 64
 // values of it, blockIdx.z, as attn_decode's parts are (attn_join).
 template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
 {
@@ -47,9 +47,9 @@ template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
     __shared__ float red[2][4], w[kMaxParts];
     __shared__ Pack<float, V> sum[G][T];
     const AttnArgs &a = t.a;
-    const AttnPart u = a.parts[blockIdx.x];
+    const AttnPart u = a.parts[blockIdx.y];
     if (u.count == 0) return;
-    const int row = blockIdx.y, node = t.by_group.of(row), head = u.unit * a.group + (row - node * a.group), tid = threadIdx.x;
+    const int row = blockIdx.x, node = t.by_group.of(row), head = u.unit * a.group + (row - node * a.group), tid = threadIdx.x;
     const int64_t out_row = (int64_t)u.seq * t.n_nodes + node;
     auto slot = [&](int i) { return part_at(t, u, row, i); };
     const int group = tid / T, d = (int)blockIdx.z * 64 + tid % T * V;
@@ -113,10 +113,10 @@ template <int V> __global__ __launch_bounds__(256) void tree_join(TreeArgs t)
 __global__ __launch_bounds__(256) void tree_join_rows(TreeArgs t, int lanes, Divisor by_lanes)
 {
     const AttnArgs &a = t.a;
-    const AttnPart u = a.parts[blockIdx.x];
+    const AttnPart u = a.parts[blockIdx.y];
     if (u.count == 0) return;
     const int r = by_lanes.of((int)threadIdx.x), lane = (int)threadIdx.x - r * lanes, per = by_lanes.of(256);
-    const int row = (int)blockIdx.y * per + r, d = lane * 4;
+    const int row = (int)blockIdx.x * per + r, d = lane * 4;
     if (r >= per || row >= t.rows) return;
     const int node = t.by_group.of(row), head = u.unit * a.group + (row - node * a.group);
     const int64_t out_row = (int64_t)u.seq * t.n_nodes + node;
@@ -192,10 +192,10 @@ hipError_t tree_launch(const TreeArgs &t, int cache_dtype, hipStream_t stream)
     const int joins = a.part_of_unit ? a.n_seqs * a.kv_heads : a.grid / a.blocks;
     if (a.dim % 4 == 0 && (int64_t)joins * t.rows * ceil_div(a.dim, 64) > 8 * kAttnCus) {
         const int lanes = a.dim / 4;
-        hipLaunchKernelGGL(tree_join_rows, dim3(joins, ceil_div(t.rows, 256 / lanes)), dim3(256), 0, stream, t, lanes, Divisor((unsigned)lanes));
+        hipLaunchKernelGGL(tree_join_rows, dim3(ceil_div(t.rows, 256 / lanes), joins), dim3(256), 0, stream, t, lanes, Divisor((unsigned)lanes));
         return hipGetLastError();
     }
-    const dim3 grid(joins, t.rows, ceil_div(a.dim, 64));
+    const dim3 grid(t.rows, joins, ceil_div(a.dim, 64));
     if (a.dim % 4) hipLaunchKernelGGL((tree_join<1>), grid, dim3(256), 0, stream, t);
     else hipLaunchKernelGGL((tree_join<4>), grid, dim3(256), 0, stream, t);
     return hipGetLastError();

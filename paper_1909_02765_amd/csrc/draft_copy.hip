@@ -4,6 +4,8 @@
 // pieces of up to 16 bytes, each read once and written once; what bounds it is
 // the memory, or for the few tokens of a tree the chain of accesses before the
 // first piece (counts, path, tables).
+#include <algorithm>
+
 #include "draft.h"
 
 namespace ilpm {
@@ -25,11 +27,11 @@ struct Move {
     int64_t from, to;
 };
 
-__device__ inline Move move_of(const CopyArgs &a, int seq, int i)
+__device__ inline Move move_of(const CopyArgs &a, int seq, int64_t i)
 {
     Move m = {-1, -1};
     if (i >= min(a.counts[seq], a.max_count)) return m;
-    const int step = a.path ? a.path[(int64_t)seq * a.path_stride + i] : i;
+    const int64_t step = a.path ? a.path[(int64_t)seq * a.path_stride + i] : i;
     if (step < 0) return m;
     m.from = slot_of(a, a.src_table, a.src_table_stride, a.src_max_pages, seq, (int64_t)a.src_start[seq] + step);
     m.to = slot_of(a, a.dst_table, a.dst_table_stride, a.dst_max_pages, seq, (int64_t)a.dst_start[seq] + i);
@@ -86,38 +88,44 @@ template <int P, int N> __global__ __launch_bounds__(256) void copy_path(CopyArg
     }
 }
 
-constexpr int kTokens = 16;  // of a workgroup
+constexpr int kTokens = 16;  // of a workgroup at a time
 
+// Without one: a thread takes one piece of kTokens tokens, and reads them all before
+// it writes the first, so that as many accesses are on their way.
 template <int P> __global__ __launch_bounds__(256) void copy_rows(CopyArgs a)
 {
     __shared__ Place places[kTokens];
-    const int seq = blockIdx.y, tid = threadIdx.x, first = (int)blockIdx.x * kTokens;
-    if (first >= a.counts[seq]) return;
-    if (tid < kTokens) places[tid] = place_of(a, move_of(a, seq, first + tid));
-    __syncthreads();
-    const int per_head = a.row_bytes / P, per = a.kv_heads * per_head;
-    for (int i0 = tid; i0 < 2 * per; i0 += 256) {
-        const bool value = i0 >= per;
-        const int i = value ? i0 - per : i0, h = i / per_head, e = (i - h * per_head) * P;
-        char *pool = value ? (char *)a.v + (int64_t)h * a.v_head + e : (char *)a.k + (int64_t)h * a.k_head + e;
-        Piece<P> got[kTokens];
+    const int seq = blockIdx.y, tid = threadIdx.x, per_head = a.row_bytes / P, per = a.kv_heads * per_head;
+    const int count = min(a.counts[seq], a.max_count);
+    for (int64_t first = (int64_t)blockIdx.x * kTokens; first < count; first += (int64_t)gridDim.x * kTokens) {
+        if (tid < kTokens) places[tid] = place_of(a, move_of(a, seq, first + tid));
+        __syncthreads();
+        for (int i0 = tid; i0 < 2 * per; i0 += 256) {
+            const bool value = i0 >= per;
+            const int i = value ? i0 - per : i0, h = i / per_head, e = (i - h * per_head) * P;
+            char *pool = value ? (char *)a.v + (int64_t)h * a.v_head + e : (char *)a.k + (int64_t)h * a.k_head + e;
+            Piece<P> got[kTokens];
 #pragma unroll
-        for (int n = 0; n < kTokens; ++n) {
-            const int64_t from = value ? places[n].v_from : places[n].k_from;
-            if (from >= 0) got[n] = load_loose<unsigned short, P / 2>((const unsigned short *)(pool + from));
-        }
+            for (int n = 0; n < kTokens; ++n) {
+                const int64_t from = value ? places[n].v_from : places[n].k_from;
+                if (from >= 0) got[n] = load_loose<unsigned short, P / 2>((const unsigned short *)(pool + from));
+            }
 #pragma unroll
-        for (int n = 0; n < kTokens; ++n) {
-            const int64_t to = value ? places[n].v_to : places[n].k_to;
-            if (to >= 0) store_loose<unsigned short, P / 2>((unsigned short *)(pool + to), got[n]);
+            for (int n = 0; n < kTokens; ++n) {
+                const int64_t to = value ? places[n].v_to : places[n].k_to;
+                if (to >= 0) store_loose<unsigned short, P / 2>((unsigned short *)(pool + to), got[n]);
+            }
         }
+        __syncthreads();  // the places have been read
     }
 }
 
 template <int P> hipError_t launch(const CopyArgs &a, hipStream_t stream)
 {
     if (!a.path) {
-        hipLaunchKernelGGL((copy_rows<P>), dim3(ceil_div(a.max_count, kTokens), a.n_seqs), dim3(256), 0, stream, a);
+        // (A workgroup for every kTokens that there may be: those beyond the counts end at once.)
+        const int64_t groups = std::min<int64_t>(((int64_t)a.max_count + kTokens - 1) / kTokens, 1 << 16);
+        hipLaunchKernelGGL((copy_rows<P>), dim3((unsigned)groups, a.n_seqs), dim3(256), 0, stream, a);
         return hipGetLastError();
     }
     const dim3 grid((unsigned)((2ll * a.kv_heads * (a.row_bytes / P) + 255) / 256), a.n_seqs);

@@ -830,3 +830,77 @@ def test_refusals_of_the_binding():
         ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], z, z, z, path=torch.zeros((4, 65), dtype=torch.int32, device="cuda"))
     with pytest.raises(ilpm.IlpmError):
         ilpm.kv_copy(s["kp"], s["vp"], s["table"], s["table"], z, z, z, max_count=-1)
+
+
+# ---- places beyond 2^31 elements and 2^32 bytes ----
+
+def test_places_beyond_32_bits():
+    """Pools of 4.4 GB each, with the pages that are used at both ends; a row of probabilities behind 2^31 others."""
+    ilpm = lib()
+    g = gen(41)
+    n_pages, page, hk, d = 67200, 16, 8, 256
+    kp, vp = (torch.empty((n_pages, page, hk, d), dtype=BF16, device="cuda") for _ in range(2))
+    used = [0, 1, n_pages - 3, n_pages - 2, n_pages - 1, 65537]
+    small = attn_case(g, [40], [[-1, 0, 0, 1]], 16, hk, d, BF16, BF16, page)
+    # The small case's pages, at these places.
+    small["kp"], small["vp"] = (randn(g, (len(used), page, hk, d), BF16) for _ in range(2))
+    order = torch.tensor([[4, 2, 3]])
+    small["table"] = order.to(torch.int32)
+    big = torch.tensor(used)[order].to(torch.int32).cuda()
+    for i, p in enumerate(used):
+        kp[p], vp[p] = small["kp"][i].cuda(), small["vp"][i].cuda()
+    note("[far] attn_tree")
+    check_attn(small, "far pages", dict(kp=kp, vp=vp, table=big))
+    check_attn(small, "far pages, split", dict(kp=kp, vp=vp, table=torch.cat((big, torch.full((1, 500), -1, dtype=torch.int32, device="cuda")), 1)))
+    note("[far] kv_append_norm")
+    c = append_case(g, 4, 1, 16, hk, d, 128, BF16, BF16, page, 3, "rms")
+    t = {k: v.cuda() for k, v in c.items()}
+    c["table"], c["kp"], c["vp"] = small["table"], small["kp"], small["vp"]
+    c["slots"] = ints([0, 15, 16, 47])
+    ilpm.kv_append_norm(t["k"], t["v"], kp, vp, big, t["seq"], t["pos"], slots=c["slots"].cuda(), q=t["q"], norm="rms", q_w=t["q_w"], k_w=t["k_w"],
+                        eps=1e-5, cos=t["cos"], sin=t["sin"])
+    torch.cuda.synchronize()
+    keys, err, values, written = ref.append(c["k"], c["v"], c["kp"], c["vp"], c["table"], c["seq"].tolist(), c["pos"].tolist(), c["slots"].tolist(),
+                                            "rms", c["k_w"], 1e-5, c["cos"], c["sin"], False)
+    err = torch.where(written[:, :, None, None], err + U[BF16] * (keys.abs() + err) + TINY[BF16], 0.0)
+    for i, p in enumerate(used):
+        near(kp[p], keys[i], err[i], f"page {p} keys")
+        assert torch.equal(vp[p].cpu().double(), values[i])
+    note("[far] kv_copy")
+    now = [torch.stack([x[p] for p in used]).cpu() for x in (kp, vp)]
+    src, dst = torch.tensor([[4, 2, 3]]), torch.tensor([[1, 5, 0]])
+    path = ints([[20, 3, 40, 41, 0]])
+    for p in (None, path):
+        z, n = ints([0]).cuda(), ints([5 if p is not None else 45]).cuda()
+        ilpm.kv_copy(kp, vp, torch.tensor(used)[src].to(torch.int32).cuda(), torch.tensor(used)[dst].to(torch.int32).cuda(), z, z, n,
+                     path=None if p is None else p.cuda())
+        torch.cuda.synchronize()
+        now = [ref.copy(x, src, dst, [0], [0], n.tolist(), p, 48) for x in now]
+        for x, want in zip((kp, vp), now):
+            for i, at in enumerate(used):
+                assert torch.equal(x[at].cpu(), want[i]), at
+    del kp, vp
+    note("[far] verify_drafts")
+    for draft in (False, True):
+        v = verify_case(g, 2, 3, 40000, BF16, draft)
+        far = torch.empty((1 << 31) + 3 * 80000, dtype=BF16, device="cuda").as_strided((2, 3, 40000), ((1 << 31) + 7, 80000, 1))
+        far.copy_(v["target"])
+        cuda = dict(target=far)
+        if draft:
+            cuda["draft"] = torch.empty(3 * 80000 + (1 << 31), dtype=BF16, device="cuda").as_strided((2, 3, 40000), ((1 << 31) + 7, 80000, 1))
+            cuda["draft"].copy_(v["draft"])
+        check_verify(v, f"far rows, draft {draft}", cuda)
+
+
+def test_attention_of_very_many_rows_of_a_head():
+    """More rows of one key head than a dimension of a grid holds."""
+    ilpm = lib()
+    g = gen(42)
+    c = attn_case(g, [600], [chain(64)], 1100, 1, 64, BF16, BF16, 16, extra=50)
+    t = {k: v.cuda() for k, v in c.items()}
+    got, lse = ilpm.attn_tree(t["q"], t["kp"], t["vp"], t["table"], t["lengths"], t["parents"], return_lse=True)
+    torch.cuda.synchronize()
+    few = [0, 1, 515, 1098, 1099]
+    want, want_lse, err, err_lse = ref.attention(c["q"][:, few], c["kp"], c["vp"], c["table"], c["lengths"], c["parents"], 64 ** -0.5)
+    near(got[:, few], want, err, "some heads of 1100")
+    near(lse[:, few], want_lse, err_lse, "some heads of 1100, lse")
