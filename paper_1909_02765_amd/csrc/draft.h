@@ -63,6 +63,7 @@ struct TreeArgs {
     Divisor by_group{1};
     int row_blocks;  // of 16 rows that a workgroup takes
     bool pieces;     // heads are whole pieces of 16 bytes
+    bool by_rows;    // the waves take rows, not keys (short sequences)
 };
 // What a unit costs beside its tiles, in tiles, by its row blocks.
 __host__ __device__ inline int tree_unit_cost(int row_blocks) { return 12 + 4 * row_blocks; }

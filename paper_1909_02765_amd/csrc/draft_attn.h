@@ -90,7 +90,10 @@ __device__ inline const TreeArgs &args_of(TreeArgsAt at)
 }
 
 // A head size's class, and what of AttnKernel's does not hold here.
-template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeKernel : AttnKernel<TC, Q16, DC, R, false> {
+// MA: blocks of 16 rows that a wave holds.  RS (for short sequences): the waves of a
+// workgroup take a block each and all keys, in the place of all blocks and a quarter
+// of the keys, and have nothing to join.
+template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS> struct TreeKernel : AttnKernel<TC, Q16, DC, R, false> {
     using Base = AttnKernel<TC, Q16, DC, R, false>;
     // Of the three that a wave gives to at the end, how many at once: what LDS has room for.
     static constexpr int GIVE = MA == 4 ? 2 : 3;
@@ -98,30 +101,32 @@ template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeKernel : Att
     // moved up to them, and what f16 probabilities are scaled by so that they still fit.
     static constexpr float SLACK = __is_same(TC, _Float16) ? 4.f : 8.f;
     static constexpr float UP = __is_same(TC, _Float16) ? 0x1p11f : 1.f;
+    static constexpr int WB = RS ? 4 : MA;  // blocks of rows of a workgroup
     // Workgroups that a compute unit holds at once.
     static constexpr int PER_CU = R == kAny ? (DC >= 192 ? 1 : 2)
                                   : sizeof(TC) == 4 ? (DC >= 192 ? 1 : DC == 64 && MA == 1 ? 3 : 2)
                                   : MA == 1 ? (DC == 64 ? 4 : DC == 96 ? 3 : 2) : MA == 2 ? (DC == 64 ? 3 : DC <= 128 ? 2 : 1) : 2;
 };
 
-template <typename Cfg, int MA> struct TreeLds {
+template <typename Cfg, int MA, bool RS> struct TreeLds {
+    static constexpr int WB = Cfg::WB;
     Places places[4][2];
     FindShare found;
     // Of each row: the nodes that it sees, and the first place (a row of no node: 0 bits).
-    unsigned long long bits[16 * MA];
-    int low[16 * MA];
-    float unscale[16 * MA];
+    unsigned long long bits[16 * WB];
+    int low[16 * WB];
+    float unscale[16 * WB];
     int top_low;  // the largest of low
     // Values of rows that are not finite for a key that not all rows see.
     int any_odd;
-    unsigned odd[16 * MA][16];
+    unsigned odd[16 * WB][16];
     // Of each row each wave's maximum and sum.
-    float m[4][16 * MA], l[4][16 * MA];
+    float m[RS ? 1 : 4][16 * MA], l[RS ? 1 : 4][16 * MA];
     union {
         // The queries, as the lanes of the first product take them, in parts those of 32 bits.
-        Words16 q[Cfg::QP][Cfg::NK][MA][64];
+        Words16 q[Cfg::QP][Cfg::NK][WB][64];
         // What each wave gives to another of its outputs, as they lie in registers.
-        floatx4 give[Cfg::GIVE][4][MA * Cfg::NO / 4][64];
+        floatx4 give[RS ? 1 : Cfg::GIVE][RS ? 1 : 4][RS ? 1 : MA * Cfg::NO / 4][64];
     };
 };
 
@@ -136,11 +141,11 @@ struct TreeSegment {
 __device__ inline int row_in_unit(const TreeSegment &seg, int rows_of_block, int r) { return seg.block * rows_of_block + r; }
 
 // What a wave reads for a segment's rows: its lanes' parents, and queries as they
-// lie in memory.  Wave w takes block w % MA, and of it every (4 / MA)-th piece.
-template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeRows {
-    using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
+// lie in memory.  Wave w takes block w % WB, and of it every (4 / WB)-th piece.
+template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS> struct TreeRows {
+    using Cfg = TreeKernel<TC, Q16, DC, R, MA, RS>;
     using TQ = std::conditional_t<Q16, TC, float>;
-    static constexpr int KV = Cfg::KV, NK = Cfg::NK, QP = Cfg::QP, STEP = 4 / MA, MINE = (NK + STEP - 1) / STEP;
+    static constexpr int KV = Cfg::KV, NK = Cfg::NK, QP = Cfg::QP, WB = Cfg::WB, STEP = 4 / WB, MINE = (NK + STEP - 1) / STEP;
     int parent;
     const TQ *row;
     Words16 q[QP == 1 ? MINE : 1];
@@ -149,9 +154,9 @@ template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeRows {
     {
         const TreeArgs &t = args_of(args);
         const AttnArgs &a = t.a;
-        const int n16 = lane & 15, g = lane >> 4, ma = wave % MA, c0 = wave / MA;
+        const int n16 = lane & 15, g = lane >> 4, ma = wave % WB, c0 = wave / WB;
         parent = lane < t.n_nodes ? t.parents[(int64_t)seg.seq * t.n_nodes + lane] : -2;
-        const int in_unit = min(row_in_unit(seg, 16 * MA, ma * 16 + n16), t.rows - 1), node = t.by_group.of(in_unit);
+        const int in_unit = min(row_in_unit(seg, 16 * WB, ma * 16 + n16), t.rows - 1), node = t.by_group.of(in_unit);
         row = (const TQ *)a.q + ((int64_t)seg.seq * t.n_nodes + node) * a.q_row +
               ((int64_t)seg.kvh * a.group + (in_unit - node * a.group)) * a.q_head;
         if constexpr (QP == 1) {
@@ -165,8 +170,8 @@ template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeRows {
     {
         const TreeArgs &t = args_of(args);
         const AttnArgs &a = t.a;
-        const int ma = wave % MA, c0 = wave / MA;
-        for (int i = threadIdx.x; i < 16 * MA * 16; i += 256) lds.odd[i / 16][i % 16] = 0;
+        const int ma = wave % WB, c0 = wave / WB;
+        for (int i = threadIdx.x; i < 16 * WB * 16; i += 256) lds.odd[i / 16][i % 16] = 0;
         if (threadIdx.x == 0) lds.any_odd = 0;
         if constexpr (QP == 1) {
 #pragma unroll
@@ -192,7 +197,8 @@ template <typename TC, bool Q16, int DC, Rows R, int MA> struct TreeRows {
 #pragma unroll 1
             for (int d = 32; d > 0; d >>= 1) top = max(top, __shfl_xor(top, d));
         if (lane == 0) lds.top_low = top;
-        const int r = min(lane, 16 * MA - 1), in_block = row_in_unit(seg, 16 * MA, r), node = min(t.by_group.of(in_block), t.n_nodes - 1);
+        static_assert(16 * WB <= 64, "a lane for each row");
+        const int r = min(lane, 16 * WB - 1), in_block = row_in_unit(seg, 16 * WB, r), node = min(t.by_group.of(in_block), t.n_nodes - 1);
         const unsigned b0 = __shfl((unsigned)bits, node), b1 = __shfl((unsigned)(bits >> 32), node);
         const int l = __shfl(low, node);
         lds.bits[r] = in_block < t.rows ? (unsigned long long)b1 << 32 | b0 : 0ull;
@@ -264,320 +270,12 @@ template <typename TC> __device__ inline unsigned not_finite(unsigned w)
     return ((w & E) == E ? 0xffffu : 0u) | ((w & (E << 16)) == (E << 16) ? 0xffff0000u : 0u);
 }
 
-// A wave's part of a segment, every fourth tile of it, and the join of the
-// four waves' parts, 16 rows at a time.
-template <typename TC, bool Q16, int DC, Rows R, int MA, typename Put>
-__device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment &seg, TreeLds<TreeKernel<TC, Q16, DC, R, MA>, MA> &lds, Put put)
+// Joins the four waves' parts of all rows, and puts them out.
+template <typename Cfg, int MA, typename Lds, typename Put>
+__device__ __forceinline__ void tree_join(TreeArgsAt args, const TreeSegment &seg, Lds &lds, floatx4 (&o)[MA][Cfg::NO], float (&m)[MA],
+                                          float (&l)[MA], int wave, int n16, int g, int lane, Put put)
 {
-    using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
-    constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
-    constexpr int QP = Cfg::QP, PP = Cfg::PP;
-    constexpr bool C16 = Cfg::C16;
-
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));
-    const int wave = uniform((int)(threadIdx.x >> 6));
-    const int n16 = lane & 15, g = lane >> 4;
-    const int seq = seg.seq;
-    const TreeRange range = seg.range;
-    const int sink_tiles = (range.sinks + 15) / 16;
-    // Tile j of this wave is tile 4j + wave of the segment.
-    int tiles = max(0, (seg.tile1 - seg.tile0 - wave + 3) / 4);
-    auto start_of = [&](int tile) { return tile < sink_tiles ? tile * 16 : range.first + (tile - sink_tiles) * 16; };
-
-    // Lane (n, g) looks up key n of tile 4*group + g.
-    struct Entry {
-        int page, slot;
-    };
-    auto look_up = [&](int group) {
-        const AttnArgs &a = args_of(args).a;
-        Entry e = {-1, 0};
-        const int tile = seg.tile0 + (group * 4 + g) * 4 + wave;
-        const int64_t key = (int64_t)start_of(tile) + n16;
-        if (tile < seg.tile1 && key < (tile < sink_tiles ? range.sinks : range.end)) {
-            const int p = (int)key / a.page_size;
-            e.slot = (int)key - p * a.page_size;
-            e.page = a.table[(int64_t)seq * a.table_stride + p];
-            if (a.mask && (key >= a.mask_len || !a.mask[(int64_t)seq * a.mask_stride + key])) e.page = -1;
-        }
-        return e;
-    };
-    // Where a group's keys lie, in LDS (those that are not seen at the pool's first row: it is read, and none of it
-    // used), and which are seen: bit 16t + n is key n of its tile t.
-    unsigned long long seen_of[2] = {0, 0};
-    auto place = [&](int group, Entry e) {
-        const AttnArgs &a = args_of(args).a;
-        const bool ok = e.page >= 0 && e.page < a.n_pages;
-        Places &p = lds.places[wave][group & 1];
-        p.k[lane] = ok ? (int64_t)e.page * a.k_page + (int64_t)e.slot * a.k_slot : 0;
-        p.v[lane] = ok ? (int64_t)e.page * a.v_page + (int64_t)e.slot * a.v_slot : 0;
-        const unsigned long long seen = __builtin_amdgcn_ballot_w64(ok);
-        if (group & 1) seen_of[1] = seen;
-        else seen_of[0] = seen;
-        // (Only this wave reads them, and a wave's LDS accesses keep their order.)
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    };
-    const TreeArgs &t = args_of(args);
-    const AttnArgs &a = t.a;
-    const TC *kh = (const TC *)a.k + (int64_t)seg.kvh * a.k_head;
-    const TC *vh = (const TC *)a.v + (int64_t)seg.kvh * a.v_head;
-    const int dim = a.dim, all_sinks = t.sinks;
-    const float softcap = a.softcap;
-    Words16 kt[NK];
-    Words<sizeof(TC) * VV> vt[4][NV];
-    // (Behind the last tile that one again.)
-    auto load_k = [&](int j) {
-        j = min(j, tiles - 1);
-        const TC *row = kh + lds.places[wave][(j >> 2) & 1].k[(j & 3) * 16 + n16];
-#pragma unroll
-        for (int c = 0; c < NK; ++c) kt[c] = load_piece<TC, KV, R, true>(row, (g + 4 * c) * KV, dim);
-    };
-    auto load_v = [&](int j) {
-        j = min(j, tiles - 1);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const TC *row = vh + lds.places[wave][(j >> 2) & 1].v[(j & 3) * 16 + 4 * g + r];
-#pragma unroll
-            for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
-                vt[r][c] = load_piece<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R, false>(row, (n16 + 16 * c) * VV, dim);
-        }
-    };
-
-    Entry e0 = {}, next = {};
-    if (tiles > 0) e0 = look_up(0);
-    if (tiles > 4) next = look_up(1);
-    // The first tile, the rows' nodes and queries: none waits for another.
-    TreeRows<TC, Q16, DC, R, MA> rows;
-    rows.load(args, seg, lane, wave);
-    // (Behind the last node of a smaller tree there is nothing to do.)
-    const unsigned long long nodes = __builtin_amdgcn_ballot_w64(rows.parent >= -1 && rows.parent < lane);
-    if (row_in_unit(seg, 16 * MA, 0) >= (64 - (nodes ? __builtin_clzll(nodes) : 64)) * a.group) tiles = 0;
-    if (tiles > 0) {
-        place(0, e0);
-        load_k(0);
-        load_v(0);
-    }
-    rows.store(args, seg, lane, wave, lds);
-    __syncthreads();
-
-    floatx4 o[MA][NO];
-    float m[MA], l[MA];
-#pragma unroll
-    for (int ma = 0; ma < MA; ++ma) {
-        m[ma] = -INFINITY;
-        l[ma] = 0.f;
-#pragma unroll
-        for (int i = 0; i < NO; ++i) o[ma][i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    const float scale2 = softcap > 0.f ? a.scale / softcap : a.scale * kLog2e;
-    const float cap2 = softcap * kLog2e;
-    const int top_low = uniform(lds.top_low);
-    constexpr bool UNSCALE = QP == 3 && __is_same(TC, _Float16);  // (parts of bf16 need none)
-
-    // Value i of piece c of a lane's four rows, put together from their 16-bit halves.
-    auto values = [&](int c, int i) {
-        const unsigned halves = i & 1 ? 0x07060302u : 0x05040100u;
-        return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], halves), __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], halves)};
-    };
-    // Which of the keys key0..key0 + 15 row r sees, where they are in the cache.
-    auto sees = [&](int r, int64_t key0) {
-        auto upto = [](int64_t n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << (int)n) - 1u; };  // the first n keys
-        const unsigned long long bits = lds.bits[r];
-        const int64_t node0 = key0 - range.length;
-        const unsigned nodes = (unsigned)(node0 >= 0 ? node0 < 64 ? bits >> (int)node0 : 0 : node0 > -16 ? bits << (int)-node0 : 0);
-        const unsigned before = upto(-node0);  // the sequence's own
-        return (nodes & ~before & 0xffffu) | (before & (~upto(lds.low[r] - key0) | upto(all_sinks - key0)));
-    };
-    // Takes values that are not finite out of a tile whose rows do not see the same keys, and marks the rows that see
-    // them: bit c * VV + i of odd[row][n] stands for value (n + 16c) * VV + i.  (Hardly ever.)
-    auto take_out = [&](int64_t key0) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            unsigned odd = 0;
-#pragma unroll
-            for (int c = 0; c < NV; ++c) {
-                if constexpr (C16) {
-#pragma unroll
-                    for (int i = 0; i < VV / 2; ++i) {
-                        const unsigned w = not_finite<TC>(vt[r][c][i]);
-                        vt[r][c][i] &= ~w;
-                        odd |= (w & 1u) << (c * VV + 2 * i) | (w >> 31) << (c * VV + 2 * i + 1);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < VV; ++i) {
-                        const bool is = (vt[r][c][i] & 0x7f800000u) == 0x7f800000u;
-                        vt[r][c][i] = is ? 0u : vt[r][c][i];
-                        odd |= (is ? 1u : 0u) << (c * VV + i);
-                    }
-                }
-            }
-            if (odd == 0) continue;
-            lds.any_odd = 1;
-#pragma unroll 1
-            for (int row = 0; row < 16 * MA; ++row)
-                if ((sees(row, key0) >> (4 * g + r)) & 1) atomicOr(&lds.odd[row][n16], odd);
-        }
-    };
-
-#pragma unroll 1
-    for (int j = 0; j < tiles; ++j) {
-        if ((j & 3) == 2 && j + 2 < tiles) {
-            place(j / 4 + 1, next);
-            if (j + 6 < tiles) next = look_up(j / 4 + 2);
-        }
-        const int tile = seg.tile0 + 4 * j + wave;
-        const int64_t key0 = start_of(tile);
-        const bool special = key0 + 15 >= range.length || (tile >= sink_tiles && key0 < top_low);
-
-        // The scores of the blocks of rows, then the next tile's keys are on their way.
-        floatx4 s[MA];
-        int ql = lane;
-        asm volatile("" : "+v"(ql));  // (read for each tile, not kept)
-#pragma unroll
-        for (int ma = 0; ma < MA; ++ma) {
-            floatx4 x = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (!C16) {
-#pragma unroll
-                for (int c = 0; c < NK; ++c) {
-                    const floatx4 q = __builtin_bit_cast(floatx4, lds.q[0][c][ma][ql]);
-#pragma unroll
-                    for (int i = 0; i < KV; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, kt[c])[i], q[i], x, 0, 0, 0);
-                }
-            } else {
-                floatx4 low = x;
-#pragma unroll
-                for (int c = 0; c < NK; ++c) {
-                    x = mfma_scores<TC>(kt[c], lds.q[0][c][ma][ql], x);
-                    if constexpr (QP == 3) {
-                        low = mfma_scores<TC>(kt[c], lds.q[1][c][ma][ql], low);
-                        low = mfma_scores<TC>(kt[c], lds.q[2][c][ma][ql], low);
-                    }
-                }
-                if constexpr (QP == 3) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] += low[r] - low[r] == 0.f ? low[r] : 0.f;
-                }
-            }
-            s[ma] = x;
-        }
-        load_k(j + 1);
-
-        // Scores times `by` are logarithms to the base 2; with a cap, or a scale that is not above 0, they are first made so.
-        float by[MA];
-#pragma unroll
-        for (int ma = 0; ma < MA; ++ma) by[ma] = UNSCALE ? scale2 * lds.unscale[ma * 16 + n16] : scale2;
-        if (softcap > 0.f || !(scale2 > 0.f)) {
-#pragma unroll
-            for (int ma = 0; ma < MA; ++ma) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[ma][r] *= by[ma];
-                    if (softcap > 0.f) s[ma][r] = cap2 * tanh_of(s[ma][r]);
-                }
-                by[ma] = 1.f;
-            }
-        }
-        // Most tiles are seen whole by all rows.
-        const unsigned tile_seen = (unsigned)((j & 4 ? seen_of[1] : seen_of[0]) >> ((j & 3) * 16)) & 0xffffu;
-        if (special || tile_seen != 0xffffu) {
-            bool seen[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) seen[r] = ((tile_seen >> (4 * g + r)) & 1) != 0;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int c = 0; c < NV; ++c) {
-                    using V = std::remove_reference_t<decltype(vt[r][c])>;
-                    vt[r][c] = seen[r] ? vt[r][c] : V{};
-                }
-            if (special) take_out(key0);
-#pragma unroll
-            for (int ma = 0; ma < MA; ++ma) {
-                const unsigned see = (special ? sees(ma * 16 + n16, key0) & tile_seen : tile_seen) >> (4 * g);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[ma][r] = (see >> r) & 1 ? s[ma][r] : -INFINITY;
-            }
-        }
-        constexpr int PW = !C16 ? 4 : PP == 3 ? 6 : 4;
-        unsigned part[MA][PW];  // probabilities: hi and lo of four keys, a third part; or 32 bits
-#pragma unroll
-        for (int ma = 0; ma < MA; ++ma) {
-            const float top = fmaxf(fmaxf(s[ma][0], s[ma][1]), fmaxf(s[ma][2], s[ma][3])) * by[ma];
-            // (m may lie up to SLACK below the maximum: most tiles after the first leave it where it is.)
-            if (__builtin_amdgcn_ballot_w64(top > m[ma] + Cfg::SLACK)) {
-                const float m_new = fmaxf(m[ma], max_of_head(top));
-                const float alpha = __builtin_amdgcn_exp2f(m[ma] - (m_new == -INFINITY ? 0.f : m_new));
-                m[ma] = m_new;
-                l[ma] *= alpha;
-#pragma unroll
-                for (int i = 0; i < NO; ++i) o[ma][i] *= alpha;
-            }
-            const float base = m[ma] == -INFINITY ? 0.f : m[ma];
-            float x[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ma][r], by[ma], -base));
-            l[ma] += (x[0] + x[1]) + (x[2] + x[3]);
-            if constexpr (!C16) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) part[ma][r] = __builtin_bit_cast(unsigned, x[r]);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[r] *= Cfg::UP;
-                    if constexpr (Cfg::UP != 1.f) asm("" : "+v"(x[r]));  // (one product, not one for each of its uses)
-                }
-#pragma unroll
-                for (int i = 0; i < PP; ++i) {
-                    Pack<TC, 4> h;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        h.v[r] = (TC)x[r];
-                        x[r] -= (float)h.v[r];
-                    }
-                    const Words<8> w = __builtin_bit_cast(Words<8>, h);
-                    part[ma][2 * i] = w[0];
-                    part[ma][2 * i + 1] = w[1];
-                }
-            }
-        }
-
-        // The same four keys twice, against the first and second parts of their probabilities.
-        auto weigh = [&](int ma, int i, Words16 vv) {
-            floatx4 &sum = o[ma][i];
-            sum = mfma_values32<TC>(vv, Words16{part[ma][0], part[ma][1], part[ma][2], part[ma][3]}, sum);
-            // (By the same instruction: one of 16x16x16 right after it, on the same registers, found them as they were
-            // before it.)
-            if constexpr (PP == 3) sum = mfma_values32<TC>(vv, Words16{part[ma][4], part[ma][5], 0u, 0u}, sum);
-        };
-        if constexpr (!C16) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int c = 0; c < NV; ++c)
-#pragma unroll
-                    for (int i = 0; i < VV; ++i) {
-                        const float v = __builtin_bit_cast(floatx4, vt[r][c])[i];
-#pragma unroll
-                        for (int ma = 0; ma < MA; ++ma) {
-                                            o[ma][c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __builtin_bit_cast(float, part[ma][r]), o[ma][c * VV + i], 0, 0, 0);
-                        }
-                    }
-        } else {
-#pragma unroll
-            for (int c = 0; c < NV; ++c)
-#pragma unroll
-                for (int i = 0; i < VV; ++i) {
-                    const Words<8> v = values(c, i);
-#pragma unroll
-                    for (int ma = 0; ma < MA; ++ma) weigh(ma, c * VV + i, Words16{v[0], v[1], v[0], v[1]});
-                }
-        }
-        load_v(j + 1);
-    }
-
+    constexpr int NO = Cfg::NO, VV = Cfg::VV;
     // Join the waves.  Lane (n, g) holds values (4g + r + 16c) * VV + i of row n; what is no
     // node has seen keys of the sequence, and none counts.
 #pragma unroll
@@ -679,13 +377,358 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     });
 }
 
-template <typename TC, bool Q16, int DC, Rows R, int MA>
-__global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void tree_split(TreeArgs)
+// A wave's part of a segment, every fourth tile of it, and the join of the
+// four waves' parts; or (RS) all tiles for a block of rows.
+template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS, typename Put>
+__device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment &seg, TreeLds<TreeKernel<TC, Q16, DC, R, MA, RS>, MA, RS> &lds, Put put)
 {
-    using Cfg = TreeKernel<TC, Q16, DC, R, MA>;
+    using Cfg = TreeKernel<TC, Q16, DC, R, MA, RS>;
+    constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
+    constexpr int QP = Cfg::QP, PP = Cfg::PP;
+    constexpr bool C16 = Cfg::C16;
+
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int wave = uniform((int)(threadIdx.x >> 6));
+    const int n16 = lane & 15, g = lane >> 4;
+    const int seq = seg.seq;
+    const TreeRange range = seg.range;
+    const int sink_tiles = (range.sinks + 15) / 16;
+    // Tile j of this wave is tile 4j + wave (RS: j) of the segment.
+    constexpr int EVERY = RS ? 1 : 4, WB = Cfg::WB;
+    const int tile_of = seg.tile0 + (RS ? 0 : wave);
+    int tiles = max(0, (seg.tile1 - tile_of + EVERY - 1) / EVERY);
+    auto block = [&](int ma) { return RS ? wave : ma; };  // of the workgroup's
+    auto start_of = [&](int tile) { return tile < sink_tiles ? tile * 16 : range.first + (tile - sink_tiles) * 16; };
+
+    // Lane (n, g) looks up key n of tile 4*group + g.
+    struct Entry {
+        int page, slot;
+    };
+    auto look_up = [&](int group) {
+        const AttnArgs &a = args_of(args).a;
+        Entry e = {-1, 0};
+        const int tile = tile_of + (group * 4 + g) * EVERY;
+        const int64_t key = (int64_t)start_of(tile) + n16;
+        if (tile < seg.tile1 && key < (tile < sink_tiles ? range.sinks : range.end)) {
+            const int p = (int)key / a.page_size;
+            e.slot = (int)key - p * a.page_size;
+            e.page = a.table[(int64_t)seq * a.table_stride + p];
+            if (a.mask && (key >= a.mask_len || !a.mask[(int64_t)seq * a.mask_stride + key])) e.page = -1;
+        }
+        return e;
+    };
+    // Where a group's keys lie, in LDS (those that are not seen at the pool's first row: it is read, and none of it
+    // used), and which are seen: bit 16t + n is key n of its tile t.
+    unsigned long long seen_of[2] = {0, 0};
+    auto place = [&](int group, Entry e) {
+        const AttnArgs &a = args_of(args).a;
+        const bool ok = e.page >= 0 && e.page < a.n_pages;
+        Places &p = lds.places[wave][group & 1];
+        p.k[lane] = ok ? (int64_t)e.page * a.k_page + (int64_t)e.slot * a.k_slot : 0;
+        p.v[lane] = ok ? (int64_t)e.page * a.v_page + (int64_t)e.slot * a.v_slot : 0;
+        const unsigned long long seen = __builtin_amdgcn_ballot_w64(ok);
+        if (group & 1) seen_of[1] = seen;
+        else seen_of[0] = seen;
+        // (Only this wave reads them, and a wave's LDS accesses keep their order.)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    const TreeArgs &t = args_of(args);
+    const AttnArgs &a = t.a;
+    const TC *kh = (const TC *)a.k + (int64_t)seg.kvh * a.k_head;
+    const TC *vh = (const TC *)a.v + (int64_t)seg.kvh * a.v_head;
+    const int dim = a.dim, all_sinks = t.sinks;
+    const float softcap = a.softcap;
+    Words16 kt[NK];
+    Words<sizeof(TC) * VV> vt[4][NV];
+    // (Behind the last tile that one again.)
+    auto load_k = [&](int j) {
+        j = min(j, tiles - 1);
+        const TC *row = kh + lds.places[wave][(j >> 2) & 1].k[(j & 3) * 16 + n16];
+#pragma unroll
+        for (int c = 0; c < NK; ++c) kt[c] = load_piece<TC, KV, R, true>(row, (g + 4 * c) * KV, dim);
+    };
+    auto load_v = [&](int j) {
+        j = min(j, tiles - 1);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const TC *row = vh + lds.places[wave][(j >> 2) & 1].v[(j & 3) * 16 + 4 * g + r];
+#pragma unroll
+            for (int c = 0; c < NV; ++c)  // (sixteen lanes may reach beyond a whole row)
+                vt[r][c] = load_piece<TC, VV, R == kWhole && Cfg::DO != DC ? kPieces : R, false>(row, (n16 + 16 * c) * VV, dim);
+        }
+    };
+
+    Entry e0 = {}, next = {};
+    if (tiles > 0) e0 = look_up(0);
+    if (tiles > 4) next = look_up(1);
+    // The first tile, the rows' nodes and queries: none waits for another.
+    TreeRows<TC, Q16, DC, R, MA, RS> rows;
+    rows.load(args, seg, lane, wave);
+    // (Behind the last node of a smaller tree there is nothing to do.)
+    const unsigned long long nodes = __builtin_amdgcn_ballot_w64(rows.parent >= -1 && rows.parent < lane);
+    if (row_in_unit(seg, 16 * WB, RS ? wave * 16 : 0) >= (64 - (nodes ? __builtin_clzll(nodes) : 64)) * a.group) tiles = 0;
+    if (tiles > 0) {
+        place(0, e0);
+        load_k(0);
+        load_v(0);
+    }
+    rows.store(args, seg, lane, wave, lds);
+    __syncthreads();
+
+    floatx4 o[MA][NO];
+    float m[MA], l[MA];
+#pragma unroll
+    for (int ma = 0; ma < MA; ++ma) {
+        m[ma] = -INFINITY;
+        l[ma] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) o[ma][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float scale2 = softcap > 0.f ? a.scale / softcap : a.scale * kLog2e;
+    const float cap2 = softcap * kLog2e;
+    const int top_low = uniform(lds.top_low);
+    constexpr bool UNSCALE = QP == 3 && __is_same(TC, _Float16);  // (parts of bf16 need none)
+
+    // Value i of piece c of a lane's four rows, put together from their 16-bit halves.
+    auto values = [&](int c, int i) {
+        const unsigned halves = i & 1 ? 0x07060302u : 0x05040100u;
+        return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], halves), __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], halves)};
+    };
+    // Which of the keys key0..key0 + 15 row r sees, where they are in the cache.
+    auto sees = [&](int r, int64_t key0) {
+        auto upto = [](int64_t n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << (int)n) - 1u; };  // the first n keys
+        const unsigned long long bits = lds.bits[r];
+        const int64_t node0 = key0 - range.length;
+        const unsigned nodes = (unsigned)(node0 >= 0 ? node0 < 64 ? bits >> (int)node0 : 0 : node0 > -16 ? bits << (int)-node0 : 0);
+        const unsigned before = upto(-node0);  // the sequence's own
+        return (nodes & ~before & 0xffffu) | (before & (~upto(lds.low[r] - key0) | upto(all_sinks - key0)));
+    };
+    // Takes values that are not finite out of a tile whose rows do not see the same keys, and marks the rows that see
+    // them: bit c * VV + i of odd[row][n] stands for value (n + 16c) * VV + i.  (Hardly ever.)
+    auto take_out = [&](int64_t key0) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            unsigned odd = 0;
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                if constexpr (C16) {
+#pragma unroll
+                    for (int i = 0; i < VV / 2; ++i) {
+                        const unsigned w = not_finite<TC>(vt[r][c][i]);
+                        vt[r][c][i] &= ~w;
+                        odd |= (w & 1u) << (c * VV + 2 * i) | (w >> 31) << (c * VV + 2 * i + 1);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VV; ++i) {
+                        const bool is = (vt[r][c][i] & 0x7f800000u) == 0x7f800000u;
+                        vt[r][c][i] = is ? 0u : vt[r][c][i];
+                        odd |= (is ? 1u : 0u) << (c * VV + i);
+                    }
+                }
+            }
+            if (odd == 0) continue;
+            lds.any_odd = 1;
+#pragma unroll 1
+            for (int row = block(0) * 16; row < block(0) * 16 + 16 * MA; ++row)
+                if ((sees(row, key0) >> (4 * g + r)) & 1) atomicOr(&lds.odd[row][n16], odd);
+        }
+    };
+
+#pragma unroll 1
+    for (int j = 0; j < tiles; ++j) {
+        if ((j & 3) == 2 && j + 2 < tiles) {
+            place(j / 4 + 1, next);
+            if (j + 6 < tiles) next = look_up(j / 4 + 2);
+        }
+        const int tile = tile_of + j * EVERY;
+        const int64_t key0 = start_of(tile);
+        const bool special = key0 + 15 >= range.length || (tile >= sink_tiles && key0 < top_low);
+
+        // The scores of the blocks of rows, then the next tile's keys are on their way.
+        floatx4 s[MA];
+        int ql = lane;
+        asm volatile("" : "+v"(ql));  // (read for each tile, not kept)
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) {
+            floatx4 x = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (!C16) {
+#pragma unroll
+                for (int c = 0; c < NK; ++c) {
+                    const floatx4 q = __builtin_bit_cast(floatx4, lds.q[0][c][block(ma)][ql]);
+#pragma unroll
+                    for (int i = 0; i < KV; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, kt[c])[i], q[i], x, 0, 0, 0);
+                }
+            } else {
+                floatx4 low = x;
+#pragma unroll
+                for (int c = 0; c < NK; ++c) {
+                    x = mfma_scores<TC>(kt[c], lds.q[0][c][block(ma)][ql], x);
+                    if constexpr (QP == 3) {
+                        low = mfma_scores<TC>(kt[c], lds.q[1][c][block(ma)][ql], low);
+                        low = mfma_scores<TC>(kt[c], lds.q[2][c][block(ma)][ql], low);
+                    }
+                }
+                if constexpr (QP == 3) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] += low[r] - low[r] == 0.f ? low[r] : 0.f;
+                }
+            }
+            s[ma] = x;
+        }
+        load_k(j + 1);
+
+        // Scores times `by` are logarithms to the base 2; with a cap, or a scale that is not above 0, they are first made so.
+        float by[MA];
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) by[ma] = UNSCALE ? scale2 * lds.unscale[block(ma) * 16 + n16] : scale2;
+        if (softcap > 0.f || !(scale2 > 0.f)) {
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[ma][r] *= by[ma];
+                    if (softcap > 0.f) s[ma][r] = cap2 * tanh_of(s[ma][r]);
+                }
+                by[ma] = 1.f;
+            }
+        }
+        // Most tiles are seen whole by all rows.
+        const unsigned tile_seen = (unsigned)((j & 4 ? seen_of[1] : seen_of[0]) >> ((j & 3) * 16)) & 0xffffu;
+        if (special || tile_seen != 0xffffu) {
+            bool seen[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) seen[r] = ((tile_seen >> (4 * g + r)) & 1) != 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < NV; ++c) {
+                    using V = std::remove_reference_t<decltype(vt[r][c])>;
+                    vt[r][c] = seen[r] ? vt[r][c] : V{};
+                }
+            if (special) take_out(key0);
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma) {
+                const unsigned see = (special ? sees(block(ma) * 16 + n16, key0) & tile_seen : tile_seen) >> (4 * g);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[ma][r] = (see >> r) & 1 ? s[ma][r] : -INFINITY;
+            }
+        }
+        constexpr int PW = !C16 ? 4 : PP == 3 ? 6 : 4;
+        unsigned part[MA][PW];  // probabilities: hi and lo of four keys, a third part; or 32 bits
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) {
+            const float top = fmaxf(fmaxf(s[ma][0], s[ma][1]), fmaxf(s[ma][2], s[ma][3])) * by[ma];
+            // (m may lie up to SLACK below the maximum: most tiles after the first leave it where it is.)
+            if (__builtin_amdgcn_ballot_w64(top > m[ma] + Cfg::SLACK)) {
+                const float m_new = fmaxf(m[ma], max_of_head(top));
+                const float alpha = __builtin_amdgcn_exp2f(m[ma] - (m_new == -INFINITY ? 0.f : m_new));
+                m[ma] = m_new;
+                l[ma] *= alpha;
+#pragma unroll
+                for (int i = 0; i < NO; ++i) o[ma][i] *= alpha;
+            }
+            const float base = m[ma] == -INFINITY ? 0.f : m[ma];
+            float x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ma][r], by[ma], -base));
+            l[ma] += (x[0] + x[1]) + (x[2] + x[3]);
+            if constexpr (!C16) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) part[ma][r] = __builtin_bit_cast(unsigned, x[r]);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[r] *= Cfg::UP;
+                    if constexpr (Cfg::UP != 1.f) asm("" : "+v"(x[r]));  // (one product, not one for each of its uses)
+                }
+#pragma unroll
+                for (int i = 0; i < PP; ++i) {
+                    Pack<TC, 4> h;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        h.v[r] = (TC)x[r];
+                        x[r] -= (float)h.v[r];
+                    }
+                    const Words<8> w = __builtin_bit_cast(Words<8>, h);
+                    part[ma][2 * i] = w[0];
+                    part[ma][2 * i + 1] = w[1];
+                }
+            }
+        }
+
+        // The same four keys twice, against the first and second parts of their probabilities.
+        auto weigh = [&](int ma, int i, Words16 vv) {
+            floatx4 &sum = o[ma][i];
+            sum = mfma_values32<TC>(vv, Words16{part[ma][0], part[ma][1], part[ma][2], part[ma][3]}, sum);
+            // (By the same instruction: one of 16x16x16 right after it, on the same registers, found them as they were
+            // before it.)
+            if constexpr (PP == 3) sum = mfma_values32<TC>(vv, Words16{part[ma][4], part[ma][5], 0u, 0u}, sum);
+        };
+        if constexpr (!C16) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < NV; ++c)
+#pragma unroll
+                    for (int i = 0; i < VV; ++i) {
+                        const float v = __builtin_bit_cast(floatx4, vt[r][c])[i];
+#pragma unroll
+                        for (int ma = 0; ma < MA; ++ma) {
+                                            o[ma][c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __builtin_bit_cast(float, part[ma][r]), o[ma][c * VV + i], 0, 0, 0);
+                        }
+                    }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int i = 0; i < VV; ++i) {
+                    const Words<8> v = values(c, i);
+#pragma unroll
+                    for (int ma = 0; ma < MA; ++ma) weigh(ma, c * VV + i, Words16{v[0], v[1], v[0], v[1]});
+                }
+        }
+        load_v(j + 1);
+    }
+
+    if constexpr (RS) {
+        l[0] += __shfl_xor(l[0], 16);
+        l[0] += __shfl_xor(l[0], 32);
+        const int r = wave * 16 + n16;
+        if (row_in_unit(seg, 16 * WB, r) >= args_of(args).rows) return;
+        const bool real = lds.bits[r] != 0;  // (what is no node has seen keys of the sequence, and none counts)
+        unsigned odd[4] = {0, 0, 0, 0};
+        if (lds.any_odd) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) odd[i] = lds.odd[r][4 * g + i];
+        }
+        put(args_of(args), row_in_unit(seg, 16 * WB, r), r, real ? m[0] : -INFINITY, real ? l[0] : 0.f, g == 0, [&](auto &&give) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    Pack<float, VV> p;
+#pragma unroll
+                    for (int i = 0; i < VV; ++i)
+                        p.v[i] = !real ? 0.f : (odd[k] >> (c * VV + i)) & 1 ? __builtin_nanf("") : o[0][c * VV + i][k];
+                    give((4 * g + k + 16 * c) * VV, p);
+                }
+        });
+    } else {
+        tree_join<Cfg, MA>(args, seg, lds, o, m, l, wave, n16, g, lane, put);
+    }
+}
+
+template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS>
+__global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA, RS>::PER_CU)) void tree_split(TreeArgs)
+{
+    using Cfg = TreeKernel<TC, Q16, DC, R, MA, RS>;
     const int unit_cost = tree_unit_cost(MA);
     using TQ = std::conditional_t<Q16, TC, float>;
-    __shared__ TreeLds<Cfg, MA> lds;
+    __shared__ TreeLds<Cfg, MA, RS> lds;
     const TreeArgsAt args = (TreeArgsAt)__builtin_amdgcn_kernarg_segment_ptr();
     const TreeArgs &t = args_of(args);
     const AttnArgs &a = t.a;
@@ -698,13 +741,14 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
     const int share_at = wg / a.blocks, block = wg - share_at * a.blocks, shares = (int)gridDim.x / a.blocks;
     Share share = {0, 0, true};
     Begin begin;
-    if (a.split) share = find_share(a, share_at, shares, units, lds.found, &begin, [&](int n) { return tree_tiles(t, n); }, unit_cost);
+    if constexpr (!RS)
+        if (a.split) share = find_share(a, share_at, shares, units, lds.found, &begin, [&](int n) { return tree_tiles(t, n); }, unit_cost);
 
     // This workgroup's place: a sequence, its length and its units' tiles, a unit
     // of it, and how far into the unit's length the share has come.
     int seq, length, unit, tiles_all, x0 = 0;
     int at = 0, last = 0;
-    if (a.split && !a.part_of_unit && block == 0 && threadIdx.x == 0) a.parts[share_at] = AttnPart{0, 0, 0, 0};  // (whatever follows, the join reads it)
+    if (!RS && a.split && !a.part_of_unit && block == 0 && threadIdx.x == 0) a.parts[share_at] = AttnPart{0, 0, 0, 0};  // (whatever follows, the join reads it)
     if (share.whole) {
         if (share_at >= a.n_seqs * units) return;
         seq = share_at / units;
@@ -723,7 +767,7 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
         x0 = in - unit * (tiles_all + unit_cost);
     }
 
-    const bool split = a.split, part_of_unit = a.part_of_unit;
+    const bool split = !RS && a.split, part_of_unit = a.part_of_unit;
     const int n_seqs = a.n_seqs;
     for (;;) {
         const int x1 = share.whole ? tiles_all + unit_cost : min(tiles_all + unit_cost, x0 + (last - at));
@@ -739,7 +783,7 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
         if (seg.range.end == 0) seg.tile1 = tile0;  // (no keys, and perhaps no pool)
         const bool all = seg_tiles == tiles_all;  // of the unit's tiles
         // Row `row` of the unit, r of its block: its maximum and sum, and its values, in packs, from `each`.
-        tree_segment<TC, Q16, DC, R, MA>(args, seg, lds, [&](const TreeArgs &t, int row, int r, float top, float sum, bool lead, auto each) {
+        tree_segment<TC, Q16, DC, R, MA, RS>(args, seg, lds, [&](const TreeArgs &t, int row, int r, float top, float sum, bool lead, auto each) {
             const AttnArgs &a = t.a;
             auto put = [&](auto *to, float by) {
                 each([&](int d, auto p) {
@@ -772,6 +816,7 @@ __global__ __launch_bounds__(256, (TreeKernel<TC, Q16, DC, R, MA>::PER_CU)) void
                 }
             }
         });
+        if (RS) return;
         const AttnArgs &a = args_of(args).a;
         // Who begins a unit says whether others go on with it.
         if (split && block == 0 && threadIdx.x == 0 && tile0 == 0) {
@@ -806,10 +851,14 @@ template <typename TC, bool Q16, int DC> hipError_t tree_split_launch(const Tree
 {
     constexpr int MOST = kMostBlocks<TC, DC>;
     auto launch = [&](auto rows, auto blocks) {
-        hipLaunchKernelGGL((tree_split<TC, Q16, DC, decltype(rows)::value, decltype(blocks)::value>), dim3(t.a.grid), dim3(256), 0, stream, t);
+        hipLaunchKernelGGL((tree_split<TC, Q16, DC, decltype(rows)::value, decltype(blocks)::value, false>), dim3(t.a.grid), dim3(256), 0, stream, t);
         return hipGetLastError();
     };
     auto by_blocks = [&](auto rows) {
+        if (t.by_rows) {
+            hipLaunchKernelGGL((tree_split<TC, Q16, DC, decltype(rows)::value, 1, true>), dim3(t.a.grid), dim3(256), 0, stream, t);
+            return hipGetLastError();
+        }
         if constexpr (MOST >= 4)
             if (t.row_blocks == 4) return launch(rows, std::integral_constant<int, 4>{});
         if constexpr (MOST >= 2)
@@ -843,9 +892,9 @@ template <typename TC, bool Q16> int tree_card_by_dim(int dim, bool pieces, int 
 {
     return kAttnCus * tree_by_class<TC, Q16>(dim, [&](auto dc) {
         constexpr int DC = decltype(dc)::value;
-        if (!pieces) return TreeKernel<TC, Q16, DC, kAny, 1>::PER_CU;
-        return blocks == 4 ? TreeKernel<TC, Q16, DC, kPieces, 4>::PER_CU
-               : blocks == 2 ? TreeKernel<TC, Q16, DC, kPieces, 2>::PER_CU : TreeKernel<TC, Q16, DC, kPieces, 1>::PER_CU;
+        if (!pieces) return TreeKernel<TC, Q16, DC, kAny, 1, false>::PER_CU;
+        return blocks == 4 ? TreeKernel<TC, Q16, DC, kPieces, 4, false>::PER_CU
+               : blocks == 2 ? TreeKernel<TC, Q16, DC, kPieces, 2, false>::PER_CU : TreeKernel<TC, Q16, DC, kPieces, 1, false>::PER_CU;
     });
 }
 

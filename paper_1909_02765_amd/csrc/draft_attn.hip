@@ -145,7 +145,18 @@ __global__ __launch_bounds__(256) void tree_join_rows(TreeArgs t, int lanes, Div
 
 // As attn_plan: either a unit (a key head of a sequence) goes to a workgroup for each
 // of its blocks of rows, or as many workgroups as the card holds share all tiles,
-// each share a workgroup for each block.
+// each share a workgroup for each block, and a second kernel joins their parts.  Up to
+// 16 tiles, and with W workgroups up to W / 2 tiles and 100, units are faster (tiles of
+// more than 8 KB count as several: 140 units of 64 tiles of 32 KB 45 us shared and 63 by units): 40 x 600
+// bf16 keys of 8 heads of 128 under 16 nodes of 32 heads 40 us shared and 31 by units
+// (W 320, 39 tiles), 8 x 400 25 and 18 (64, 26), 20 x 1200 35 and 33 (160, 76), but 8 x
+// 800 under 3 nodes, f32 over f16 heads of 80, 18 and 19 (64, 51), 8 x 1500 20 and 28.
+//
+// By units, up to 16 tiles and for more than 32 rows, the waves of a workgroup take rows
+// and not keys: a unit of one tile then takes 7 us in the place of 12 (2048 units of 64
+// rows, bf16 heads of 128, 48 -> 29 us; at 8 tiles 66 and 65).  With few workgroups, which
+// leave compute units idle, that makes the tiles' chain longer from 5 tiles on (12 nodes
+// of 80 / 8 f32 heads over 60 keys 13.6 -> 16.1 us), and keys are split there.
 size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
 {
     AttnArgs *a = &t->a;
@@ -165,8 +176,12 @@ size_t tree_plan(TreeArgs *t, int cache_dtype, bool q32, int max_len)
     const int64_t tiles = std::max<int64_t>(1, (keys + 15) / 16 + (sinks + 15) / 16);
     // (Tiles are counted in 32 bits.  Where a table could name more, there are units enough without a split.)
     const int64_t span = (((int64_t)a->capacity + 15) / 16 + 2 + tree_unit_cost(t->row_blocks)) * units;
-    a->split = tiles > kWholeTiles && units > 0 && (span < INT_MAX || units == 1);
+    const int64_t groups = units * a->blocks;
+    const int64_t weight = std::max<int64_t>(8 << 10, (int64_t)a->dim * element_bytes(cache_dtype) * 32);
+    a->split = tiles > kWholeTiles && tiles * weight > std::min<int64_t>(100, groups / 2) * (8 << 10) && units > 0 && (span < INT_MAX || units == 1);
+    t->by_rows = !a->split && t->pieces && t->rows > 32 && tiles <= kWholeTiles && (tiles <= 4 || units * ceil_div(t->rows, 64) >= 32);
     if (!a->split) {
+        if (t->by_rows) t->row_blocks = 4, a->blocks = ceil_div(t->rows, 64);
         a->grid = (int)units * a->blocks;
         return 0;
     }
