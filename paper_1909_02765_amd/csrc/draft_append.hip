@@ -121,7 +121,10 @@ template <typename TX, typename TC, typename TP> __global__ __launch_bounds__(25
     else put((TC *)a.kc + (int64_t)at.page * a.kc_page + (int64_t)at.slot * a.kc_slot + h * a.kc_head);
 }
 
-constexpr int kCardGroups = 256 * 8;  // workgroups of 256 threads that the card holds at once
+// Workgroups of 256 threads in a launch at most: twice what the card holds at once of the
+// largest variant.  16381 tokens of 56 bf16 heads of 128 take 102 us (4.7 TB/s) so and with
+// half as many, 140 with a workgroup for each token, which all begin anew.
+constexpr int kCardGroups = 256 * 8;
 
 // N weights from i on.
 template <typename TP, int N> __device__ inline void load_weights(const void *w, int i, float *to)
@@ -162,19 +165,30 @@ template <int VEC> struct Lanes {
     }
 };
 
-// 2^log lanes a head, one or two packs of VEC elements each; what a pack shares with
+// How heads lie over a wave: `lanes` each (of which the last may have nothing to do), and
+// as many heads as fit; log: lanes are 2^log, or -1.
+struct Spread {
+    int lanes, log, heads;
+    int blocks, slices;  // waves that a token takes, tokens that the launch takes at a time
+    Divisor by_lanes{1}, by_blocks{1};
+};
+
+// `lanes` lanes a head, one or two packs of VEC elements each; what a pack shares with
 // the one before it counts in the sums once, and both write the same.  A lane keeps
-// its place in a head and its weights over the tokens blockIdx.y, blockIdx.y +
-// gridDim.y, ...  What bounds it: the bytes of queries, keys and values, read and
-// written once.
+// its place in a head and its weights over every `slices`th token.  Waves lie one
+// after the other over a token's heads and then over tokens (with whole workgroups for
+// each token, 8191 f32 tokens of 56 heads of 128 took 101 us and not 89).  What bounds
+// it: the bytes of queries, keys and values, read and written once.
 template <typename TX, typename TC, typename TP, int VEC>
-__global__ __launch_bounds__(256) void append_norm_packs(AppendNormArgs n, Divisor by_page, int log)
+__global__ __launch_bounds__(256) void append_norm_packs(AppendNormArgs n, Divisor by_page, Spread spread)
 {
     const AppendArgs &a = n.a;
     const Lanes<VEC> as(a.dim, a.rot_dim, a.pairs != 0);
-    const int lanes = 1 << log, heads = a.q_heads + 2 * a.kv_heads, half = a.rot_dim / 2;
-    const int id = (int)(blockIdx.x * 256 + threadIdx.x), i = id >> log, u = id & (lanes - 1);
-    if (i >= heads) return;  // (whole heads: a wave's lanes of a head stay together)
+    const int heads = a.q_heads + 2 * a.kv_heads, half = a.rot_dim / 2;
+    const int lane = (int)threadIdx.x & 63, in_wave = spread.by_lanes.of(lane), u = lane - in_wave * spread.lanes;
+    const int wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
+    const int t0 = spread.by_blocks.of(wave), i = (wave - t0 * spread.blocks) * spread.heads + in_wave;
+    if (t0 >= spread.slices || i >= heads || in_wave >= spread.heads) return;  // (whole heads: a head's lanes stay together)
     const bool query = i < a.q_heads, value = i >= a.q_heads + a.kv_heads, on = u < as.all;
     const int h = query ? i : value ? i - a.q_heads - a.kv_heads : i - a.q_heads;
     const bool rotated = u < as.turned, two = rotated ? as.two_turned : as.two_rest;
@@ -207,9 +221,9 @@ __global__ __launch_bounds__(256) void append_norm_packs(AppendNormArgs n, Divis
         k.slot = n.slots[t];
         return k;
     };
-    Token next = read((int)blockIdx.y);
+    Token next = read(t0);
 #pragma unroll 1
-    for (int t = (int)blockIdx.y; t < a.n_tokens; t += (int)gridDim.y) {
+    for (int t = t0; t < a.n_tokens; t += spread.slices) {
         const Token k = next;
         const bool known = a.rot_dim > 0 && k.pos >= 0 && k.pos < a.n_positions, turn = turns && known;
         Place at = {-1, 0};
@@ -226,7 +240,7 @@ __global__ __launch_bounds__(256) void append_norm_packs(AppendNormArgs n, Divis
             c[0] = load_loose<float, HV>(cs + first), s[0] = load_loose<float, HV>(sn + first);
             c[1] = load_loose<float, HV>(cs + second), s[1] = load_loose<float, HV>(sn + second);
         }
-        next = read((int)min((int64_t)t + gridDim.y, (int64_t)a.n_tokens));  // (behind what this token waits for)
+        next = read((int)min((int64_t)t + spread.slices, (int64_t)a.n_tokens));  // (behind what this token waits for)
         float x[VEC], y[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) x[j] = (float)k.p.v[j], y[j] = (float)k.p2.v[j];
@@ -239,7 +253,18 @@ __global__ __launch_bounds__(256) void append_norm_packs(AppendNormArgs n, Divis
                     v += j >= over ? f(x[j]) : 0.f;
                     v2 += j >= over ? f(y[j]) : 0.f;
                 }
-                return sum_lanes(two ? v + v2 : v, log);
+                v = two ? v + v2 : v;
+                if (spread.log >= 0) return sum_lanes(v, spread.log);
+                float all = 0.f;
+#pragma unroll 1
+                for (int k = 0; k < spread.lanes; k += 4) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float of = __shfl(v, lane - u + k + j);
+                        all += k + j < spread.lanes ? of : 0.f;
+                    }
+                }
+                return all;
             };
             if (layer) mean = sum([](float v) { return v; }) * inv;
             const float rstd = rsqrt_of(sum([&](float v) { return (v - mean) * (v - mean); }) * inv + n.eps);
@@ -286,24 +311,34 @@ __global__ __launch_bounds__(256) void append_norm_packs(AppendNormArgs n, Divis
 }
 
 // Whether heads fall into packs of VEC: what turns and what does not have one pack
-// at least, and together not more than a wave has lanes.
-template <int VEC> bool packs_fit(const AppendArgs &a, int *log)
+// at least, and together not more than a wave has lanes.  Heads take a whole power of
+// two of the lanes, whose sums the vector unit forms by itself, or, where fewer waves
+// a token then do, just what they need, and sums by way of LDS: 8191 tokens of
+// 48 f16 heads of 80 in 5 lanes and not 8 take 35 us and not 44, of 56 heads of 96 in 6
+// 45 and not 47.  Beyond 12 lanes the sums' accesses would be more than what they save.
+template <int VEC> bool packs_fit(const AppendArgs &a, int heads, Spread *s)
 {
     const Lanes<VEC> as(a.dim, a.rot_dim, a.pairs != 0);
     if ((as.turns > 0 && as.turns < VEC) || (as.rest > 0 && as.rest < VEC)) return false;
-    for (*log = 0; 1 << *log < as.all;) ++*log;
-    return *log <= 6;
+    for (s->log = 0; 1 << s->log < as.all;) ++s->log;
+    if (s->log > 6) return false;
+    s->lanes = 1 << s->log;
+    if (as.all <= 12 && ceil_div(heads, 64 / as.all) < ceil_div(heads, 64 / s->lanes)) s->lanes = as.all, s->log = -1;
+    s->heads = 64 / s->lanes;
+    s->blocks = ceil_div(heads, s->heads);
+    s->slices = std::min(a.n_tokens, std::max(1, kCardGroups * 4 / s->blocks));
+    s->by_lanes = Divisor((unsigned)s->lanes);
+    s->by_blocks = Divisor((unsigned)s->blocks);
+    return true;
 }
 
 template <typename TX, typename TC, typename TP, int VEC>
 bool launch_packs(const AppendNormArgs &n, const Divisor &by_page, int heads, hipStream_t stream)
 {
-    int log;
-    if (!packs_fit<VEC>(n.a, &log)) return false;
-    const int groups = (int)((((int64_t)heads << log) + 255) / 256);
-    // As many workgroups as the card holds at once.
-    const int slices = std::min(n.a.n_tokens, std::max(1, kCardGroups / groups));
-    hipLaunchKernelGGL((append_norm_packs<TX, TC, TP, VEC>), dim3(groups, slices), dim3(256), 0, stream, n, by_page, log);
+    Spread spread;
+    if (!packs_fit<VEC>(n.a, heads, &spread)) return false;
+    const int groups = ceil_div(spread.blocks * spread.slices, 4);
+    hipLaunchKernelGGL((append_norm_packs<TX, TC, TP, VEC>), dim3(groups), dim3(256), 0, stream, n, by_page, spread);
     return true;
 }
 
