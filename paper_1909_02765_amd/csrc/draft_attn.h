@@ -102,9 +102,14 @@ template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS> struct TreeKer
     static constexpr float SLACK = __is_same(TC, _Float16) ? 4.f : 8.f;
     static constexpr float UP = __is_same(TC, _Float16) ? 0x1p11f : 1.f;
     static constexpr int WB = RS ? 4 : MA;  // blocks of rows of a workgroup
+    // Whether a wave that takes rows keeps the first of their three query parts in registers: less to read, and of LDS
+    // to hold (192 units of 189 rows of f32 over 130 bf16 keys, heads of 128 38.5 -> 32.5 us, of 192 62 -> 52; of 80 the
+    // same, of 256 no room.  Queries in one part gain nothing by it, and lose up to a third where they take many registers).
+    static constexpr bool KEEP = RS && Base::QP == 3 && DC >= 128 && DC <= 192;
     // Workgroups that a compute unit holds at once.
     static constexpr int PER_CU = R == kAny ? (DC >= 192 ? 1 : 2)
                                   : sizeof(TC) == 4 ? (DC >= 192 ? 1 : DC == 64 && MA == 1 ? 3 : 2)
+                                  : KEEP && DC == 128 ? 3
                                   : MA == 1 ? (DC == 64 ? 4 : DC == 96 ? 3 : 2) : MA == 2 ? (DC == 64 ? 3 : DC <= 128 ? 2 : 1) : 2;
 };
 
@@ -124,7 +129,7 @@ template <typename Cfg, int MA, bool RS> struct TreeLds {
     float m[RS ? 1 : 4][16 * MA], l[RS ? 1 : 4][16 * MA];
     union {
         // The queries, as the lanes of the first product take them, in parts those of 32 bits.
-        Words16 q[Cfg::QP][Cfg::NK][WB][64];
+        Words16 q[Cfg::KEEP ? 2 : Cfg::QP][Cfg::NK][WB][64];
         // What each wave gives to another of its outputs, as they lie in registers.
         floatx4 give[RS ? 1 : Cfg::GIVE][RS ? 1 : 4][RS ? 1 : MA * Cfg::NO / 4][64];
     };
@@ -165,19 +170,19 @@ template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS> struct TreeRow
         }
     }
 
-    // Rows' bits and lows, and the queries in their layout, into LDS.
-    template <typename Lds> __device__ __forceinline__ void store(TreeArgsAt args, const TreeSegment &seg, int lane, int wave, Lds &lds)
+    // Rows' bits and lows, and the queries in their layout, into LDS or `kept`.
+    template <typename Lds> __device__ __forceinline__ void store(TreeArgsAt args, const TreeSegment &seg, int lane, int wave, Lds &lds, Words16 *kept)
     {
         const TreeArgs &t = args_of(args);
         const AttnArgs &a = t.a;
-        const int ma = wave % WB, c0 = wave / WB;
+        const int ma = wave % WB, c0 = RS ? 0 : wave / WB;
         for (int i = threadIdx.x; i < 16 * WB * 16; i += 256) lds.odd[i / 16][i % 16] = 0;
         if (threadIdx.x == 0) lds.any_odd = 0;
         if constexpr (QP == 1) {
 #pragma unroll
             for (int i = 0; i < MINE; ++i) lds.q[0][min(c0 + i * STEP, NK - 1)][ma][lane] = q[i];
         } else {
-            split(t, lane, ma, c0, lds);
+            split(t, lane, ma, c0, lds, kept);
         }
         if (wave != 0) return;
         unsigned long long bits = seen_nodes(parent, lane, t.n_nodes);
@@ -206,7 +211,7 @@ template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS> struct TreeRow
     }
 
     // Queries of 32 bits in three parts (see decode_attn.h).
-    template <typename Lds> __device__ __forceinline__ void split(const TreeArgs &t, int lane, int ma, int c0, Lds &lds)
+    template <typename Lds> __device__ __forceinline__ void split(const TreeArgs &t, int lane, int ma, int c0, Lds &lds, Words16 *kept)
     {
         const int n16 = lane & 15, g = lane >> 4, dim = t.a.dim;
         struct Values {
@@ -237,7 +242,8 @@ template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS> struct TreeRow
             back = __builtin_ldexpf(1.f, -by);
         }
         if (c0 == 0 && g == 0) lds.unscale[ma * 16 + n16] = back;
-#pragma unroll 2
+        constexpr int ROLL = Cfg::KEEP ? NK : 2;
+#pragma unroll ROLL
         for (int c = c0; c < NK; c += STEP) {
             const Values p = get(c);
             Pack<TC, KV> part[3];
@@ -256,7 +262,11 @@ template <typename TC, bool Q16, int DC, Rows R, int MA, bool RS> struct TreeRow
                 part[2].v[i] = (TC)(v - (float)part[1].v[i]);
             }
 #pragma unroll
-            for (int n = 0; n < 3; ++n) lds.q[n][c][ma][lane] = __builtin_bit_cast(Words16, part[n]);
+            for (int n = 0; n < 3; ++n) {
+                const Words16 w = __builtin_bit_cast(Words16, part[n]);
+                if (Cfg::KEEP && n == 0) kept[Cfg::KEEP ? c : 0] = w;
+                else lds.q[Cfg::KEEP ? n - 1 : n][c][ma][lane] = w;
+            }
         }
     }
 };
@@ -475,7 +485,8 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         load_k(0);
         load_v(0);
     }
-    rows.store(args, seg, lane, wave, lds);
+    Words16 kept[Cfg::KEEP ? NK : 1];
+    rows.store(args, seg, lane, wave, lds, kept);
     __syncthreads();
 
     floatx4 o[MA][NO];
@@ -552,6 +563,9 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         floatx4 s[MA];
         int ql = lane;
         asm volatile("" : "+v"(ql));  // (read for each tile, not kept)
+        auto query = [&](int n, int c, int ma) {
+            return Cfg::KEEP && n == 0 ? kept[Cfg::KEEP ? c : 0] : lds.q[Cfg::KEEP ? n - 1 : n][c][block(ma)][ql];
+        };
 #pragma unroll
         for (int ma = 0; ma < MA; ++ma) {
             floatx4 x = {0.f, 0.f, 0.f, 0.f};
@@ -566,10 +580,10 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
                 floatx4 low = x;
 #pragma unroll
                 for (int c = 0; c < NK; ++c) {
-                    x = mfma_scores<TC>(kt[c], lds.q[0][c][block(ma)][ql], x);
+                    x = mfma_scores<TC>(kt[c], query(0, c, ma), x);
                     if constexpr (QP == 3) {
-                        low = mfma_scores<TC>(kt[c], lds.q[1][c][block(ma)][ql], low);
-                        low = mfma_scores<TC>(kt[c], lds.q[2][c][block(ma)][ql], low);
+                        low = mfma_scores<TC>(kt[c], query(1, c, ma), low);
+                        low = mfma_scores<TC>(kt[c], query(2, c, ma), low);
                     }
                 }
                 if constexpr (QP == 3) {
