@@ -396,6 +396,7 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
     constexpr int QP = Cfg::QP, PP = Cfg::PP;
     constexpr bool C16 = Cfg::C16;
+    constexpr int AHEAD = C16 ? 4 : 2;  // query operands that are read before the one in use
 
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
@@ -567,31 +568,36 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
             return Cfg::KEEP && n == 0 ? kept[Cfg::KEEP ? c : 0] : lds.q[Cfg::KEEP ? n - 1 : n][c][block(ma)][ql];
         };
 #pragma unroll
-        for (int ma = 0; ma < MA; ++ma) {
-            floatx4 x = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (!C16) {
+        for (int ma = 0; ma < MA; ++ma) s[ma] = floatx4{0.f, 0.f, 0.f, 0.f};
+        floatx4 low[MA];
 #pragma unroll
-                for (int c = 0; c < NK; ++c) {
-                    const floatx4 q = __builtin_bit_cast(floatx4, lds.q[0][c][block(ma)][ql]);
+        for (int ma = 0; ma < MA; ++ma) low[ma] = s[ma];
+        // (Reads ahead, held in their places: the compiler, short of registers, waits for each.  8 trees of 1024 rows of f32
+        // over up to 2049 bf16 keys of 256 73 -> 56 us, 64 such rows of 128 over 131071 keys 151 -> 136; as fast with 2,
+        // 6 or, where registers last, 10 ahead of 4.)
+        constexpr int ALL = NK * QP * MA;
+        Words16 got[AHEAD + 1];
+        auto read = [&](int i) { got[i % (AHEAD + 1)] = query(i / MA % QP, i / (MA * QP), i % MA); };
 #pragma unroll
-                    for (int i = 0; i < KV; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, kt[c])[i], q[i], x, 0, 0, 0);
-                }
+        for (int i = 0; i < AHEAD; ++i) read(i);
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) {
+            if (i + AHEAD < ALL) read(i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+            floatx4 &x = i / MA % QP == 0 ? s[i % MA] : low[i % MA];
+            const Words16 k = kt[i / (MA * QP)], q = got[i % (AHEAD + 1)];
+            if constexpr (C16) {
+                x = mfma_scores<TC>(k, q, x);
             } else {
-                floatx4 low = x;
 #pragma unroll
-                for (int c = 0; c < NK; ++c) {
-                    x = mfma_scores<TC>(kt[c], query(0, c, ma), x);
-                    if constexpr (QP == 3) {
-                        low = mfma_scores<TC>(kt[c], query(1, c, ma), low);
-                        low = mfma_scores<TC>(kt[c], query(2, c, ma), low);
-                    }
-                }
-                if constexpr (QP == 3) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] += low[r] - low[r] == 0.f ? low[r] : 0.f;
-                }
+                for (int e = 0; e < KV; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, k)[e], __builtin_bit_cast(floatx4, q)[e], x, 0, 0, 0);
             }
-            s[ma] = x;
+        }
+        if constexpr (QP == 3) {
+#pragma unroll
+            for (int ma = 0; ma < MA; ++ma)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[ma][r] += low[ma][r] - low[ma][r] == 0.f ? low[ma][r] : 0.f;
         }
         load_k(j + 1);
 
