@@ -541,8 +541,10 @@ size_t ends_bytes(int n_seqs) { return ((size_t)n_seqs * sizeof(VerifyEnd) + 15)
 
 }  // namespace
 
-// Rows of up to 128 KB are one kernel's work, a workgroup a sequence; longer ones are
-// summed in chunks by many.
+// Rows of up to 128 KB are one kernel's work, a workgroup a sequence, bounded by a chain
+// of accesses (12 us for one row of 32000 f32 values); longer ones are summed in chunks by
+// many (64 rows of 131072 values, 34 MB, 17.6 us, half of it in the second kernel, which finds
+// the chunk and the token).
 size_t verify_plan(VerifyArgs *a)
 {
     const int most = a->v.dtype == ILPM_F32 ? kShortVocab<float> : kShortVocab<__bf16>;
