@@ -405,7 +405,7 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     constexpr int KV = Cfg::KV, NK = Cfg::NK, VV = Cfg::VV, NV = Cfg::NV, NO = Cfg::NO;
     constexpr int QP = Cfg::QP, PP = Cfg::PP;
     constexpr bool C16 = Cfg::C16;
-    constexpr int AHEAD = C16 ? 4 : 2;  // query operands that are read before the one in use
+    constexpr int AHEAD = std::min(C16 ? 4 : 2, NK * QP * MA);  // query operands that are read before the one in use
 
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
