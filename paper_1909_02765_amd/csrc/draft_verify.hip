@@ -30,11 +30,44 @@ __device__ inline double left_of(double a, double b, float p, float q)
 // What is the same in all lanes, as the compiler cannot know of values from LDS.
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// A value's two words, each moved as the vector unit can: sums over a wave lie in every
+// chain here, and by way of LDS cost 2 of 12 us for a row of 32000 values, of 17.6 for 64 of
+// 131072.
+template <typename F> __device__ inline double by_words(double v, F f)
+{
+    const unsigned long long x = __builtin_bit_cast(unsigned long long, v);
+    return __builtin_bit_cast(double, (unsigned long long)f((unsigned)(x >> 32)) << 32 | f((unsigned)x));
+}
+// (Where the other lane would lie in another sixteen, 0.)
+template <int CTRL> __device__ inline double dpp(double v)
+{
+    return by_words(v, [](unsigned w) { return (unsigned)__builtin_amdgcn_mov_dpp((int)w, CTRL, 0xf, 0xf, true); });
+}
+__device__ inline double of_lane(double v, int lane)
+{
+    return by_words(v, [=](unsigned w) { return (unsigned)__builtin_amdgcn_readlane((int)w, lane); });
+}
+
+// (Once the lanes of a four or eight hold the same, a mirror is as good a partner as any.)
 __device__ inline double sum_wave(double v)
 {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    v += dpp<0xb1>(v);   // of pairs
+    v += dpp<0x4e>(v);   // of fours
+    v += dpp<0x141>(v);  // eight mirrored
+    v += dpp<0x140>(v);  // sixteen mirrored
+    return (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
+}
+
+// The sum of a lane's value and those of all lanes before it.
+__device__ inline double sum_up_to(double v)
+{
+    v += dpp<0x111>(v);  // of the lane 1 before it in its sixteen, then 2, 4 and 8
+    v += dpp<0x112>(v);
+    v += dpp<0x114>(v);
+    v += dpp<0x118>(v);
+    const double a = of_lane(v, 15), b = a + of_lane(v, 31), c = b + of_lane(v, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    return v + (row == 0 ? 0. : row == 1 ? a : row == 2 ? b : c);
 }
 
 // The sum over the workgroup, in all threads.
@@ -254,17 +287,11 @@ template <typename T, bool DRAFT> __device__ __forceinline__ Rest<T, DRAFT> rest
 // it passes `want`, else the last above 0 (-1: none); *before: the sum before it.
 __device__ inline int pick_lane(double own, double want, double *before)
 {
-    const int lane = threadIdx.x & 63;
-    double up_to = own;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(up_to, d);
-        if (lane >= d) up_to += o;
-    }
+    const double up_to = sum_up_to(own);
     const unsigned long long passed = __builtin_amdgcn_ballot_w64(own > 0. && up_to > want);
     const unsigned long long some = __builtin_amdgcn_ballot_w64(own > 0.);
     const int at = passed ? __builtin_ctzll(passed) : some ? 63 - __builtin_clzll(some) : -1;
-    *before = __shfl(up_to - own, max(at, 0));
+    *before = of_lane(up_to - own, max(at, 0));
     return at;
 }
 
@@ -309,7 +336,7 @@ template <typename T, bool DRAFT> __global__ __launch_bounds__(kShortThreads) vo
     }
     auto piece = [&](int k) { return (int64_t)(k * kShortThreads + tid) * VEC; };
     // What is left of the row, or, where that is nothing, the row itself.  (In loops: most of the instructions run
-    // once or twice, and cost their fetching.  With the rounds unrolled this took 30 us for 32000 values, now 12.)
+    // once or twice, and cost their fetching.  With the rounds unrolled this took 30 us for 32000 values, in loops 12, and now 10.)
     const int rounds = (v.vocab + kShortThreads * VEC - 1) / (kShortThreads * VEC);
     double own[2], total = 0.;
     bool whole = false;
@@ -542,8 +569,8 @@ size_t ends_bytes(int n_seqs) { return ((size_t)n_seqs * sizeof(VerifyEnd) + 15)
 }  // namespace
 
 // Rows of up to 128 KB are one kernel's work, a workgroup a sequence, bounded by a chain
-// of accesses (12 us for one row of 32000 f32 values); longer ones are summed in chunks by
-// many (64 rows of 131072 values, 34 MB, 17.6 us, half of it in the second kernel, which finds
+// of accesses (10 us for one row of 32000 f32 values); longer ones are summed in chunks by
+// many (64 rows of 131072 values, 34 MB, 16 us, 7 of it in the second kernel, which finds
 // the chunk and the token).
 size_t verify_plan(VerifyArgs *a)
 {
