@@ -690,7 +690,7 @@ int ilpm_attn_tree_workspace_size(const ilpm_kv_cache *cache, int q_heads, int n
  * the smallest v with w(0) + ... + w(v) > uniforms[s][0] (w(0) + w(1) + ...),
  * or the last one with w(v) > 0 where there is none; over p in the place of w
  * where w is 0 everywhere, and -1 where p is as well.
- * Sums are held in 64 bits.  A probability that is not above 0 (NaN among them)
+ * uniforms[s][0] below 0 counts as 0.  Sums are held in 64 bits.  A probability that is not above 0 (NaN among them)
  * counts as 0, one above the largest fp32 number as that.  A child whose token is
  * outside [0, vocab) is not kept and changes nothing.
  *   tokens, parents  int32 [n_seqs][n_nodes], contiguous, n_nodes in [1, ILPM_MAX_NODES]

@@ -283,6 +283,14 @@ template <typename T, bool DRAFT> __device__ __forceinline__ Rest<T, DRAFT> rest
                           DRAFT ? row_of<T>(v.draft, v.draft_seq_stride, v.draft_node_stride, seq, node) : nullptr, a, b, v.vocab, nullptr, 0};
 }
 
+// How much of `total` lies before the next token.  (A number below 0 counts as 0: the
+// searches end where they have passed what is wanted, and must have found a place by then.)
+__device__ inline double wanted(const ilpm_verify_args &v, int seq, double total)
+{
+    const float u = v.uniforms[(int64_t)seq * v.n_nodes];
+    return (double)(u < 0.f ? 0.f : u) * total;
+}
+
 // Of 64 lanes' values in their order the first at which the sum with all before
 // it passes `want`, else the last above 0 (-1: none); *before: the sum before it.
 __device__ inline int pick_lane(double own, double want, double *before)
@@ -364,7 +372,7 @@ template <typename T, bool DRAFT> __global__ __launch_bounds__(kShortThreads) vo
         if (tid == 0) v.next_tokens[seq] = -1;
         return;
     }
-    double want = (double)v.uniforms[(int64_t)seq * v.n_nodes] * total, before;
+    double want = wanted(v, seq, total), before;
     // The wave and round that hold it: among the first 64, or the others where there are any.
     int at = -1;
 #pragma unroll 1
@@ -505,7 +513,7 @@ template <typename T, bool DRAFT> __global__ __launch_bounds__(kThreads) void ve
         if (tid == 0) v.next_tokens[seq] = -1;
         return;
     }
-    double want = (double)v.uniforms[(int64_t)seq * v.n_nodes] * total, before = 0., rest = 0.;
+    double want = wanted(v, seq, total), before = 0., rest = 0.;
     int chunk = 0;
     for (int c0 = 0; c0 < a.chunks; c0 += 64) {
         const double own = c0 + lane < a.chunks ? sums[c0 + lane] : 0.;

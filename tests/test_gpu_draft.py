@@ -538,6 +538,18 @@ def test_verify_odd_probabilities():
         check_verify(c, f"odd probabilities, draft {draft}")
 
 
+@pytest.mark.parametrize("dtype,vocab,zeros", [(F32, 32768, 20000), (BF16, 65536, 40000), (F32, 300000, 270000), (F16, 300000, 262145)], ids=str)
+@pytest.mark.parametrize("draft", [False, True])
+def test_verify_numbers_below_zero_over_rows_that_begin_with_zeros(dtype, vocab, zeros, draft):
+    """The next token of a number below 0 is the first that has a probability, however far from the row's beginning."""
+    c = verify_case(gen(11), 4, 2, vocab, dtype, draft, std=1.0)
+    c["target"][:, :, :zeros] = 0.0
+    c["target"][:, :, zeros + 7] = 0.5   # (in every row above 0)
+    c["uniforms"][:, 0] = torch.tensor([-1.0, -math.inf, -1e-30, 0.0])
+    c["uniforms"][:, 1] = 2.0            # (the child is refused, except where that passes)
+    check_verify(c, f"numbers below 0, {vocab} {dtype} draft {draft}")
+
+
 def test_verify_strided_and_given_outputs():
     ilpm = lib()
     g = gen(10)
