@@ -512,6 +512,17 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
     const float cap2 = softcap * kLog2e;
     const int top_low = uniform(lds.top_low);
     constexpr bool UNSCALE = QP == 3 && __is_same(TC, _Float16);  // (parts of bf16 need none)
+    // With a cap, or a scale that is not above 0, scores are scaled before their maximum is taken; and where a row's
+    // scale is 0 or infinite only together with that of its parts (queries near either end of a float): such a product
+    // of a score that is 0, or of -infinity for a key that is not seen, would be NaN.
+    bool apart = softcap > 0.f || !(scale2 > 0.f);
+    if constexpr (UNSCALE) {
+#pragma unroll
+        for (int ma = 0; ma < MA; ++ma) {
+            const float by = scale2 * lds.unscale[block(ma) * 16 + n16];
+            apart = apart || __builtin_amdgcn_ballot_w64(!(by > 0.f && by < INFINITY)) != 0;
+        }
+    }
 
     // Value i of piece c of a lane's four rows, put together from their 16-bit halves.
     auto values = [&](int c, int i) {
@@ -610,16 +621,17 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         }
         load_k(j + 1);
 
-        // Scores times `by` are logarithms to the base 2; with a cap, or a scale that is not above 0, they are first made so.
+        // Scores times `by` are logarithms to the base 2; where that product would not do, they are first made so.
         float by[MA];
 #pragma unroll
         for (int ma = 0; ma < MA; ++ma) by[ma] = UNSCALE ? scale2 * lds.unscale[block(ma) * 16 + n16] : scale2;
-        if (softcap > 0.f || !(scale2 > 0.f)) {
+        if (apart) {
 #pragma unroll
             for (int ma = 0; ma < MA; ++ma) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    s[ma][r] *= by[ma];
+                    if constexpr (UNSCALE) s[ma][r] *= lds.unscale[block(ma) * 16 + n16];
+                    s[ma][r] *= scale2;
                     if (softcap > 0.f) s[ma][r] = cap2 * tanh_of(s[ma][r]);
                 }
                 by[ma] = 1.f;

@@ -325,6 +325,21 @@ def test_attention_large_scores(x, cache):
     check_attn(c, "large scores", scale=20.0)
 
 
+@pytest.mark.parametrize("x,cache", PAIRS, ids=str)
+@pytest.mark.parametrize("softcap", [0.0, 10.0])
+@pytest.mark.parametrize("hq,nodes", [(4, 14), (10, 14)])
+def test_attention_scales_at_the_ends_of_a_float(x, cache, softcap, hq, nodes):
+    """Queries and scales so small that their product is none, and so large, over keys of 0, that it is infinite: scores of 0."""
+    g = gen(14)
+    c = attn_case(g, [20], [some_tree(g, nodes)], hq, 1, 64, x, cache, 16)
+    c["q"] = randn(g, c["q"].shape, F32, 2.0 ** -119).to(x)
+    hide_unseen(c)
+    check_attn(c, "small queries and scale", scale=2.0 ** -30, softcap=softcap)
+    c["q"] = randn(g, c["q"].shape, F32, 2.0 ** 120).clamp(-65504.0, 65504.0).to(x) if x == F16 else randn(g, c["q"].shape, F32, 2.0 ** 120).to(x)
+    c["kp"] = torch.where(torch.isnan(c["kp"]), c["kp"], torch.zeros((), dtype=cache))
+    check_attn(c, "large queries and scale over keys of 0", scale=2.0 ** 30, softcap=softcap)
+
+
 def test_attention_pages_that_are_none():
     g = gen(6)
     c = attn_case(g, [100, 50, 64], [some_tree(g, 10) for _ in range(3)], 4, 2, 64, BF16, BF16, 16)
