@@ -545,7 +545,7 @@ PyObject *verify_drafts_workspace_size(PyObject *, PyObject *const *args, Py_ssi
 }
 
 // (k_pages, v_pages, src_table, dst_table, src_start, dst_start, counts, path, max_count) -> None; max_count None: as many
-// as the path has, or the tables can name
+// as the path has, or any number
 PyObject *kv_copy(PyObject *, PyObject *const *args, Py_ssize_t n_args)
 {
     HANDLE_TH_ERRORS
@@ -562,8 +562,7 @@ PyObject *kv_copy(PyObject *, PyObject *const *args, Py_ssize_t n_args)
         return p;
     };
     const int32_t *src = row(args[4], "src_start"), *dst = row(args[5], "dst_start"), *counts = row(args[6], "counts"), *path = nullptr;
-    const int64_t most = (int64_t)std::min(c.max_pages, wide) * c.page_size;
-    int64_t path_stride = 0, max_count = std::min<int64_t>(most, INT_MAX);
+    int64_t path_stride = 0, max_count = INT_MAX;
     if (given(args[7])) {
         const at::Tensor &t = tensor(args[7], "path");
         path = ints_of(t, "path", 2);

@@ -97,8 +97,12 @@ template <int P> __global__ __launch_bounds__(256) void copy_rows(CopyArgs a)
 {
     __shared__ Place places[kTokens];
     const int seq = blockIdx.y, tid = threadIdx.x, per_head = a.row_bytes / P, per = a.kv_heads * per_head;
-    const int count = min(a.counts[seq], a.max_count);
-    for (int64_t first = (int64_t)blockIdx.x * kTokens; first < count; first += (int64_t)gridDim.x * kTokens) {
+    // Tokens that have places in both tables: no more than the grid was made for, whatever counts and starts are.
+    const int64_t from = a.src_start[seq], to = a.dst_start[seq];
+    const int64_t begin = max((int64_t)0, -min(from, to));
+    const int64_t end = min((int64_t)min(a.counts[seq], a.max_count),
+                            min((int64_t)a.src_max_pages * a.page_size - from, (int64_t)a.dst_max_pages * a.page_size - to));
+    for (int64_t first = begin + (int64_t)blockIdx.x * kTokens; first < end; first += (int64_t)gridDim.x * kTokens) {
         if (tid < kTokens) places[tid] = place_of(a, move_of(a, seq, first + tid));
         __syncthreads();
         for (int i0 = tid; i0 < 2 * per; i0 += 256) {
@@ -125,7 +129,8 @@ template <int P> hipError_t launch(const CopyArgs &a, hipStream_t stream)
 {
     if (!a.path) {
         // (A workgroup for every kTokens that there may be: those beyond the counts end at once.)
-        const int64_t groups = std::min<int64_t>(((int64_t)a.max_count + kTokens - 1) / kTokens, 1 << 16);
+        const int64_t most = std::min<int64_t>(a.max_count, (int64_t)std::min(a.src_max_pages, a.dst_max_pages) * a.page_size);
+        const int64_t groups = std::min<int64_t>((most + kTokens - 1) / kTokens, 1 << 16);
         hipLaunchKernelGGL((copy_rows<P>), dim3((unsigned)groups, a.n_seqs), dim3(256), 0, stream, a);
         return hipGetLastError();
     }

@@ -643,6 +643,19 @@ def test_copy_leaves_out_what_names_no_place():
     check_copy(c, starts, [0, 0, 0, 0, 2 ** 31 - 1, 60], [10] * 6, path, "no place on a path")
 
 
+def test_copy_from_before_the_beginning():
+    """Starts below 0: what lies before the beginning is left out, and all tokens that have places are copied, however many
+    do not."""
+    g = gen(5)
+    c = copy_case(g, 6, 4, 16, 2, 64, BF16)
+    src = [-10, -10, -100, -1, -2 ** 31, 3]
+    dst = [-10, -3, -70, -64, -2 ** 31, -5]
+    check_copy(c, src, dst, [80, 200, 2 ** 31 - 1, 128, 2 ** 31 - 1, 70], None, "before the beginning")
+    check_copy(c, src, dst, [80, 200, 100, 128, 0, 70], None, "before the beginning, bounded", max_count=75)
+    path = torch.randint(0, 64, (6, 40), generator=g).to(torch.int32)
+    check_copy(c, src, dst, [40] * 6, path, "before the beginning on a path")
+
+
 def test_copy_a_beam_from_one_row():
     """Rows that share their source, and tables of different widths."""
     g = gen(4)
