@@ -741,6 +741,10 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         const int r = wave * 16 + n16;
         if (row_in_unit(seg, 16 * WB, r) >= args_of(args).rows) return;
         const bool real = lds.bits[r] != 0;  // (what is no node has seen keys of the sequence, and none counts)
+        // (Only this wave marked its rows, each lane for others.)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         unsigned odd[4] = {0, 0, 0, 0};
         if (lds.any_odd) {
 #pragma unroll
