@@ -22,9 +22,11 @@ template <typename T> __device__ inline float prob(T v)
     return fminf(fmaxf((float)v, 0.f), 3.402823466e38f);  // (of a NaN and a number the number)
 }
 
+// (Rounded in the same places wherever it is formed: what a sum found above 0 the search in
+// it must find above 0 again.)
 __device__ inline double left_of(double a, double b, float p, float q)
 {
-    return fmax(a * (double)p - b * (double)q, 0.);
+    return fmax(__builtin_fma(a, (double)p, -(b * (double)q)), 0.);
 }
 
 // What is the same in all lanes, as the compiler cannot know of values from LDS.
