@@ -620,8 +620,9 @@ typedef struct ilpm_append_options {
  * Tokens are left out as ilpm_kv_append leaves them out, their place in the
  * cache by slots[t]; a query is normed wherever its key goes, and is rotated
  * where its position is in [0, n_positions).  q_out may be q itself (same data and strides).
- * head_dim is at most 1024 (ILPM_ERR_UNSUPPORTED above, and for element types
- * other than ilpm_kv_append's).
+ * head_dim is at most 1024, n_tokens 2^24 - 1, and n_tokens times the heads of
+ * queries, keys and values 2^26 - 4 (ILPM_ERR_UNSUPPORTED above, and for element
+ * types other than ilpm_kv_append's).
  */
 int ilpm_kv_append_norm(const ilpm_kv_cache *cache, const ilpm_heads *k, const ilpm_heads *v, const ilpm_heads *q,
                         const ilpm_heads *q_out, const ilpm_append_options *options, int n_tokens, hipStream_t stream);
@@ -662,7 +663,8 @@ typedef struct ilpm_tree_options {
  * fp32 ones, over f16 to 2^-23, or by up to 2^-35 of the largest where that is more.
  * An infinite v_j that is seen gives infinity or NaN.  Of fp32 queries over f16 what
  * is below 2^-39 of a row's largest value is lost.
- * head_dim is at most 256 (ILPM_ERR_UNSUPPORTED above).
+ * head_dim is at most 256, and n_seqs * n_nodes * q_heads 2^24 - 1
+ * (ILPM_ERR_UNSUPPORTED above).
  * The workspace is as ilpm_attn_decode's, of ilpm_attn_tree_workspace_size bytes.
  */
 int ilpm_attn_tree(const ilpm_kv_cache *cache, const ilpm_heads *q, const int32_t *lengths, const int32_t *parents,
@@ -701,6 +703,7 @@ int ilpm_attn_tree_workspace_size(const ilpm_kv_cache *cache, int q_heads, int n
  *   counts  int32 [n_seqs]: how many they are;  next_tokens  int32 [n_seqs]
  * A sequence whose parents[s][0] is not -1 has no tree: its path is all -1, its
  * count 0 and its next token -1.
+ * n_seqs is at most 65535 and vocab 2^30 (ILPM_ERR_UNSUPPORTED above).
  * The workspace is as ilpm_attn_decode's, of ilpm_verify_drafts_workspace_size bytes.
  */
 typedef struct ilpm_verify_args {
@@ -732,6 +735,8 @@ int ilpm_verify_drafts_workspace_size(int n_seqs, int n_nodes, int vocab, size_t
  * Of two rows neither may write what the other reads or writes, except the same
  * values onto themselves.  A token that is outside its table, or in no page of the
  * pool, is neither read nor written; counts below 0 are taken as 0.
+ *   n_seqs is at most 65535 and kv_heads * head_dim 2^26 (ILPM_ERR_UNSUPPORTED
+ * above).
  *   dst_table  int32 [n_seqs][dst_max_pages], rows dst_table_stride apart (0: the same pages)
  *   src_start, dst_start, counts  int32 [n_seqs]
  */
