@@ -719,7 +719,7 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
                         const float v = __builtin_bit_cast(floatx4, vt[r][c])[i];
 #pragma unroll
                         for (int ma = 0; ma < MA; ++ma) {
-                                            o[ma][c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __builtin_bit_cast(float, part[ma][r]), o[ma][c * VV + i], 0, 0, 0);
+                            o[ma][c * VV + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __builtin_bit_cast(float, part[ma][r]), o[ma][c * VV + i], 0, 0, 0);
                         }
                     }
         } else {

@@ -92,7 +92,8 @@ template <int P, int N> __global__ __launch_bounds__(256) void copy_path(CopyArg
 constexpr int kTokens = 16;  // of a workgroup at a time
 
 // Without one: a thread takes one piece of kTokens tokens, and reads them all before
-// it writes the first, so that as many accesses are on their way.
+// it writes the first, so that as many reads are on their way.  (Stores are not: each is
+// behind a condition, and waits for the one before it.)
 template <int P> __global__ __launch_bounds__(256) void copy_rows(CopyArgs a)
 {
     __shared__ Place places[kTokens];
@@ -137,8 +138,8 @@ template <int P> hipError_t launch(const CopyArgs &a, hipStream_t stream)
     const dim3 grid((unsigned)((2ll * a.kv_heads * (a.row_bytes / P) + 255) / 256), a.n_seqs);
     if (a.max_count <= 8) hipLaunchKernelGGL((copy_path<P, 8>), grid, dim3(256), 0, stream, a);
     else if (a.max_count <= 16) hipLaunchKernelGGL((copy_path<P, 16>), grid, dim3(256), 0, stream, a);
-    else if (a.max_count <= 32) hipLaunchKernelGGL((copy_path<P, 32>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((copy_path<P, 64>), grid, dim3(256), 0, stream, a);
+    else if (P == 16 || a.max_count <= 32) hipLaunchKernelGGL((copy_path<P, 32>), grid, dim3(256), 0, stream, a);
+    else if constexpr (P < 16) hipLaunchKernelGGL((copy_path<P, 64>), grid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
