@@ -28,16 +28,22 @@ struct Move {
     int64_t from, to;
 };
 
-__device__ inline Move move_of(const CopyArgs &a, int seq, int64_t i)
+__device__ inline Move move_of(const CopyArgs &a, int seq, int64_t from, int64_t to)
 {
-    Move m = {-1, -1};
-    if (i >= min(a.counts[seq], a.max_count)) return m;
-    const int64_t step = a.path ? a.path[(int64_t)seq * a.path_stride + i] : i;
-    if (step < 0) return m;
-    m.from = slot_of(a, a.src_table, a.src_table_stride, a.src_max_pages, seq, (int64_t)a.src_start[seq] + step);
-    m.to = slot_of(a, a.dst_table, a.dst_table_stride, a.dst_max_pages, seq, (int64_t)a.dst_start[seq] + i);
+    Move m;
+    m.from = slot_of(a, a.src_table, a.src_table_stride, a.src_max_pages, seq, from);
+    m.to = slot_of(a, a.dst_table, a.dst_table_stride, a.dst_max_pages, seq, to);
     if (m.from < 0 || m.to < 0 || m.from == m.to) m.from = m.to = -1;
     return m;
+}
+
+// Of token i of a path.
+__device__ inline Move move_of_path(const CopyArgs &a, int seq, int i)
+{
+    if (i >= min(a.counts[seq], a.max_count)) return Move{-1, -1};
+    const int step = a.path[(int64_t)seq * a.path_stride + i];
+    if (step < 0) return Move{-1, -1};
+    return move_of(a, seq, (int64_t)a.src_start[seq] + step, (int64_t)a.dst_start[seq] + i);
 }
 
 // The byte offset in a pool of a slot over all pages.
@@ -67,7 +73,7 @@ template <int P, int N> __global__ __launch_bounds__(256) void copy_path(CopyArg
 {
     __shared__ Place places[N];
     const int seq = blockIdx.y, tid = threadIdx.x;
-    if (tid < N) places[tid] = place_of(a, move_of(a, seq, tid));
+    if (tid < N) places[tid] = place_of(a, move_of_path(a, seq, tid));
     __syncthreads();
     const int per_head = a.row_bytes / P, per = a.kv_heads * per_head;
     int i = (int)(blockIdx.x * 256 + tid);
@@ -104,7 +110,7 @@ template <int P> __global__ __launch_bounds__(256) void copy_rows(CopyArgs a)
     const int64_t end = min((int64_t)min(a.counts[seq], a.max_count),
                             min((int64_t)a.src_max_pages * a.page_size - from, (int64_t)a.dst_max_pages * a.page_size - to));
     for (int64_t first = begin + (int64_t)blockIdx.x * kTokens; first < end; first += (int64_t)gridDim.x * kTokens) {
-        if (tid < kTokens) places[tid] = place_of(a, move_of(a, seq, first + tid));
+        if (tid < kTokens) places[tid] = place_of(a, first + tid < end ? move_of(a, seq, from + first + tid, to + first + tid) : Move{-1, -1});
         __syncthreads();
         for (int i0 = tid; i0 < 2 * per; i0 += 256) {
             const bool value = i0 >= per;
