@@ -529,13 +529,14 @@ __device__ __forceinline__ void tree_segment(TreeArgsAt args, const TreeSegment 
         const unsigned halves = i & 1 ? 0x07060302u : 0x05040100u;
         return Words<8>{__builtin_amdgcn_perm(vt[1][c][i / 2], vt[0][c][i / 2], halves), __builtin_amdgcn_perm(vt[3][c][i / 2], vt[2][c][i / 2], halves)};
     };
-    // Which of the keys key0..key0 + 15 row r sees, where they are in the cache.
+    // Which of the keys key0..key0 + 15 row r sees, where they are in the cache (what is no node none: no value that is
+    // not finite may mark it).
     auto sees = [&](int r, int64_t key0) {
         auto upto = [](int64_t n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << (int)n) - 1u; };  // the first n keys
         const unsigned long long bits = lds.bits[r];
         const int64_t node0 = key0 - range.length;
         const unsigned nodes = (unsigned)(node0 >= 0 ? node0 < 64 ? bits >> (int)node0 : 0 : node0 > -16 ? bits << (int)-node0 : 0);
-        const unsigned before = upto(-node0);  // the sequence's own
+        const unsigned before = bits ? upto(-node0) : 0;  // the sequence's own
         return (nodes & ~before & 0xffffu) | (before & (~upto(lds.low[r] - key0) | upto(all_sinks - key0)));
     };
     // Takes values that are not finite out of a tile whose rows do not see the same keys, and marks the rows that see

@@ -108,6 +108,29 @@ def test_values_that_are_not_finite(x, cache, d, nodes, hq, hk):
         check_marks(c, f"{what}: {nodes} nodes of ({hq},{hk})x{d}, {x} over {cache}", **kw)
 
 
+@pytest.mark.parametrize("x,cache", PAIRS, ids=str)
+@pytest.mark.parametrize("nodes,hq,hk", [(5, 4, 2), (25, 8, 2)])
+@pytest.mark.parametrize("d", [64, 80, 256])
+def test_rows_of_no_node_beside_values_that_are_not_finite(x, cache, nodes, hq, hk, d):
+    """What is no node gives 0 and -infinity, whatever lies in the keys of the sequence and in those before its window."""
+    ilpm = lib()
+    g = gen(nodes + d)
+    parents = [[-1, 0, -2] + [-2 if i % 2 else 1 for i in range(3, nodes)], [-2] * nodes, [2] + [0] * (nodes - 1)]
+    none = torch.tensor([[a is None for a in ref.above(row)] for row in parents]).view(-1)
+    for length in (9, 120):
+        for window in (0, 1, 4):
+            for extra in (0, 100):
+                c = attn_case(g, [length, length - 3, length // 2], parents, hq, hk, d, x, cache, 16, extra=extra)
+                c["vp"][:, :, :, d - 1], c["vp"][:, :, :, 1] = math.nan, math.inf
+                t = {k: v.cuda() for k, v in c.items()}
+                note(f"[no nodes] {length} + {nodes}, window {window}, extra {extra}")
+                got, lse = ilpm.attn_tree(t["q"], t["kp"], t["vp"], t["table"], t["lengths"], t["parents"], window=window, return_lse=True)
+                torch.cuda.synchronize()
+                assert (got.cpu()[none] == 0).all() and (lse.cpu()[none] == -math.inf).all()
+                assert torch.isnan(got.cpu()[~none][:, :, d - 1]).all() and torch.isfinite(lse.cpu()[~none]).all()
+                assert torch.isfinite(got.cpu()[~none][:, :, 2:d - 1]).all()
+
+
 # ---- splits ----
 
 @pytest.mark.parametrize("x,cache", [(BF16, BF16), (F32, BF16), (F16, F16)], ids=str)
