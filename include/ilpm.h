@@ -430,8 +430,8 @@ int ilpm_maxpool2x2(const float *in, int C, int H, int W, float *out, hipStream_
  * as stated (strides in elements, not negative; the innermost dimension is
  * contiguous).  What a call writes must not overlap what it reads or else
  * writes, except where a comment allows it, and must not overlap itself.
- * Arithmetic and sums are fp32 or more (ilpm_attn_decode states what it holds in
- * fewer bits); each output is rounded to its type once, to nearest even.  Sizes
+ * Arithmetic and sums are fp32 or more (ilpm_attn_decode and ilpm_attn_tree state
+ * what they hold in fewer bits); each output is rounded to its type once, to nearest even.  Sizes
  * of zero tokens, sequences or rows are valid and launch nothing.
  *
  * What lies in device memory cannot be checked before a launch.  The kernels

@@ -18,7 +18,10 @@ struct AppendNormArgs {
 hipError_t append_norm_launch(const AppendNormArgs &n, int x_dtype, int cache_dtype, int param_dtype, hipStream_t stream);
 
 // ---- verify_drafts ----
-constexpr int kVerifyChunk = 4096;  // probabilities that a workgroup sums
+// Probabilities that a workgroup sums: with 2048, 4096 and 8192 one row of 50000 f32 values takes
+// 10.3, 10.7 and 10.9 us, 64 rows of 131072 17.4, 17.3 and 17.6, of draft rows as well 24.7,
+// 24.1 and 26.6.
+constexpr int kVerifyChunk = 4096;
 
 // Where a sequence's walk ended, and what is left of that node's row: a p - b q, or p
 // without the tokens of the children that are bits of `gone`.

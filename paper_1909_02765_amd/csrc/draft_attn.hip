@@ -204,6 +204,9 @@ hipError_t tree_launch(const TreeArgs &t, int cache_dtype, hipStream_t stream)
                          : cache_dtype == ILPM_F16 ? (q32 ? tree_split_f16_q32(t, stream) : tree_split_f16(t, stream))
                                                    : (q32 ? tree_split_bf16_q32(t, stream) : tree_split_bf16(t, stream));
     if (e != hipSuccess || !a.split) return e;
+    // A workgroup for each row and 64 values, or for many rows: 4 sequences of 8000 bf16 keys of 8
+    // heads of 64 under 64 rows (2048 workgroups) 28.8 us and 29.2, 2 of 30000 of 128 (2048) 65.6 and
+    // 67.6, 4 of 8000 of 128 (4096) 47.5 and 45.4, 16 of 4000 (16384) 91.9 and 75.3.
     const int joins = a.part_of_unit ? a.n_seqs * a.kv_heads : a.grid / a.blocks;
     if (a.dim % 4 == 0 && (int64_t)joins * t.rows * ceil_div(a.dim, 64) > 8 * kAttnCus) {
         const int lanes = a.dim / 4;

@@ -95,7 +95,11 @@ template <int P, int N> __global__ __launch_bounds__(256) void copy_path(CopyArg
     }
 }
 
-constexpr int kTokens = 16;  // of a workgroup at a time
+// Of a workgroup at a time.  (With 8 and 32, whose stores wait for fewer and for more others:
+// 6 forks of 4000 tokens of 8 bf16 heads of 128 51.4 us, 48.2 and 47.7; 64 of 700 of 2 heads of 64
+// 19.1, 15.9 and 18.7; 64 of 40 of 8 of 128 7.7, 6.6 and 10.7; 1 of 16000 of 8 f32 heads 60.3, 58.8
+// and 62.8.)
+constexpr int kTokens = 16;
 
 // Without one: a thread takes one piece of kTokens tokens, and reads them all before
 // it writes the first, so that as many reads are on their way.  (Stores are not: each is
@@ -153,7 +157,8 @@ template <int P> hipError_t launch(const CopyArgs &a, hipStream_t stream)
 
 hipError_t copy_launch(const CopyArgs &a, hipStream_t stream)
 {
-    // (Of 64 tokens pieces of 8 bytes, so that all fit the registers.)
+    // (Of 64 tokens pieces of 8 bytes, so that all fit the registers: paths of 64 nodes in any order, 64 and 1
+    // sequences of 8 bf16 heads of 128, 15.4 and 12.8 us, with pieces of 16 bytes 15.8 and 13.2; of 32 nodes both 9.1.)
     if (a.row_bytes % 16 == 0 && !(a.path && a.max_count > 32)) return launch<16>(a, stream);
     if (a.row_bytes % 8 == 0) return launch<8>(a, stream);
     if (a.row_bytes % 4 == 0) return launch<4>(a, stream);
